@@ -40,7 +40,8 @@
  *    e = min(22, 39 - ceil(log2 n)), outside the range in which the int64
  *    fixed-point sums of the k-means means are exact (2^22 for n <= 2^17,
  *    2^15 at n = 2^24), also set for non-finite input; bit 2: an initial
- *    row index out of range, replaced by the default row).  The inputs are
+ *    row index out of range, replaced by the default row; bit 3: a key set
+ *    that is not strictly ascending in [0, n), call 7).  The inputs are
  *    checked in the first update pass of calls 1 and 2.  Nothing aborts or
  *    prints.
  *  - Determinism: every output is bitwise reproducible run to run and
@@ -337,6 +338,90 @@ int32_t scope_sparse_attention_noalloc(const scope_shape *shape,
                                        const int32_t *sel_counts,
                                        const int32_t *sel_idx, float scale,
                                        void *o, void *stream);
+
+/* Training through the layer: calls 1-4 decide index sets, which have no
+ * gradient; the attention over them is differentiable in Q, K and V.
+ *
+ * Dropout, in the calls that take `dropout` and `rng`: each probability (or
+ * element) is kept or dropped on its own and the kept ones are scaled by
+ * 1 / (1 - p'), where p' = T / 65536, T = min(65535, rint(65536 * dropout)).
+ * No mask is stored: `rng` (device, two uint64: seed and offset, read when the
+ * kernels run, so a captured graph draws new masks when the caller writes new
+ * values between replays) keys Philox4x32-10, and a backward call with the
+ * same rng values repeats the forward's mask.  Calls that must not share a mask
+ * (layers, steps, GPUs that hold other heads) need different seeds or offsets;
+ * attention and scope_dropout draw from separate streams of one (seed, offset).
+ *   pairs:    (a0, a1) = the first two words of Philox with key = seed and
+ *             counter (i, 2^31 + 2h, offset low, offset high) for query token
+ *             i of head h, (b0, b1) of (j, 2^31 + 2h + 1, offset low, offset
+ *             high) for key token j; z = upper xor lower word of the 64-bit
+ *             product (a0 xor b0) * ((a1 + b1) mod 2^32); kept if z >> 16 >= T
+ *   elements: Philox of counter (e / 8 low, e / 8 high, offset low, offset
+ *             high) gives element e's eight neighbours a 16-bit number each,
+ *             low halves first; kept if it is >= T
+ * 0 <= dropout < 1, else SCOPE_ERR_INVALID_ARGUMENT; rng is 8-byte aligned and
+ * may be NULL where T = 0.
+ *
+ * Workspace bytes that suffice for calls 6 and 7 with these sizes (the ranges
+ * of the shape are checked and not used).                                   */
+int32_t scope_training_workspace_size(const scope_shape *shape, int32_t c_q,
+                                      size_t *bytes);
+
+/* 6. Attention for training.  As call 5, with the rows' statistics and dropout:
+ *   lse_i = log sum_{j in S_c} exp(scale <q_i, k_j>)        (fp32, natural log)
+ *   O_i   = sum_{j in S_c} exp(scale <q_i, k_j> - lse_i) m_ij v_j,
+ * m_ij the dropout factor of the pair (0 or 1 / (1 - p')).  bf16 inputs run on
+ * the bf16 matrix cores with the weights rounded to bf16; fp32 inputs are not
+ * rounded (fp32 matrix products), unlike call 5's.  Sums and statistics are
+ * fp32.  A cluster without keys gives O = 0 and lse = -inf.  Rows of queries in
+ * no cluster are left as they were, in O and lse [heads][n].
+ * S_c must be strictly ascending (as call 4 writes it): a key counts once.
+ * Requirements and errors as call 5, and SCOPE_ERR_UNSUPPORTED for c_q > 1024;
+ * the outputs must not overlap the inputs or each other.                    */
+int32_t scope_sparse_attention_train(const scope_shape *shape, const void *q,
+                                     const void *k, const void *v, int32_t c_q,
+                                     const int32_t *offsets,
+                                     const int32_t *perm,
+                                     const int32_t *sel_counts,
+                                     const int32_t *sel_idx, float scale,
+                                     float dropout, const uint64_t *rng,
+                                     void *o, float *lse, void *workspace,
+                                     size_t ws_bytes, void *stream);
+
+/* 7. Gradients of call 6.  From its inputs, its O and lse, and d_o, the
+ * gradient of O (of the input dtype, [heads][n][d]), with the probabilities
+ * recomputed from lse:
+ *   p_ij = exp(scale <q_i, k_j> - lse_i), D_i = <d_o_i, O_i>
+ *   ds_ij = p_ij (m_ij <d_o_i, v_j> - D_i)
+ *   dQ_i = scale sum_j ds_ij k_j, dK_j = scale sum_i ds_ij q_i,
+ *   dV_j = sum_i p_ij m_ij d_o_i,
+ * j over S_c and i over the queries whose cluster keeps j.  Types as call 6:
+ * for bf16 inputs p and ds enter the matrix products rounded to bf16, every sum
+ * is fp32.  dK and dV are written for every key (0 where no cluster keeps it),
+ * dQ for every query in a cluster (0 where its cluster keeps no key); rows of
+ * queries in no cluster are left as they were and give no gradient.  Bad sets
+ * cannot fault: a set that is not strictly ascending in [0, n) sets bit 3 of
+ * dev_status (may be NULL) and its gradients are unspecified.  Requirements and
+ * errors as call 6.                                                         */
+int32_t scope_sparse_attention_backward(
+    const scope_shape *shape, const void *q, const void *k, const void *v,
+    const void *o, const float *lse, const void *d_o, int32_t c_q,
+    const int32_t *offsets, const int32_t *perm, const int32_t *sel_counts,
+    const int32_t *sel_idx, float scale, float dropout, const uint64_t *rng,
+    void *dq, void *dk, void *dv, void *workspace, size_t ws_bytes,
+    int32_t *dev_status, void *stream);
+
+/* 8. Dropout of a tensor of `count` elements (0 <= count <= 2^40) of a
+ * scope_dtype, with an optional residual (NULL: none):
+ *   y_e = x_e / (1 - p') where kept, else 0, plus residual_e,
+ * computed in fp32 and rounded once.  A dropped element gives 0 whatever x_e is
+ * (infinities and NaN among it).  The gradient of x is the same call on the
+ * gradient of y with the same rng and no residual.  y may be x or the residual;
+ * otherwise they must not overlap.  Pointers are aligned to their elements
+ * (16-byte alignment of all is faster, the results are the same).           */
+int32_t scope_dropout(int32_t dtype, int64_t count, const void *x,
+                      const void *residual, float dropout, const uint64_t *rng,
+                      void *y, void *stream);
 
 /* Diagnostics: the measured peaks that roofline fractions are also quoted
  * against.  scope_debug_copy copies `bytes` (a multiple of 16; src and dst

@@ -29,6 +29,8 @@ ENTRY_POINTS = (
     "scope_sparse_attention_noalloc", "scope_debug_copy", "scope_debug_mfma_loop",
     "scope_cluster_queries_warm", "scope_cluster_key_subspaces_warm",
     "scope_debug_attention_items",
+    "scope_training_workspace_size", "scope_sparse_attention_train",
+    "scope_sparse_attention_backward", "scope_dropout",
 )
 MAX_SUBSPACES, MAX_D = 8, 128
 POLICIES = {"online": 0, "fixed": 1, "topp": 2}
@@ -121,6 +123,13 @@ def lib() -> ctypes.CDLL:
         L.scope_proxy_scores_partition.argtypes = [SP, P, I, P, PP, P, P, P, P, Z, P]
         L.scope_select_partition.argtypes = [SP, I, PP, P, P, P, P, ctypes.c_float, I,
                                              P, P, P, P, P, P, Z, I, P]
+        F = ctypes.c_float
+        L.scope_training_workspace_size.argtypes = [SP, I, ctypes.POINTER(Z)]
+        L.scope_sparse_attention_train.argtypes = [SP, P, P, P, I, P, P, P, P, F, F, P,
+                                                   P, P, P, Z, P]
+        L.scope_sparse_attention_backward.argtypes = [SP, P, P, P, P, P, P, I, P, P, P, P, F, F,
+                                                      P, P, P, P, P, Z, P, P]
+        L.scope_dropout.argtypes = [I, ctypes.c_int64, P, P, F, P, P, P]
         for name in ENTRY_POINTS[2:]:
             getattr(L, name).restype = I
         _lib = L
@@ -320,6 +329,95 @@ def scope_sparse_attention_noalloc(shape, q, k, v, c_q, offsets, perm, sel_count
         _ptr(sel_counts, torch.int32, H * c_q, "sel_counts"),
         _ptr(sel_idx, torch.int32, H * c_q * N, "sel_idx"), float(scale),
         _ptr(o, dt, H * N * D, "o"), _stream(stream)))
+
+
+def scope_training_workspace_size(shape: Shape, c_q: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check("scope_training_workspace_size", lib().scope_training_workspace_size(
+        ctypes.byref(shape), int(c_q), ctypes.byref(out)))
+    return int(out.value)
+
+
+def alloc_training_workspace(shape: Shape, c_q: int, device="cuda"):
+    """A uint8 workspace tensor for the training calls."""
+    return torch.empty(max(scope_training_workspace_size(shape, c_q), 1),
+                       dtype=torch.uint8, device=device)
+
+
+def _on_device(call, stream, *tensors):
+    """Runs call(stream pointer) with the tensors' device current: the current
+    stream is that device's, and all tensors have to be on it."""
+    tensors = [t for t in tensors if t is not None]
+    dev = tensors[0].device
+    for t in tensors:
+        if t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device}")
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"tensors on {dev}, the stream on {stream.device}")
+    if dev.index == torch.cuda.current_device():
+        return call(_stream(stream))
+    with torch.cuda.device(dev):
+        return call(_stream(stream))
+
+
+def _rng(rng, dropout):
+    if rng is None and float(dropout) != 0.0:
+        raise ValueError("dropout needs rng: an int64 tensor (seed, offset) on the GPU")
+    return _ptr(rng, torch.int64, 2, "rng", optional=True)
+
+
+def scope_sparse_attention_train(shape, q, k, v, c_q, offsets, perm, sel_counts, sel_idx, scale,
+                                 dropout, rng, o, lse, workspace, stream=None):
+    H, N, D = shape.heads, shape.n, shape.d
+    dt = _data_dtype(shape)
+    args = (ctypes.byref(shape), _ptr(q, dt, H * N * D, "q"), _ptr(k, dt, H * N * D, "k"),
+            _ptr(v, dt, H * N * D, "v"), int(c_q),
+            _ptr(offsets, torch.int32, H * (c_q + 1), "offsets"),
+            _ptr(perm, torch.int32, H * N, "perm"),
+            _ptr(sel_counts, torch.int32, H * c_q, "sel_counts"),
+            _ptr(sel_idx, torch.int32, H * c_q * N, "sel_idx"), float(scale), float(dropout),
+            _rng(rng, dropout), _ptr(o, dt, H * N * D, "o"), _ptr(lse, torch.float32, H * N, "lse"),
+            _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel())
+    _check("scope_sparse_attention_train", _on_device(
+        lambda s: lib().scope_sparse_attention_train(*args, s), stream,
+        q, k, v, offsets, perm, sel_counts, sel_idx, rng, o, lse, workspace))
+
+
+def scope_sparse_attention_backward(shape, q, k, v, o, lse, d_o, c_q, offsets, perm, sel_counts,
+                                    sel_idx, scale, dropout, rng, dq, dk, dv, workspace,
+                                    dev_status=None, stream=None):
+    H, N, D = shape.heads, shape.n, shape.d
+    dt = _data_dtype(shape)
+    data = {name: _ptr(t, dt, H * N * D, name) for name, t in
+            (("q", q), ("k", k), ("v", v), ("o", o), ("d_o", d_o), ("dq", dq), ("dk", dk),
+             ("dv", dv))}
+    args = (ctypes.byref(shape), data["q"], data["k"], data["v"], data["o"],
+            _ptr(lse, torch.float32, H * N, "lse"), data["d_o"], int(c_q),
+            _ptr(offsets, torch.int32, H * (c_q + 1), "offsets"),
+            _ptr(perm, torch.int32, H * N, "perm"),
+            _ptr(sel_counts, torch.int32, H * c_q, "sel_counts"),
+            _ptr(sel_idx, torch.int32, H * c_q * N, "sel_idx"), float(scale), float(dropout),
+            _rng(rng, dropout), data["dq"], data["dk"], data["dv"],
+            _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel(),
+            _ptr(dev_status, torch.int32, 1, "dev_status", optional=True))
+    _check("scope_sparse_attention_backward", _on_device(
+        lambda s: lib().scope_sparse_attention_backward(*args, s), stream,
+        q, k, v, o, lse, d_o, offsets, perm, sel_counts, sel_idx, rng, dq, dk, dv, workspace,
+        dev_status))
+
+
+def scope_dropout(x, residual, dropout, rng, y, stream=None):
+    """y = dropout(x) + residual, elementwise over x's elements."""
+    if x.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"x must be bfloat16 or float32, got {x.dtype}")
+    for t, name in ((residual, "residual"), (y, "y")):
+        if t is not None and t.numel() != x.numel():
+            raise ValueError(f"{name} needs {x.numel()} elements, has {t.numel()}")
+    args = (BF16 if x.dtype == torch.bfloat16 else F32, x.numel(), _ptr(x, None, None, "x"),
+            _ptr(residual, x.dtype, None, "residual", optional=True), float(dropout),
+            _rng(rng, dropout), _ptr(y, x.dtype, None, "y"))
+    _check("scope_dropout", _on_device(lambda s: lib().scope_dropout(*args, s), stream,
+                                       x, residual, rng, y))
 
 
 def scope_debug_copy(src, dst, stream=None):

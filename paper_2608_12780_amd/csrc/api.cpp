@@ -6,6 +6,8 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <initializer_list>
+
 #include "../../include/scope.h"
 #include "kernels.h"
 
@@ -876,6 +878,54 @@ float attention_scale(const scope_shape *shape, float scale) {
                       : static_cast<float>(1.0 / sqrt(static_cast<double>(shape->d)));
 }
 
+// The dropout threshold in the upper 16 bits of *drop.
+int32_t check_dropout(float p, const uint64_t *rng, uint32_t *drop) {
+  if (!(p >= 0.0f && p < 1.0f)) return SCOPE_ERR_INVALID_ARGUMENT;
+  const double t = rint(static_cast<double>(p) * 65536.0);
+  *drop = static_cast<uint32_t>(t < 65535.0 ? t : 65535.0) << 16;
+  if (*drop && !rng) return SCOPE_ERR_INVALID_ARGUMENT;
+  if (reinterpret_cast<uintptr_t>(rng) % 8) return SCOPE_ERR_INVALID_ARGUMENT;
+  return SCOPE_OK;
+}
+
+// Whether one of the first `outs` arrays overlaps another (arrays of one size).
+bool outputs_overlap(const scope_shape *s, int outs, std::initializer_list<const void *> arrays) {
+  const uintptr_t bytes = static_cast<uintptr_t>(s->heads) * s->n * s->d * (s->dtype == SCOPE_BF16 ? 2 : 4);
+  int i = 0;
+  for (const void *p : arrays) {
+    if (i++ >= outs) break;
+    int j = 0;
+    for (const void *q : arrays) {
+      const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+      if (j++ != i - 1 && a < b + bytes && b < a + bytes) return true;
+    }
+  }
+  return false;
+}
+
+void set_train(const scope_shape *s, const void *q, const void *k, const void *v, int32_t c_q,
+               const int32_t *offsets, const int32_t *perm, const int32_t *sel_counts,
+               const int32_t *sel_idx, float scale, uint32_t drop, const uint64_t *rng, float *lse,
+               void *workspace, scope::TrainArgs *a, scope::TrainCall *c) {
+  a->n = s->n;
+  a->c_q = c_q;
+  a->q = q;
+  a->k = k;
+  a->v = v;
+  a->offsets = offsets;
+  a->perm = perm;
+  a->sel_counts = sel_counts;
+  a->sel_idx = sel_idx;
+  a->scale = attention_scale(s, scale);
+  a->scale_log2 = a->scale * 1.4426950408889634f;
+  a->drop = drop;
+  a->kept_scale = 65536.0f / static_cast<float>(65536u - (drop >> 16));
+  a->lse = lse;
+  c->heads = s->heads;
+  c->rng = rng;
+  scope::train_workspace(s->heads, s->n, c_q, workspace, a, c);
+}
+
 }  // namespace
 
 extern "C" {
@@ -924,6 +974,96 @@ int32_t scope_sparse_attention(const scope_shape *shape, const void *q,
                                  offsets, perm, sel_counts, sel_idx,
                                  attention_scale(shape, scale), w,
                                  static_cast<hipStream_t>(stream)));
+  return SCOPE_OK;
+}
+
+int32_t scope_training_workspace_size(const scope_shape *shape, int32_t c_q, size_t *bytes) {
+  int32_t st = check_shape(shape);
+  if (st) return st;
+  if ((st = check_cq(shape, c_q))) return st;
+  if (shape->d != 64 && shape->d != 128) return SCOPE_ERR_UNSUPPORTED;
+  if (!bytes) return SCOPE_ERR_INVALID_ARGUMENT;
+  *bytes = scope::train_workspace(shape->heads, shape->n, c_q, nullptr, nullptr, nullptr);
+  return SCOPE_OK;
+}
+
+int32_t scope_sparse_attention_train(const scope_shape *shape, const void *q, const void *k,
+                                     const void *v, int32_t c_q, const int32_t *offsets,
+                                     const int32_t *perm, const int32_t *sel_counts,
+                                     const int32_t *sel_idx, float scale, float dropout,
+                                     const uint64_t *rng, void *o, float *lse, void *workspace,
+                                     size_t ws_bytes, void *stream) {
+  int32_t st = check_attention(shape, q, k, v, c_q, offsets, perm, sel_counts, sel_idx, scale, o);
+  if (st) return st;
+  if (c_q > scope::kTrainMaxClusters) return SCOPE_ERR_UNSUPPORTED;
+  if (!lse || reinterpret_cast<uintptr_t>(lse) % 4) return SCOPE_ERR_INVALID_ARGUMENT;
+  if (outputs_overlap(shape, 1, {o, q, k, v})) return SCOPE_ERR_INVALID_ARGUMENT;
+  uint32_t drop = 0;
+  if ((st = check_dropout(dropout, rng, &drop))) return st;
+  scope::TrainArgs a{};
+  scope::TrainCall c{};
+  if ((st = check_ws(workspace, ws_bytes,
+                     scope::train_workspace(shape->heads, shape->n, c_q, nullptr, nullptr, nullptr))))
+    return st;
+  set_train(shape, q, k, v, c_q, offsets, perm, sel_counts, sel_idx, scale, drop, rng, lse,
+            workspace, &a, &c);
+  c.o = o;
+  SCOPE_TRY(scope::train_forward(shape->d, shape->dtype == SCOPE_BF16, a, c,
+                                 static_cast<hipStream_t>(stream)));
+  return SCOPE_OK;
+}
+
+int32_t scope_sparse_attention_backward(
+    const scope_shape *shape, const void *q, const void *k, const void *v, const void *o,
+    const float *lse, const void *d_o, int32_t c_q, const int32_t *offsets, const int32_t *perm,
+    const int32_t *sel_counts, const int32_t *sel_idx, float scale, float dropout,
+    const uint64_t *rng, void *dq, void *dk, void *dv, void *workspace, size_t ws_bytes,
+    int32_t *dev_status, void *stream) {
+  int32_t st = check_attention(shape, q, k, v, c_q, offsets, perm, sel_counts, sel_idx, scale, o);
+  if (st) return st;
+  if (c_q > scope::kTrainMaxClusters) return SCOPE_ERR_UNSUPPORTED;
+  if (!lse || reinterpret_cast<uintptr_t>(lse) % 4) return SCOPE_ERR_INVALID_ARGUMENT;
+  for (const void *p : {d_o, static_cast<const void *>(dq), static_cast<const void *>(dk),
+                        static_cast<const void *>(dv)})
+    if (!p || reinterpret_cast<uintptr_t>(p) % 16) return SCOPE_ERR_INVALID_ARGUMENT;
+  if (outputs_overlap(shape, 3, {dq, dk, dv, q, k, v, o, d_o})) return SCOPE_ERR_INVALID_ARGUMENT;
+  uint32_t drop = 0;
+  if ((st = check_dropout(dropout, rng, &drop))) return st;
+  scope::TrainArgs a{};
+  scope::TrainCall c{};
+  if ((st = check_ws(workspace, ws_bytes,
+                     scope::train_workspace(shape->heads, shape->n, c_q, nullptr, nullptr, nullptr))))
+    return st;
+  set_train(shape, q, k, v, c_q, offsets, perm, sel_counts, sel_idx, scale, drop, rng,
+            const_cast<float *>(lse), workspace, &a, &c);
+  a.d_o = d_o;
+  c.o = const_cast<void *>(o);
+  c.dq = dq;
+  c.dk = dk;
+  c.dv = dv;
+  c.status = dev_status;
+  SCOPE_TRY(scope::train_backward(shape->d, shape->dtype == SCOPE_BF16, a, c,
+                                  static_cast<hipStream_t>(stream)));
+  return SCOPE_OK;
+}
+
+int32_t scope_dropout(int32_t dtype, int64_t count, const void *x, const void *residual,
+                      float dropout, const uint64_t *rng, void *y, void *stream) {
+  if (dtype != SCOPE_F32 && dtype != SCOPE_BF16) return SCOPE_ERR_UNSUPPORTED;
+  if (count < 0) return SCOPE_ERR_INVALID_ARGUMENT;
+  if (count > (1ll << 40)) return SCOPE_ERR_UNSUPPORTED;
+  uint32_t drop = 0;
+  const int32_t st = check_dropout(dropout, rng, &drop);
+  if (st) return st;
+  if (count == 0) return SCOPE_OK;
+  const uintptr_t size = dtype == SCOPE_BF16 ? 2 : 4, bytes = size * count;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y),
+                  r = reinterpret_cast<uintptr_t>(residual);
+  if (!x || !y || a % size || b % size || r % size) return SCOPE_ERR_INVALID_ARGUMENT;
+  if (a != b && a < b + bytes && b < a + bytes) return SCOPE_ERR_INVALID_ARGUMENT;
+  if (r && r != b && r < b + bytes && b < r + bytes) return SCOPE_ERR_INVALID_ARGUMENT;
+  SCOPE_TRY(scope::dropout_run(dtype == SCOPE_BF16, count, x, residual, drop >> 16, rng, y,
+                               static_cast<hipStream_t>(stream)));
   return SCOPE_OK;
 }
 

@@ -25,47 +25,17 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "mfma.h"
 
 namespace scope {
 
 namespace {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
 constexpr int kBN = 64;          // keys per tile
 constexpr int kNW = 8;           // waves per block
 constexpr int kQB = 1;           // 32-query column blocks per wave
 constexpr int kBM = 32 * kQB * kNW;
 constexpr float kRescale = 8.0f; // lazy rescale: running max may lag by 2^8
-
-__device__ __forceinline__ bf16x8 as_bf16x8(uint4 u) {
-  return __builtin_bit_cast(bf16x8, u);
-}
-
-// Two floats -> packed bf16 (round to nearest even, v_cvt_pk_bf16_f32).
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  bf16x2 r;
-  r[0] = static_cast<__bf16>(a);
-  r[1] = static_cast<__bf16>(b);
-  return __builtin_bit_cast(uint32_t, r);
-}
-
-// 8 consecutive input elements as packed bf16.
-template <bool BF16IN>
-__device__ __forceinline__ uint4 load8(const void *base, size_t elem) {
-  if (BF16IN) {
-    return *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(base) + elem);
-  } else {
-    const float4 a = *reinterpret_cast<const float4 *>(static_cast<const float *>(base) + elem);
-    const float4 b = *reinterpret_cast<const float4 *>(static_cast<const float *>(base) + elem + 4);
-    return make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y),
-                      pack_bf16(b.z, b.w));
-  }
-}
 
 // Work slots run in list order: heads one after the other and, within a
 // head, by estimated cost, largest first, with a cluster's row chunks

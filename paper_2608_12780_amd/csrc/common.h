@@ -18,6 +18,7 @@ constexpr int kWave = 64;
 constexpr int kStatusNonFinite = 1;
 constexpr int kStatusRange = 2;
 constexpr int kStatusBadInit = 4;
+constexpr int kStatusBadSet = 8;
 
 // Element loads: bf16 storage widens exactly to fp32.
 __device__ __forceinline__ float bf16_to_f32(uint16_t b) {

@@ -257,4 +257,38 @@ bool attention_copies_kv(int n, int d, int c_q, bool bf16);
 bool attention_ordered(int heads, int n, int d, int c_q);
 size_t attention_order_entries(int heads, int n, int d, int c_q);
 
+// Attention for training (attention_train.hip).  TrainArgs goes to the kernels;
+// TrainCall holds what the host needs besides.
+constexpr int kTrainMaxClusters = 1024;
+struct TrainArgs {
+  int n, c_q, items_per_head;
+  const void *q, *k, *v, *d_o;
+  const int32_t *offsets, *perm, *sel_counts, *sel_idx;
+  float scale, scale_log2;
+  uint32_t drop;           // dropout threshold in the upper 16 bits, 0: none
+  float kept_scale;        // 1 / (1 - p), p the threshold's probability
+  float *lse;
+  const int4 *items;
+  const uint2 *words;      // [heads][query, key][n]
+  const float2 *stats;     // [heads][n]
+  const uint32_t *masks;   // [heads][ceil(n / 32)][c_q]
+};
+struct TrainCall {
+  int heads;
+  const uint64_t *rng;
+  void *o, *dq, *dk, *dv;
+  int4 *items, *tiles;
+  int32_t *status;
+};
+int train_items_per_head(int n, int c_q, int rows);
+// Lays the workspace out (base null: only its size).
+size_t train_workspace(int heads, int n, int c_q, void *base, TrainArgs *a, TrainCall *c);
+hipError_t train_forward(int d, bool bf16, const TrainArgs &a, const TrainCall &c, hipStream_t s);
+hipError_t train_backward(int d, bool bf16, const TrainArgs &a, const TrainCall &c, hipStream_t s);
+
+// Dropout of `count` elements (dropout.hip): y = x kept / (1 - p) + residual
+// (residual null: none); threshold as TrainArgs::drop.
+hipError_t dropout_run(bool bf16, int64_t count, const void *x, const void *residual,
+                       uint32_t threshold, const uint64_t *rng, void *y, hipStream_t s);
+
 }  // namespace scope

@@ -4,6 +4,11 @@ ScopeLayer owns every output and the workspace for one problem size and runs
 Alg. 1 end to end through the C ABI: query clustering, key-subspace
 clustering, score tables, selection and sparse attention.  Nothing here
 computes; it allocates device memory and sequences the calls.
+
+For training, TrainingAttention holds the buffers of the attention with row
+statistics and of its gradients, ScopeLayer.attention and
+DenseAttention.attention are differentiable in q, k and v, dropout in its input
+and residual, and ScopeLayer.forward_train runs the layer with both.
 """
 from __future__ import annotations
 
@@ -12,7 +17,145 @@ import torch
 from . import binding as B
 
 
-class ScopeLayer:
+class TrainingAttention:
+    """Attention over given clusters and key sets with the rows' log-sum-exp
+    (call 6) and its gradients (call 7), on buffers allocated once.  `dropout`
+    drops attention probabilities; `rng` is an int64 tensor (seed, offset) on
+    the GPU, the same in backward as in forward."""
+
+    def __init__(self, heads, n, d, c_q, dtype="bf16", device="cuda"):
+        self.heads, self.n, self.d, self.c_q = int(heads), int(n), int(d), int(c_q)
+        self.dtype = B.BF16 if dtype == "bf16" else B.F32
+        self.tdtype = torch.bfloat16 if self.dtype == B.BF16 else torch.float32
+        self.shape = B.make_shape(heads, n, d, self.dtype, _dummy_ranges(self.d))
+        self.device = torch.device(device)
+        self.workspace = B.alloc_training_workspace(self.shape, self.c_q, device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self._out = self._grads = None
+
+    def _rows(self):
+        return torch.empty(self.heads, self.n, self.d, dtype=self.tdtype, device=self.device)
+
+    def outputs(self):
+        """New (out, lse) buffers."""
+        return self._rows(), torch.empty(self.heads, self.n, dtype=torch.float32,
+                                         device=self.device)
+
+    def gradients(self):
+        """New (dq, dk, dv) buffers."""
+        return self._rows(), self._rows(), self._rows()
+
+    def forward(self, q, k, v, offsets, perm, sel_counts, sel_idx, scale=0.0, dropout=0.0,
+                rng=None, into=None, stream=None):
+        """Returns (out, lse): `into`, or the buffers this object holds."""
+        if into is None:
+            self._out = into = self._out or self.outputs()
+        B.scope_sparse_attention_train(self.shape, q, k, v, self.c_q, offsets, perm, sel_counts,
+                                       sel_idx, scale, dropout, rng, *into, self.workspace, stream)
+        return into
+
+    def backward(self, q, k, v, out, lse, d_out, offsets, perm, sel_counts, sel_idx, scale=0.0,
+                 dropout=0.0, rng=None, into=None, stream=None):
+        """Returns (dq, dk, dv): `into`, or the buffers this object holds."""
+        if into is None:
+            self._grads = into = self._grads or self.gradients()
+        B.scope_sparse_attention_backward(self.shape, q, k, v, out, lse, d_out, self.c_q, offsets,
+                                          perm, sel_counts, sel_idx, scale, dropout, rng, *into,
+                                          self.workspace, self.status, stream)
+        return into
+
+
+class _AttentionFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, owner, sets, scale, dropout, rng):
+        attention = owner.training_attention()
+        # the mask belongs to the values that rng holds now
+        rng = rng.clone() if rng is not None else None
+        out, lse = attention.forward(q, k, v, *sets, scale, dropout, rng,
+                                     into=attention.outputs())
+        ctx.save_for_backward(q, k, v, out, lse, *sets, *(() if rng is None else (rng,)))
+        ctx.owner, ctx.scale, ctx.dropout = owner, scale, dropout
+        ctx.selection = owner.selection
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_out):
+        q, k, v, out, lse, offsets, perm, sel_counts, sel_idx, *rng = ctx.saved_tensors
+        if ctx.owner.selection != ctx.selection:
+            raise RuntimeError("the layer's clusters or key sets changed between this attention "
+                               "and its backward pass")
+        attention = ctx.owner.training_attention()
+        grads = attention.backward(q, k, v, out, lse, d_out.contiguous(), offsets, perm,
+                                   sel_counts, sel_idx, ctx.scale, ctx.dropout,
+                                   rng[0] if rng else None, into=attention.gradients())
+        return (*grads, None, None, None, None, None)
+
+
+class _DropoutFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, p, rng):
+        rng = rng.clone() if rng is not None else None
+        ctx.save_for_backward(*(() if rng is None else (rng,)))
+        ctx.p = p
+        y = torch.empty_like(x)
+        B.scope_dropout(x, residual, p, rng, y)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_y):
+        dx = None
+        if ctx.needs_input_grad[0]:
+            d_y = d_y.contiguous()
+            dx = torch.empty_like(d_y)
+            B.scope_dropout(d_y, None, ctx.p, ctx.saved_tensors[0] if ctx.saved_tensors else None,
+                            dx)
+        return dx, d_y if ctx.needs_input_grad[1] else None, None, None
+
+
+def dropout(x, p, rng, residual=None, out=None, stream=None):
+    """x / (1 - p) where kept, else 0, plus `residual` (call 8), into `out` or a
+    new tensor; differentiable in x and residual where neither out nor stream
+    is given.  `rng` is an int64 tensor (seed, offset) on the GPU."""
+    if residual is not None and residual.shape != x.shape:
+        raise ValueError(f"residual is {tuple(residual.shape)}, x {tuple(x.shape)}")
+    if out is None and stream is None and torch.is_grad_enabled() and (
+            x.requires_grad or residual is not None and residual.requires_grad):
+        return _DropoutFunction.apply(x, residual, p, rng)
+    y = torch.empty_like(x) if out is None else out
+    B.scope_dropout(x, residual, p, rng, y, stream)
+    return y
+
+
+_dropout = dropout  # where an argument has the name
+
+
+class _Differentiable:
+    """The attention of a layer as a function that torch differentiates."""
+
+    # counts what rewrites the clusters or key sets that a backward pass reads
+    selection = 0
+    _training = None
+
+    def training_attention(self):
+        """The training calls' buffers, made on the first use."""
+        if self._training is None:
+            self._training = TrainingAttention(
+                self.heads, self.n, self.d, self.offsets.shape[1] - 1,
+                "bf16" if self.dtype == B.BF16 else "f32", self.offsets.device)
+        return self._training
+
+    def attention(self, q, k, v, scale=0.0, dropout=0.0, rng=None):
+        """Attention over the clusters and key sets that the layer holds (calls
+        6 and 7), differentiable in q, k and v.  They must not be rewritten (a
+        new clustering or selection) before the backward pass has run."""
+        return _AttentionFunction.apply(
+            q, k, v, self, (self.offsets, self.perm, self.sel_counts, self.sel_idx), float(scale),
+            float(dropout), rng)
+
+
+class ScopeLayer(_Differentiable):
     def __init__(self, heads, n, d, ranges, c_q, c_m, iters, rho, k_fix,
                  dtype="bf16", device="cuda", materialize_scores=False,
                  workspace=True):
@@ -52,6 +195,7 @@ class ScopeLayer:
     def cluster_queries(self, q, init_q=None, stream=None, warm=False, iters=None):
         """warm: start from the centroids this layer holds (calls 1w)."""
         it = self.iters if iters is None else int(iters)
+        self.selection += 1
         if warm:
             B.scope_cluster_queries_warm(self.shape, q, self.c_q, it, self.q_centroids,
                                          self.assign, self.counts, self.offsets, self.perm,
@@ -84,6 +228,7 @@ class ScopeLayer:
         """policy "online" is call 4 (Eq. 10); "fixed" and "topp" are the
         Fig. 6 variants through call 4b.  rho overrides the layer's."""
         rho = self.rho if rho is None else rho
+        self.selection += 1
         args = (self.shape, self.c_q, self.c_m,
                 self.scores if use_scores else None, self.tables,
                 self.codes, self.counts, rho, self.k_fix,
@@ -117,6 +262,23 @@ class ScopeLayer:
         if marks:
             marks(len(steps))
         return self.out
+
+    def forward_train(self, q, k, v, init_q=None, init_k=None, dropout=0.0, rng=None,
+                      residual=None, out_dropout=0.0, warm=False, warm_iters=None):
+        """The layer for training, on the current stream: clusters and key sets
+        from q and k without gradients, the attention over them with `dropout`
+        on its probabilities, then out_dropout on its output and the residual
+        added (where either is given).  Differentiable in q, k, v and residual;
+        one forward at a time: its backward pass comes before the next forward."""
+        with torch.no_grad():
+            self.cluster_queries(q.detach(), init_q, None, warm, warm_iters)
+            self.cluster_keys(k.detach(), init_k, None, warm, warm_iters)
+            self.proxy_scores()
+            self.select()
+        out = self.attention(q, k, v, 0.0, dropout, rng)
+        if residual is None and not out_dropout:
+            return out
+        return _dropout(out, out_dropout, rng, residual)
 
 
 class SparsitySchedule:
@@ -190,6 +352,7 @@ class ScopePartitionLayer(ScopeLayer):
 
     def select(self, stream=None, use_scores=False, policy="online", rho=None):
         rho = self.rho if rho is None else rho
+        self.selection += 1
         B.scope_select_partition(self.shape, self.c_q, self.part,
                                  self.scores if use_scores else None, self.tables,
                                  self.codes, self.counts, rho, self.k_fix,
@@ -198,7 +361,7 @@ class ScopePartitionLayer(ScopeLayer):
                                  policy, stream)
 
 
-class DenseAttention:
+class DenseAttention(_Differentiable):
     """Dense attention (Eq. 1) through the same attention call: one cluster
     holding every query, whose key set is every key."""
 

@@ -1,0 +1,423 @@
+"""Attention for training, its gradients and dropout on the GPU, against the
+definitions in 64 bits, within bounds derived per value."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+from paper_2608_12780_amd import binding as B  # noqa: E402
+from paper_2608_12780_amd import inputs  # noqa: E402
+from paper_2608_12780_amd.layer import (  # noqa: E402
+    DenseAttention, ScopeLayer, TrainingAttention, dropout)
+
+import gpu_harness as G  # noqa: E402
+import training_reference as R  # noqa: E402
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.lib()
+
+
+def rng_of(seed, offset):
+    return torch.tensor([seed, offset], dtype=torch.int64, device="cuda")
+
+
+POISON = 123.0
+
+
+def run(x, p=0.0, rng=None, scale=0.0, attention=None):
+    """Forward and backward on poisoned outputs."""
+    H, n, d, C, dtype = x["dims"]
+    a = attention or TrainingAttention(H, n, d, C, dtype)
+    r = rng_of(*rng) if rng else None
+    outs = [t.fill_(POISON) for t in a.outputs()]
+    o, lse = a.forward(x["q"], x["k"], x["v"], *R.sets(x), scale, p, r, into=outs)
+    grads = [t.fill_(POISON) for t in a.gradients()]
+    dq, dk, dv = a.backward(x["q"], x["k"], x["v"], o, lse, x["d_o"], *R.sets(x), scale, p, r,
+                            into=grads)
+    torch.cuda.synchronize()
+    assert int(a.status.item()) == 0
+    return dict(o=o, lse=lse, dq=dq, dk=dk, dv=dv)
+
+
+def check(x, got, p=0.0, rng=(0, 0), scale=None):
+    val, tol, held = R.reference(x, p, rng, scale, got["o"], got["lse"])
+    for a in ("o", "lse", "dq"):
+        R.assert_within(a, got[a], val[a], tol[a], held)
+        # rows of queries in no cluster stay as they were
+        assert (got[a][~held] == POISON).all(), a
+    for a in ("dk", "dv"):
+        R.assert_within(a, got[a], val[a], tol[a])
+
+
+CASES = [
+    # heads, n, d, dtype, c_q, keep, pattern
+    (1, 1, 64, "bf16", 1, 1.0, ""),
+    (2, 1, 128, "f32", 1, 1.0, ""),
+    (1, 2, 128, "bf16", 2, 0.5, ""),
+    (1, 31, 128, "bf16", 1, 1.0, ""),
+    (2, 32, 64, "bf16", 3, 0.6, ""),
+    (1, 33, 128, "f32", 4, 0.4, ""),
+    (2, 64, 128, "bf16", 1, 1.0, ""),
+    (1, 65, 64, "f32", 1, 1.0, ""),
+    (3, 127, 128, "bf16", 5, 0.3, "empty"),
+    (1, 129, 64, "bf16", 7, 0.5, "single"),
+    (2, 257, 128, "bf16", 9, 0.5, "uncovered"),
+    (1, 255, 128, "f32", 6, 0.5, "uncovered"),
+    (2, 300, 64, "bf16", 40, 0.2, "empty"),
+    (1, 513, 128, "bf16", 3, 0.7, "prefix"),
+    (2, 514, 64, "f32", 12, 0.15, "empty"),
+    (1, 700, 128, "bf16", 700, 0.1, ""),
+    (1, 1000, 128, "bf16", 1, 1.0, ""),
+    (2, 1031, 128, "bf16", 17, 0.53, "empty"),
+    (2, 1031, 64, "bf16", 17, 0.53, ""),
+    (1, 1031, 128, "f32", 17, 0.53, ""),
+    (1, 400, 64, "f32", 20, 0.3, "last"),
+    (1, 2100, 128, "bf16", 11, 0.05, ""),
+]
+
+
+@pytest.mark.parametrize("heads,n,d,dtype,c_q,keep,pattern", CASES)
+@pytest.mark.parametrize("p", [0.0, 0.2])
+def test_values_and_gradients(heads, n, d, dtype, c_q, keep, pattern, p):
+    G.say(f"[training] {heads}x{n} d={d} {dtype} c_q={c_q} keep={keep} {pattern} p={p}")
+    x = R.make(heads, n, d, dtype, c_q, keep, 3, pattern)
+    rng = (0x123456789AB, 77 + n)
+    got = run(x, p, rng)
+    check(x, got, p, rng)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale,scale_q", [(0.7, 1.0), (0.125, 40.0), (3e-3, 0.01)])
+def test_scales_and_peaked_rows(dtype, scale, scale_q):
+    x = R.make(2, 200, 64, dtype, 5, 0.5, 9, "empty", scale_q=scale_q)
+    got = run(x, scale=scale)
+    check(x, got, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_unselected_rows_are_not_read_into_results(dtype, d):
+    """NaN and infinities in K and V rows that no set holds (row 0 and the last
+    among them), and in rows of queries outside every cluster."""
+    n = 333
+    x = R.make(2, n, d, dtype, 4, 0.4, 5, "uncovered")
+    bad = [0, 7, 64, 200, n - 1]
+    sel, cnt = x["sel_idx"].cpu(), x["sel_counts"].cpu()
+    for h in range(2):
+        for c in range(4):
+            s = sel[h, c, :cnt[h, c]]
+            s = s[~torch.isin(s, torch.tensor(bad, dtype=torch.int32))]
+            sel[h, c, :] = -1
+            sel[h, c, :len(s)] = s
+            cnt[h, c] = len(s)
+    x["sel_idx"], x["sel_counts"] = sel.cuda(), cnt.cuda()
+    want = run(x, 0.1, (5, 6))
+    check(x, want, 0.1, (5, 6))
+    y = dict(x)
+    for a in ("k", "v"):
+        y[a] = x[a].clone()
+        y[a][:, bad[0::2]] = math.nan
+        y[a][:, bad[1::2]] = math.inf
+    _, held = R.allowed(x)
+    out = ~torch.from_numpy(held).cuda()
+    for a in ("q", "d_o"):
+        y[a] = x[a].clone()
+        y[a][out] = math.nan
+    got = run(y, 0.1, (5, 6))
+    for a in want:
+        assert torch.equal(got[a], want[a]), a
+
+
+def test_repeats_bit_for_bit_and_across_workspaces():
+    x = R.make(3, 1500, 128, "bf16", 24, 0.5, 2)
+    first = run(x, 0.1, (1, 2))
+    a = TrainingAttention(3, 1500, 128, 24, "bf16")
+    a.workspace.fill_(255)
+    for _ in range(3):
+        again = run(x, 0.1, (1, 2), attention=a)
+        for name in first:
+            assert torch.equal(first[name], again[name]), name
+
+
+def test_large_offsets_of_the_generator_and_different_masks():
+    x = R.make(1, 300, 64, "f32", 3, 0.6, 4)
+    seen = []
+    for rng in ((2 ** 63 - 1, 2 ** 40 + 5), (-1, 3), (0, 0), (0, 2 ** 32)):
+        got = run(x, 0.5, rng)
+        check(x, got, 0.5, tuple(v & (2 ** 64 - 1) for v in rng))
+        seen.append(got["o"])
+    for i in range(len(seen)):
+        for j in range(i):
+            assert not torch.equal(seen[i], seen[j])
+
+
+def test_gradients_against_differences():
+    """The gradient of <O, G> along random directions against central differences
+    of the fp32 forward."""
+    x = R.make(2, 150, 64, "f32", 4, 0.5, 8)
+    got = run(x, 0.15, (9, 9))
+    H, n, d, C, dtype = x["dims"]
+    a = TrainingAttention(H, n, d, C, dtype)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for name, grad in (("q", "dq"), ("k", "dk"), ("v", "dv")):
+        step = torch.randn(H, n, d, generator=g, device="cuda")
+        # about 2e-2 off in all: the fp32 rounding of 19200 values (1e-6 each, added
+        # at random, over 2 eps) and eps^2 times the sum's size; a tenth of the bound
+        eps = 2.0 ** -7
+        val = []
+        for sign in (1, -1):
+            y = dict(x, **{name: x[name] + sign * eps * step})
+            o, _ = a.forward(y["q"], y["k"], y["v"], *R.sets(x), 0.0, 0.15, rng_of(9, 9),
+                             into=a.outputs())
+            val.append(float((o.double() * x["d_o"].double()).sum()))
+        slope = (val[0] - val[1]) / (2 * eps)
+        want = float((got[grad].double() * step.double()).sum())
+        assert abs(slope - want) <= 2e-2 * float((got[grad].double() * step.double()).norm()), name
+
+
+def test_full_tokens_match_the_inference_call():
+    """Without dropout the output is the inference call's, to both calls' bounds,
+    on the layer's own clusters and key sets."""
+    cfg = inputs.LayerConfig("train", 2, (5, 19, 23), 128, (16, 56, 56), 32, 16, 3, 0.9,
+                             inputs.ceil_tenth(5 * 19 * 23), "bf16", 8, 31)
+    x = inputs.generate(cfg)
+    layer = G.make_layer(cfg, materialize=False)
+    G.run_gpu(layer, x)
+    q, k, v = G.to_device(x)
+    with torch.no_grad():
+        out = layer.attention(q, k, v)
+    err = (out.float() - layer.out.float()).abs().max().item()
+    assert err <= 2 * G.MAX_ABS, err
+
+
+# --- streams, devices and graphs --------------------------------------------------
+
+def test_other_stream():
+    x = R.make(2, 400, 128, "bf16", 6, 0.5, 12)
+    want = run(x, 0.1, (3, 4))
+    H, n, d, C, dtype = x["dims"]
+    a = TrainingAttention(H, n, d, C, dtype)
+    r = rng_of(3, 4)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    o, lse = a.forward(x["q"], x["k"], x["v"], *R.sets(x), 0.0, 0.1, r, stream=s)
+    grads = a.backward(x["q"], x["k"], x["v"], o, lse, x["d_o"], *R.sets(x), 0.0, 0.1, r, stream=s)
+    s.synchronize()
+    assert torch.equal(o[:], want["o"]) and torch.equal(lse, want["lse"])
+    for got, name in zip(grads, ("dq", "dk", "dv")):
+        assert torch.equal(got, want[name]), name
+
+
+def test_captured_and_replayed_with_new_masks():
+    """One graph of forward, backward and dropout, replayed after new inputs and
+    new rng values were written, with eager work in between."""
+    x = R.make(2, 300, 64, "bf16", 5, 0.5, 14)
+    H, n, d, C, dtype = x["dims"]
+    a = TrainingAttention(H, n, d, C, dtype)
+    r = rng_of(1, 1)
+    q, k, v, g = (x[t].clone() for t in ("q", "k", "v", "d_o"))
+    y = torch.empty_like(q)
+
+    def step():
+        o, lse = a.forward(q, k, v, *R.sets(x), 0.0, 0.3, r)
+        dropout(o, 0.2, r, residual=q, out=y)
+        a.backward(q, k, v, o, lse, g, *R.sets(x), 0.0, 0.3, r)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for t in range(4):
+        z = R.make(2, 300, 64, "bf16", 5, 0.5, 20 + t)
+        for dst, name in ((q, "q"), (k, "k"), (v, "v"), (g, "d_o")):
+            dst.copy_(z[name])
+        r.copy_(rng_of(7, t))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = dict(o=a._out[0], lse=a._out[1], dq=a._grads[0], dk=a._grads[1], dv=a._grads[2])
+        got = {name: t_.clone() for name, t_ in got.items()}
+        kept = y.clone()
+        new = dict(x, q=z["q"], k=z["k"], v=z["v"], d_o=z["d_o"])
+        want = run(new, 0.3, (7, t))
+        for name in want:
+            assert torch.equal(got[name], want[name]), (t, name)
+        assert torch.equal(kept, dropout(want["o"], 0.2, rng_of(7, t), residual=z["q"]))
+
+
+# --- autograd ------------------------------------------------------------------------
+
+def small_layer():
+    cfg = inputs.CONFIGS["tiny"]
+    x = inputs.generate(cfg)
+    layer = ScopeLayer(cfg.heads, cfg.n, cfg.d, cfg.ranges, cfg.c_q, (cfg.c_m,) * 3, cfg.iters,
+                       cfg.rho, cfg.k_fix, dtype=cfg.dtype)
+    q, k, v = (torch.from_numpy(a).cuda() for a in (x.q, x.k, x.v))
+    return layer, q, k, v, torch.from_numpy(x.init_q).cuda(), torch.from_numpy(x.init_k).cuda()
+
+
+def case_of(layer, q, k, v, d_o):
+    x = dict(q=q, k=k, v=v, d_o=d_o, dims=(layer.heads, layer.n, layer.d, layer.c_q, "f32"))
+    x.update({a: getattr(layer, a) for a in R.SETS})
+    return x
+
+
+def test_layer_trains_end_to_end():
+    """forward_train: the layer's stages, attention dropout, output dropout and
+    residual, and the gradients of all inputs."""
+    layer, q, k, v, iq, ik = small_layer()
+    res = torch.randn_like(q)
+    leaves = [t.clone().requires_grad_() for t in (q, k, v, res)]
+    rng = rng_of(11, 12)
+    y = layer.forward_train(*leaves[:3], iq, ik, dropout=0.1, rng=rng, residual=leaves[3],
+                            out_dropout=0.2)
+    rng.fill_(0)  # the masks belong to the forward's values
+    g = torch.randn_like(y)
+    y.backward(g)
+    torch.cuda.synchronize()
+    keep = torch.from_numpy(R.keep_elements(y.numel(), 0.2, 11, 12)).cuda().view_as(y)
+    d_o = torch.where(keep, g * (65536.0 / (65536 - R.threshold(0.2))), 0.0)
+    x = case_of(layer, q, k, v, d_o)
+    got = run(x, 0.1, (11, 12))
+    check(x, got, 0.1, (11, 12))
+    for leaf, name in zip(leaves, ("dq", "dk", "dv")):
+        assert torch.equal(leaf.grad, got[name]), name
+    assert torch.equal(leaves[3].grad, g)
+    want = torch.where(keep, got["o"] * (65536.0 / (65536 - R.threshold(0.2))), 0.0) + res
+    assert torch.equal(y, want)
+    # a second step, warm-started, on the same layer
+    y2 = layer.forward_train(*leaves[:3], dropout=0.1, rng=rng_of(11, 13), warm=True, warm_iters=1)
+    y2.square().sum().backward()
+    assert all(torch.isfinite(leaf.grad).all() for leaf in leaves[:3])
+
+
+def test_a_new_selection_before_the_backward_is_refused():
+    layer, q, k, v, iq, ik = small_layer()
+    qa = q.clone().requires_grad_()
+    y = layer.forward_train(qa, k, v, iq, ik)
+    layer.select(rho=0.5)
+    with pytest.raises(RuntimeError, match="changed"):
+        y.sum().backward()
+
+
+def test_dense_attention_differentiates():
+    n, d = 210, 64
+    dense = DenseAttention(2, n, d, "f32")
+    x = R.make(2, n, d, "f32", 1, 1.0, 6)
+    leaves = [x[t].clone().requires_grad_() for t in ("q", "k", "v")]
+    out = dense.attention(*leaves, dropout=0.25, rng=rng_of(2, 3))
+    # a gradient that is broadcast, so not contiguous
+    g = torch.randn(1, 1, d, device="cuda").expand(2, n, d)
+    out.backward(g)
+    x.update(d_o=g.contiguous(), offsets=dense.offsets, perm=dense.perm,
+             sel_counts=dense.sel_counts, sel_idx=dense.sel_idx)
+    got = run(x, 0.25, (2, 3))
+    check(x, got, 0.25, (2, 3))
+    assert torch.equal(out, got["o"])
+    for leaf, name in zip(leaves, ("dq", "dk", "dv")):
+        assert torch.equal(leaf.grad, got[name]), name
+
+
+# --- bad sets, refusals -------------------------------------------------------------
+
+def test_bad_sets_are_reported():
+    x = R.make(1, 300, 64, "bf16", 3, 0.5, 1)
+    H, n, d, C, dtype = x["dims"]
+    o, lse = (t.zero_() for t in TrainingAttention(H, n, d, C, dtype).outputs())
+    for at, value in ((5, 5000), (9, -3), (20, None)):
+        sel = x["sel_idx"].clone()
+        sel[0, 1, at] = sel[0, 1, at - 1] if value is None else value
+        a = TrainingAttention(H, n, d, C, dtype)
+        a.backward(x["q"], x["k"], x["v"], o, lse, x["d_o"], x["offsets"], x["perm"],
+                   x["sel_counts"], sel)
+        torch.cuda.synchronize()
+        assert int(a.status.item()) == 8, (at, value)
+
+
+def test_refusals():
+    x = R.make(1, 40, 64, "bf16", 2, 0.5, 1)
+    a = TrainingAttention(1, 40, 64, 2, "bf16")
+    args = (x["q"], x["k"], x["v"], *R.sets(x))
+    with pytest.raises(ValueError, match="rng"):
+        a.forward(*args, dropout=0.1)
+    with pytest.raises(ValueError, match="contiguous"):
+        a.forward(x["q"].transpose(1, 2), *args[1:])
+    with pytest.raises(ValueError, match="must be"):
+        a.forward(x["q"].float(), *args[1:])
+    with pytest.raises(ValueError, match="tensors on|GPU"):
+        a.forward(x["q"].cpu(), *args[1:])
+    with pytest.raises(B.ScopeError):
+        a.forward(*args, dropout=1.0, rng=rng_of(1, 1))
+    with pytest.raises(B.ScopeError):  # the output over an input
+        a.forward(*args, into=(x["q"], a.outputs()[1]))
+    with pytest.raises(B.ScopeError):
+        a.forward(*args, scale=math.nan)
+
+
+# --- dropout -------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("count", [0, 1, 7, 8, 9, 255, 4096, 100003])
+@pytest.mark.parametrize("residual", [False, True])
+def test_dropout(dtype, count, residual):
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(count)
+    whole = torch.randn(count + 3, generator=g, device="cuda").to(t)
+    other = torch.randn(count + 3, generator=g, device="cuda").to(t)
+    seed, offset = 0xDEADBEEF1234567, 2 ** 33 + 5
+    for shift in (0, 1, 3):        # aligned to 16 bytes and not
+        x, r = whole[shift:shift + count], other[shift:shift + count] if residual else None
+        for p in (0.1, 0.5, 0.9999999):
+            y = dropout(x, p, rng_of(seed, offset), residual=r)
+            keep = torch.from_numpy(R.keep_elements(count, p, seed, offset)).cuda()
+            scale = np.float32(65536.0 / (65536 - R.threshold(p)))
+            want = torch.where(keep, x.float() * float(scale), 0.0)
+            want = (want + r.float() if residual else want).to(t)
+            assert torch.equal(y, want), (shift, p)
+
+
+def test_dropout_drops_nan_and_works_in_place():
+    x = torch.full((1000,), math.nan, device="cuda")
+    y = dropout(x, 0.5, rng_of(1, 2))
+    keep = torch.from_numpy(R.keep_elements(1000, 0.5, 1, 2)).cuda()
+    assert torch.equal(torch.isnan(y), keep) and (y[~keep] == 0).all()
+    z = torch.randn(1001, device="cuda").bfloat16()
+    want = dropout(z, 0.3, rng_of(1, 2), residual=z)
+    assert torch.equal(dropout(z, 0.0, None), z)
+    dropout(z, 0.3, rng_of(1, 2), residual=z, out=z)
+    assert torch.equal(z, want)
+
+
+def test_dropout_rate():
+    """Kept share over 2^22 elements and pairs: six standard deviations."""
+    n = 1 << 22
+    for p in (0.1, 0.5):
+        y = dropout(torch.ones(n, device="cuda"), p, rng_of(8, 9))
+        q = R.threshold(p) / 65536
+        assert abs((y != 0).double().mean().item() - (1 - q)) <= 6 * math.sqrt(q * (1 - q) / n)
+        keep = R.keep_pairs(1, 2048, p, 8, 9)
+        assert abs(keep.mean() - (1 - q)) <= 6 * math.sqrt(q * (1 - q) / n)
+
+
+def test_dropout_refusals():
+    x = torch.randn(64, device="cuda")
+    with pytest.raises(ValueError, match="rng"):
+        dropout(x, 0.1, None)
+    with pytest.raises(B.ScopeError):
+        dropout(x, -0.1, rng_of(0, 0))
+    with pytest.raises(ValueError, match="must be"):
+        dropout(x.half(), 0.1, rng_of(0, 0))
+    with pytest.raises(ValueError, match="contiguous"):
+        dropout(x[::2], 0.1, rng_of(0, 0))
+    with pytest.raises(B.ScopeError):   # a shifted overlap
+        dropout(x[:32], 0.1, rng_of(0, 0), out=x[1:33])
+    with pytest.raises(ValueError, match="residual"):
+        dropout(x, 0.1, rng_of(0, 0), residual=x[:32])
