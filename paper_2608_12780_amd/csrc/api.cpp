@@ -888,6 +888,10 @@ int32_t check_dropout(float p, const uint64_t *rng, uint32_t *drop) {
   return SCOPE_OK;
 }
 
+size_t train_ws(const scope_shape *s, int c_q) {
+  return scope::train_workspace(s->heads, s->n, s->d, s->dtype == SCOPE_BF16, c_q, nullptr, nullptr, nullptr);
+}
+
 // Whether one of the first `outs` arrays overlaps another (arrays of one size).
 bool outputs_overlap(const scope_shape *s, int outs, std::initializer_list<const void *> arrays) {
   const uintptr_t bytes = static_cast<uintptr_t>(s->heads) * s->n * s->d * (s->dtype == SCOPE_BF16 ? 2 : 4);
@@ -921,9 +925,10 @@ void set_train(const scope_shape *s, const void *q, const void *k, const void *v
   a->drop = drop;
   a->kept_scale = 65536.0f / static_cast<float>(65536u - (drop >> 16));
   a->lse = lse;
+  a->rows = static_cast<size_t>(s->heads) * s->n;
   c->heads = s->heads;
   c->rng = rng;
-  scope::train_workspace(s->heads, s->n, c_q, workspace, a, c);
+  scope::train_workspace(s->heads, s->n, s->d, s->dtype == SCOPE_BF16, c_q, workspace, a, c);
 }
 
 }  // namespace
@@ -983,7 +988,7 @@ int32_t scope_training_workspace_size(const scope_shape *shape, int32_t c_q, siz
   if ((st = check_cq(shape, c_q))) return st;
   if (shape->d != 64 && shape->d != 128) return SCOPE_ERR_UNSUPPORTED;
   if (!bytes) return SCOPE_ERR_INVALID_ARGUMENT;
-  *bytes = scope::train_workspace(shape->heads, shape->n, c_q, nullptr, nullptr, nullptr);
+  *bytes = train_ws(shape, c_q);
   return SCOPE_OK;
 }
 
@@ -1003,7 +1008,7 @@ int32_t scope_sparse_attention_train(const scope_shape *shape, const void *q, co
   scope::TrainArgs a{};
   scope::TrainCall c{};
   if ((st = check_ws(workspace, ws_bytes,
-                     scope::train_workspace(shape->heads, shape->n, c_q, nullptr, nullptr, nullptr))))
+                     train_ws(shape, c_q))))
     return st;
   set_train(shape, q, k, v, c_q, offsets, perm, sel_counts, sel_idx, scale, drop, rng, lse,
             workspace, &a, &c);
@@ -1032,7 +1037,7 @@ int32_t scope_sparse_attention_backward(
   scope::TrainArgs a{};
   scope::TrainCall c{};
   if ((st = check_ws(workspace, ws_bytes,
-                     scope::train_workspace(shape->heads, shape->n, c_q, nullptr, nullptr, nullptr))))
+                     train_ws(shape, c_q))))
     return st;
   set_train(shape, q, k, v, c_q, offsets, perm, sel_counts, sel_idx, scale, drop, rng,
             const_cast<float *>(lse), workspace, &a, &c);

@@ -166,13 +166,14 @@ __global__ __launch_bounds__(kThreads) void train_queries_kernel(TrainArgs a, T 
   if constexpr (GRAD) {
     TileT::fragments(gf, static_cast<const T *>(a.d_o) + qi * D, valid, hf);
     if (valid) {
-      const float2 s = a.stats[qi];
-      neg_lse = s.x;
-      delta = s.y;
+      const float *st = a.stats + 2 * h * static_cast<size_t>(a.n + 1) + (qi - first);
+      neg_lse = st[0];
+      delta = st[a.n + 1];
     }
   }
   uint2 mine = make_uint2(0, 0);
-  if (DROP && valid) mine = a.words[2 * first + (qi - first)];
+  const uint32_t *wq = a.words + 4 * first, *wk = wq + 2 * static_cast<size_t>(a.n);
+  if (DROP && valid) mine = make_uint2(wq[qi - first], wq[qi - first + a.n]);
   f32x16 acc[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(kThreads) void train_queries_kernel(TrainArgs a, T 
       const int j = in ? min(max(sel[k0 + row], 0), a.n - 1) : 0;
       *reinterpret_cast<uint4 *>(&K.x[row * TileT::kStride + chunk * (16 / sizeof(T))]) = row_chunk(k, j, D, chunk, in);
       *reinterpret_cast<uint4 *>(&V.x[row * TileT::kStride + chunk * (16 / sizeof(T))]) = row_chunk(v, j, D, chunk, in);
-      if (DROP && chunk == 0) words[row] = a.words[2 * first + a.n + j];
+      if (DROP && chunk == 0) words[row] = make_uint2(wk[j], wk[j + a.n]);
     }
     __syncthreads();
     const f32x16 s = K.scores(qf, l32, hf);
@@ -263,23 +264,24 @@ __global__ __launch_bounds__(kThreads) void train_keys_kernel(TrainArgs a, T *dk
   TileT::fragments(kf, static_cast<const T *>(a.k) + kj * D, valid, hf);
   TileT::fragments(vf, static_cast<const T *>(a.v) + kj * D, valid, hf);
   uint2 mine = make_uint2(0, 0);
-  if (DROP) mine = a.words[2 * first + a.n + (kj - first)];
+  const uint32_t *wq = a.words + 4 * first, *wk = wq + 2 * static_cast<size_t>(a.n);
+  if (DROP) mine = make_uint2(wk[kj - first], wk[kj - first + a.n]);
   f32x16 dka[D / 32], dva[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dka[db][e] = dva[db][e] = 0.0f;
   // the block's four words of each cluster, one per wave
-  const int nw = (a.n + 31) / 32;
-  const uint32_t *masks = a.masks + (static_cast<size_t>(h) * nw + 4 * static_cast<size_t>(b)) * a.c_q;
-  const int words_here = min(4, nw - 4 * b);
+  constexpr int WORDS = kTrainKeyBlock / 32, SHARE = kTrainKeyBlock / kRows;
+  const uint32_t *masks = a.masks + (static_cast<size_t>(h) * ((blocks + SHARE - 1) / SHARE) + b / SHARE) * a.c_q * WORDS +
+                          kRows / 32 * (b % SHARE);
   for (int i = 0; i < a.items_per_head; ++i) {
     const int4 it = a.items[static_cast<size_t>(h) * a.items_per_head + i];
     const int c = it.x, row0 = it.y, rows = it.z;
     if (rows <= 0) break;
     uint32_t any = 0, own = 0;
-    for (int x = 0; x < words_here; ++x) {
-      const uint32_t m = masks[static_cast<size_t>(x) * a.c_q + c];
+    for (int x = 0; x < kRows / 32; ++x) {
+      const uint32_t m = masks[c * WORDS + x];
       any |= m;
       if (x == w) own = m;
     }
@@ -295,8 +297,9 @@ __global__ __launch_bounds__(kThreads) void train_keys_kernel(TrainArgs a, T *dk
       *reinterpret_cast<uint4 *>(&Q.x[row * TileT::kStride + chunk * (16 / sizeof(T))]) = row_chunk(q, qi, D, chunk, in);
       *reinterpret_cast<uint4 *>(&G.x[row * TileT::kStride + chunk * (16 / sizeof(T))]) = row_chunk(g, qi, D, chunk, in);
       if (chunk == 0) {
-        stats[row] = in ? a.stats[qi] : make_float2(-INFINITY, 0.0f);
-        if (DROP) words[row] = a.words[2 * first + (qi - first)];
+        const float *st = a.stats + 2 * h * static_cast<size_t>(a.n + 1) + (in ? qi - first : a.n);
+        stats[row] = make_float2(st[0], st[a.n + 1]);
+        if (DROP) words[row] = make_uint2(wq[qi - first], wq[qi - first + a.n]);
       }
     }
     __syncthreads();
@@ -360,7 +363,7 @@ __global__ __launch_bounds__(1024) void train_items_kernel(int n, int c_q, int r
   }
 }
 
-// Key bits: masks[head][key / 32][cluster].  A block turns one cluster's list
+// Key bits: masks[head][key / 256][cluster][8 words].  A block turns one cluster's list
 // into the bits of kMaskWords words in LDS; a list that is not strictly ascending
 // or leaves [0, n) is reported, and its bits are those that the search finds.
 constexpr int kMaskWords = 1024;
@@ -396,16 +399,18 @@ __global__ __launch_bounds__(256) void train_masks_kernel(int n, int c_q, const 
     if (bad) atomicOr(status, kStatusBadSet);
   }
   __syncthreads();
-  const int nw = (n + 31) / 32, w0 = from / 32;
-  for (int i = t; i < kMaskWords && w0 + i < nw; i += 256)
-    masks[(static_cast<size_t>(h) * nw + w0 + i) * c_q + c] = bits[i];
+  constexpr int WORDS = kTrainKeyBlock / 32;
+  const int blocks = (n + kTrainKeyBlock - 1) / kTrainKeyBlock, b0 = from / kTrainKeyBlock;
+  for (int i = t; i < kMaskWords && b0 + i / WORDS < blocks; i += 256)
+    masks[((static_cast<size_t>(h) * blocks + b0 + i / WORDS) * c_q + c) * WORDS + i % WORDS] = bits[i];
 }
 
 // The rows' statistics for the gradients: (-lse in the exp2 domain, <do, o>).
-// A row without keys has lse = -inf: its probabilities are exp2(-inf) = 0.
+// A row without keys has lse = -inf: its probabilities are exp2(-inf) = 0.  Row n
+// of a head is one of no weight, for the rows that fill up a tile.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void train_stats_kernel(size_t rows, const T *__restrict__ o, const T *__restrict__ d_o,
-                                                          const float *__restrict__ lse, float2 *stats) {
+__global__ __launch_bounds__(256) void train_stats_kernel(size_t rows, int n, const T *__restrict__ o, const T *__restrict__ d_o,
+                                                          const float *__restrict__ lse, float *stats) {
   constexpr int PER = 16 / sizeof(T), LANES = D / PER;
   const size_t i = (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x) / LANES;
   const int x = threadIdx.x % LANES;
@@ -415,13 +420,25 @@ __global__ __launch_bounds__(256) void train_stats_kernel(size_t rows, const T *
   for (int e = 0; e < PER; ++e) s = fmaf(load_elem(o, i * D + PER * x + e), load_elem(d_o, i * D + PER * x + e), s);
 #pragma unroll
   for (int k = LANES / 2; k > 0; k /= 2) s += __shfl_xor(s, k, LANES);
-  if (x == 0) stats[i] = make_float2(lse[i] == -INFINITY ? -INFINITY : -lse[i] * kLog2e, s);
+  if (x == 0) {
+    float *head = stats + (i / n) * 2 * (n + 1);
+    head[i % n] = lse[i] == -INFINITY ? -INFINITY : -lse[i] * kLog2e;
+    head[n + 1 + i % n] = s;
+    if (i % n == 0) {
+      head[n] = -INFINITY;
+      head[2 * n + 1] = 0.0f;
+    }
+  }
 }
 
 // Dropout's words: of the queries, then of the keys, per head.
-__global__ __launch_bounds__(256) void train_words_kernel(int n, const uint64_t *__restrict__ rng, uint2 *words) {
+__global__ __launch_bounds__(256) void train_words_kernel(int n, const uint64_t *__restrict__ rng, uint32_t *words) {
   const int i = blockIdx.x * 256 + threadIdx.x, side = blockIdx.y, h = blockIdx.z;
-  if (i < n) words[(2 * static_cast<size_t>(h) + side) * n + i] = pair_word(Stream(rng), i, h, side);
+  if (i >= n) return;
+  const uint2 x = pair_word(Stream(rng), i, h, side);
+  uint32_t *at = words + (4 * static_cast<size_t>(h) + 2 * side) * n + i;
+  at[0] = x.x;
+  at[n] = x.y;
 }
 
 template <typename K, typename... A>
@@ -438,7 +455,7 @@ hipError_t launch(K kernel, dim3 grid, int threads, hipStream_t s, A... args) {
 
 hipError_t common_setup(const TrainArgs &a, const TrainCall &c, hipStream_t s) {
   if (a.drop)
-    TRAIN_TRY(launch(train_words_kernel, dim3((a.n + 255) / 256, 2, c.heads), 256, s, a.n, c.rng, const_cast<uint2 *>(a.words)));
+    TRAIN_TRY(launch(train_words_kernel, dim3((a.n + 255) / 256, 2, c.heads), 256, s, a.n, c.rng, const_cast<uint32_t *>(a.words)));
   return hipSuccess;
 }
 
@@ -461,8 +478,8 @@ template <typename T, int D>
 hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
   TRAIN_TRY(common_setup(a, c, s));
   const size_t rows = static_cast<size_t>(c.heads) * a.n, lanes = D * sizeof(T) / 16;
-  TRAIN_TRY(launch(train_stats_kernel<T, D>, dim3((rows * lanes + 255) / 256), 256, s, rows, static_cast<const T *>(c.o),
-                   static_cast<const T *>(a.d_o), a.lse, const_cast<float2 *>(a.stats)));
+  TRAIN_TRY(launch(train_stats_kernel<T, D>, dim3((rows * lanes + 255) / 256), 256, s, rows, a.n, static_cast<const T *>(c.o),
+                   static_cast<const T *>(a.d_o), a.lse, const_cast<float *>(a.stats)));
   const int segments = (a.n + 32 * kMaskWords - 1) / (32 * kMaskWords);
   TRAIN_TRY(launch(train_masks_kernel, dim3(segments, a.c_q, c.heads), 256, s, a.n, a.c_q, a.sel_counts, a.sel_idx,
                    const_cast<uint32_t *>(a.masks), c.status));
@@ -472,9 +489,13 @@ hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
   const dim3 qgrid(static_cast<unsigned>(c.heads) * a.items_per_head);
   TRAIN_TRY(a.drop ? launch(train_queries_kernel<T, D, true, true>, qgrid, kThreads, s, a, static_cast<T *>(c.dq))
                    : launch(train_queries_kernel<T, D, true, false>, qgrid, kThreads, s, a, static_cast<T *>(c.dq)));
+  constexpr int tile = sizeof(T) == 2 ? kTrainKeyTile : kTile;
   a.items = c.tiles;
-  a.items_per_head = train_items_per_head(a.n, a.c_q, kTile);
-  TRAIN_TRY(make_items(a, c.heads, kTile, a.items_per_head, c.tiles, s));
+  a.items_per_head = train_items_per_head(a.n, a.c_q, tile);
+  TRAIN_TRY(make_items(a, c.heads, tile, a.items_per_head, c.tiles, s));
+  if constexpr (sizeof(T) == 2)
+    return train_keys(D, a, c.heads, train_key_splits(c.heads, a.n, a.c_q), c.parts, static_cast<uint16_t *>(c.dk),
+                      static_cast<uint16_t *>(c.dv), s);
   const dim3 kgrid(static_cast<unsigned>(c.heads) * ((a.n + kRows - 1) / kRows));
   return a.drop ? launch(train_keys_kernel<T, D, true>, kgrid, kThreads, s, a, static_cast<T *>(c.dk), static_cast<T *>(c.dv))
                 : launch(train_keys_kernel<T, D, false>, kgrid, kThreads, s, a, static_cast<T *>(c.dk), static_cast<T *>(c.dv));
@@ -484,7 +505,7 @@ hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
 
 int train_items_per_head(int n, int c_q, int rows) { return (n + rows - 1) / rows + c_q; }
 
-size_t train_workspace(int heads, int n, int c_q, void *base, TrainArgs *a, TrainCall *c) {
+size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, TrainArgs *a, TrainCall *c) {
   size_t used = 0;
   auto take = [&](size_t bytes) {
     char *p = base ? static_cast<char *>(base) + used : nullptr;
@@ -494,15 +515,18 @@ size_t train_workspace(int heads, int n, int c_q, void *base, TrainArgs *a, Trai
   const size_t H = heads;
   char *items = take(H * train_items_per_head(n, c_q, kRows) * sizeof(int4));
   char *tiles = take(H * train_items_per_head(n, c_q, kTile) * sizeof(int4));
-  char *words = take(H * n * 2 * sizeof(uint2));
-  char *stats = take(H * n * sizeof(float2));
-  char *masks = take(H * c_q * ((static_cast<size_t>(n) + 31) / 32) * sizeof(uint32_t));
+  char *words = take(H * n * 4 * sizeof(uint32_t));
+  char *stats = take(H * (n + 1) * 2 * sizeof(float));
+  char *masks = take(H * ((n + kTrainKeyBlock - 1) / kTrainKeyBlock) * c_q * (kTrainKeyBlock / 8));
+  const int splits = bf16 ? train_key_splits(heads, n, c_q) : 1;
+  char *parts = take(splits > 1 ? H * n * d * splits * 2 * sizeof(float) : 0);
   if (a) {
-    a->words = reinterpret_cast<uint2 *>(words);
-    a->stats = reinterpret_cast<float2 *>(stats);
+    a->words = reinterpret_cast<uint32_t *>(words);
+    a->stats = reinterpret_cast<float *>(stats);
     a->masks = reinterpret_cast<uint32_t *>(masks);
     c->items = reinterpret_cast<int4 *>(items);
     c->tiles = reinterpret_cast<int4 *>(tiles);
+    c->parts = reinterpret_cast<float *>(parts);
   }
   return used;
 }

@@ -269,20 +269,28 @@ struct TrainArgs {
   float kept_scale;        // 1 / (1 - p), p the threshold's probability
   float *lse;
   const int4 *items;
-  const uint2 *words;      // [heads][query, key][n]
-  const float2 *stats;     // [heads][n]
-  const uint32_t *masks;   // [heads][ceil(n / 32)][c_q]
+  size_t rows;             // heads * n
+  const uint32_t *words;   // dropout: [heads][query 0, query 1, key 0, key 1][n]
+  const float *stats;      // [heads][-lse in the exp2 domain, <do, o>][n + 1]
+  const uint32_t *masks;   // key bits: [heads][ceil(n / 256)][c_q][8]
 };
 struct TrainCall {
   int heads;
   const uint64_t *rng;
   void *o, *dq, *dk, *dv;
   int4 *items, *tiles;
+  float *parts;            // sums of the query parts (train_key_splits > 1)
   int32_t *status;
 };
+constexpr int kTrainKeyBlock = 256;  // keys of a block and of a mask row
+constexpr int kTrainKeyTile = 64;    // queries of a tile (attention_keys.hip)
+int train_key_splits(int heads, int n, int c_q);
+hipError_t train_keys(int d, const TrainArgs &a, int heads, int splits, float *parts, uint16_t *dk,
+                      uint16_t *dv, hipStream_t s);
 int train_items_per_head(int n, int c_q, int rows);
 // Lays the workspace out (base null: only its size).
-size_t train_workspace(int heads, int n, int c_q, void *base, TrainArgs *a, TrainCall *c);
+size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, TrainArgs *a,
+                       TrainCall *c);
 hipError_t train_forward(int d, bool bf16, const TrainArgs &a, const TrainCall &c, hipStream_t s);
 hipError_t train_backward(int d, bool bf16, const TrainArgs &a, const TrainCall &c, hipStream_t s);
 
