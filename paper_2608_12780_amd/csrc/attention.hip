@@ -23,6 +23,7 @@
 
 #include <mutex>
 
+#include "attention_slots.h"
 #include "common.h"
 #include "kernels.h"
 #include "mfma.h"
@@ -31,31 +32,8 @@ namespace scope {
 
 namespace {
 
-constexpr int kBN = 64;          // keys per tile
-constexpr int kNW = 8;           // waves per block
-constexpr int kQB = 1;           // 32-query column blocks per wave
-constexpr int kBM = 32 * kQB * kNW;
-constexpr float kRescale = 8.0f; // lazy rescale: running max may lag by 2^8
-
-// Work slots run in list order: heads one after the other and, within a
-// head, by estimated cost, largest first, with a cluster's row chunks
-// adjacent.  All XCDs work on the same head at a time, so one head's K/V
-// (60 MB at 118800 x 128 bf16) is what the 256 MB memory-side cache has to
-// hold.  (Where several heads' fit there, attn_plan_kernel gives the order.)
-//
-// Block b runs on XCD b mod 8.  Runs of kRun consecutive work slots (the
-// chunks of one cluster, which gather the same K/V rows) go to one XCD so
-// that they share its L2; windows of 8 * kRun slots still follow the list
-// order.  A partial last window keeps the identity map.
-constexpr int kXcds = 8, kRun = 4;
 constexpr uint64_t kMemorySideCache = 256ull << 20;
-__device__ __forceinline__ int xcd_item(int b, int total) {
-  constexpr int W = kXcds * kRun;
-  const int w0 = b / W * W;
-  if (w0 + W > total) return b;
-  const int r = b - w0;
-  return w0 + (r % kXcds) * kRun + r / kXcds;
-}
+constexpr float kRescale = 8.0f; // lazy rescale: running max may lag by 2^8
 
 // fp32 inputs without workspace for bf16 copies of K and V: rows are rounded
 // to bf16 on the way through registers.
@@ -323,27 +301,6 @@ __global__ __launch_bounds__(kNW * 64) void attn_kernel(
 }
 
 __device__ __forceinline__ int key_tiles(const int4 &e) { return e.z > 0 ? (e.w + kBN - 1) / kBN : 0; }
-
-// Half a slot: the queries of its waves 0 .. kNW/2 - 1 (half 1) or of the others
-// (half 2).  A query's result depends neither on its wave nor on its block, so
-// halves give the slot's results bit for bit.
-__device__ __forceinline__ void take_half(int4 *a, int4 *b, int half) {
-  const int first = half == 2 ? kNW / 2 : 0;
-  // the rows of an entry, whose first wave is w0, that the half's waves hold
-  auto cut = [&](int4 *e, int w0) {
-    const int from = min(max(32 * (first - w0), 0), e->z);
-    const int to = min(max(32 * (first + kNW / 2 - w0), 0), e->z);
-    e->y += from;
-    e->z = to - from;
-  };
-  const int wa = (a->z + 31) >> 5;
-  cut(a, 0);
-  cut(b, wa);
-  if (a->z <= 0) {
-    *a = *b;
-    b->z = 0;
-  }
-}
 
 // The same computation with bf16 K/V rows gathered straight into LDS by the
 // buffer unit (one 1 KB load per 4 rows at d = 128, per 8 rows at d = 64; no
@@ -1094,20 +1051,12 @@ hipError_t launch_dma(int heads, int n, const void *q, const void *k, const void
                       int c_q, const int32_t *offsets, const int32_t *perm, const int32_t *sel_idx,
                       int iph, float scale_log2, const AttnScratch &w, hipStream_t s) {
   const int total = iph * heads;
-  if (!w.order) {
-    hipLaunchKernelGGL((attn_kernel_dma<D, BF16IO>), dim3(total), dim3(kNW * 64), 0, s, n, c_q,
-                       iph, total, q, k, v, o, offsets, perm, sel_idx, w.items,
-                       static_cast<const int2 *>(nullptr), scale_log2);
-    return hipGetLastError();
-  }
-  const int slots = queue_slots(total), halved = halved_slots(heads, n, D);
-  const int queue = slots + halved;
-  hipLaunchKernelGGL(attn_plan_kernel, dim3(kXcds), dim3(kPlanThreads), 0, s, total, slots,
-                     resident_blocks(D), halved, w.items, w.order);
-  const hipError_t e = hipGetLastError();
+  int blocks = 0;
+  const hipError_t e = attention_plan(heads, n, D, c_q, w, &blocks, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attn_kernel_dma<D, BF16IO>), dim3(kXcds * queue), dim3(kNW * 64), 0, s, n, c_q,
-                     iph, total, q, k, v, o, offsets, perm, sel_idx, w.items, w.order, scale_log2);
+  hipLaunchKernelGGL((attn_kernel_dma<D, BF16IO>), dim3(blocks), dim3(kNW * 64), 0, s, n, c_q,
+                     iph, total, q, k, v, o, offsets, perm, sel_idx, w.items,
+                     static_cast<const int2 *>(w.order), scale_log2);
   return hipGetLastError();
 }
 
@@ -1221,6 +1170,26 @@ size_t attention_order_entries(int heads, int n, int d, int c_q) {
          (queue_slots(heads * attn_items_per_head(n, c_q)) + halved_slots(heads, n, d));
 }
 
+hipError_t attention_list(int heads, int n, int d, int c_q, bool pair, const int32_t *offsets,
+                          const int32_t *sel_counts, const AttnScratch &w, hipStream_t s) {
+  hipLaunchKernelGGL(attn_items_kernel, dim3(heads), dim3(1024), 0, s, n, c_q,
+                     attn_items_per_head(n, c_q), pair ? 1 : 0, w.order ? 0 : d, w.order ? 0 : 1,
+                     offsets, sel_counts, w.items);
+  return hipGetLastError();
+}
+
+hipError_t attention_plan(int heads, int n, int d, int c_q, const AttnScratch &w, int *blocks,
+                          hipStream_t s) {
+  const int total = heads * attn_items_per_head(n, c_q);
+  *blocks = total;
+  if (!w.order) return hipSuccess;
+  const int slots = queue_slots(total), halved = halved_slots(heads, n, d);
+  *blocks = kXcds * (slots + halved);
+  hipLaunchKernelGGL(attn_plan_kernel, dim3(kXcds), dim3(kPlanThreads), 0, s, total, slots,
+                     resident_blocks(d), halved, w.items, w.order);
+  return hipGetLastError();
+}
+
 hipError_t attention_run(int heads, int n, int d, bool bf16, const void *q,
                          const void *k, const void *v, void *o, int c_q,
                          const int32_t *offsets, const int32_t *perm,
@@ -1229,10 +1198,8 @@ hipError_t attention_run(int heads, int n, int d, bool bf16, const void *q,
   const int iph = attn_items_per_head(n, c_q);
   // remainder chunks share blocks only in the LDS-DMA kernel (with a block order
   // always: fewer slots leave more of them room to run as halves)
-  const int pair = c_q > 1 && (bf16 || w.kv16) ? 1 : 0;
-  hipLaunchKernelGGL(attn_items_kernel, dim3(heads), dim3(1024), 0, s, n, c_q,
-                     iph, pair, w.order ? 0 : d, w.order ? 0 : 1, offsets, sel_counts, w.items);
-  hipError_t e = hipGetLastError();
+  const bool pair = c_q > 1 && (bf16 || w.kv16);
+  const hipError_t e = attention_list(heads, n, d, c_q, pair, offsets, sel_counts, w, s);
   if (e != hipSuccess) return e;
   const float sl2 = scale * 1.4426950408889634f;
   if (d == 128)

@@ -13,6 +13,7 @@
 // the second products, as the forward's weights do.  Every tile row that is read
 // from LDS feeds two matrix instructions (two blocks of 32 keys): one block would
 // need the LDS' whole bandwidth.
+#include "attention_tile.h"
 #include "common.h"
 #include "kernels.h"
 #include "mfma.h"
@@ -25,41 +26,8 @@ namespace {
 constexpr int kTQ = 64;            // queries per tile
 constexpr int kList = 1024;        // active tiles listed at a time
 
-// 16-byte slot of a row's chunk 0 (chunk c: slot ^ c): distinct for 16 (d = 64:
-// 8 pairs of) consecutive rows, which the row-major reads take together, and four
-// chunks apart for the four rows of a transposing read.
-template <int D>
-__device__ __forceinline__ int tile_swizzle(int row) {
-  return D == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
-}
-
-// Operand whose lane holds channel l32 of a 32-channel group and 16 tile rows 4 hf +
-// 8 (j / 4) + j % 4, from transposing reads of two groups of four rows.
-__device__ __forceinline__ bf16x8 columns(const char *lo, const char *hi) {
-  const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(lo)));
-  const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(hi)));
-  return as_bf16x8(make_uint4(a.x, a.y, b.x, b.y));
-}
-
-__device__ __forceinline__ bf16x8 pack8(const float *w) {
-  return as_bf16x8(make_uint4(pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3]), pack_bf16(w[4], w[5]), pack_bf16(w[6], w[7])));
-}
-
 constexpr int kWaves = kTrainKeyBlock / 32;  // a wave owns 32 keys
 constexpr int kThreads = 64 * kWaves;
-
-// Scheduling of one phase's matrix instructions: MFMAs with LDS reads and vector
-// instructions between them, so that neither waits for the other.
-template <int N, int READS, int VALU>
-__device__ __forceinline__ void interleave() {
-  __builtin_amdgcn_sched_group_barrier(0x100, 2 * READS, 0);
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-    if (VALU) __builtin_amdgcn_sched_group_barrier(0x002, VALU, 0);
-  }
-}
 
 template <int D, bool DROP>
 __global__ __launch_bounds__(kThreads)
@@ -85,30 +53,17 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const size_t first = static_cast<size_t>(h) * a.n;
 
-  // where the lane reads, in bytes: of its row, and transposing of row 4 hf +
-  // (lane % 16) / 4; 16 channels on is the first xor 32, 32 channels on the second
-  // xor 64, eight rows down the second xor 32 plus eight rows
-  const int own_sw = tile_swizzle<D>(l32);
-  const int tr_row = 4 * hf + ((lane & 15) >> 2), tr_chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-  int row_at = 2 * D * l32 + 16 * (hf ^ own_sw);
-  int col_at = 2 * D * tr_row + 16 * (tr_chunk ^ tile_swizzle<D>(tr_row)) + 8 * (lane & 1);
-  auto row_frag = [&](const uint16_t *tile, int x) {
-    return as_bf16x8(*reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(tile) + (row_at ^ (x << 5))));
-  };
-  auto col_frag = [&](const uint16_t *tile, int db) {
-    const char *t = reinterpret_cast<const char *>(tile);
-    return columns(t + (col_at ^ (db << 6)), t + 16 * D + (col_at ^ (db << 6) ^ 32));
-  };
+  TileReader<D> at(lane);
   bf16x8 kf[D / 16], vf[VLDS ? 1 : D / 16];
   const int own_row = 32 * w + l32, key = kb * kTrainKeyBlock + own_row;
   {
-    const size_t at = (first + min(key, a.n - 1)) * D;
+    const size_t from = (first + min(key, a.n - 1)) * D;
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) {
-      kf[x] = as_bf16x8(key < a.n ? load8<true>(a.k, at + 16 * x + 8 * hf) : make_uint4(0, 0, 0, 0));
-      const uint4 v = key < a.n ? load8<true>(a.v, at + 16 * x + 8 * hf) : make_uint4(0, 0, 0, 0);
+      kf[x] = as_bf16x8(key < a.n ? load8<true>(a.k, from + 16 * x + 8 * hf) : make_uint4(0, 0, 0, 0));
+      const uint4 v = key < a.n ? load8<true>(a.v, from + 16 * x + 8 * hf) : make_uint4(0, 0, 0, 0);
       if constexpr (VLDS)
-        *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(Vs + 32 * w * D) + (row_at ^ (x << 5))) = v;
+        *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(Vs + 32 * w * D) + (at.row_at ^ (x << 5))) = v;
       else
         vf[x] = as_bf16x8(v);
     }
@@ -185,23 +140,23 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
     for (int qb = 0; qb < kTQ / 32; ++qb) {
       const uint16_t *qr = qt + 32 * qb * D, *gr = gt + 32 * qb * D;
       f32x16 s, dp;
-      asm volatile("" : "+v"(row_at));
+      asm volatile("" : "+v"(at.row_at));
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.0f;
 #pragma unroll
       for (int x = 0; x < D / 16; ++x)
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            row_frag(qr, x), kf[x], s, 0, 0, 0);
+            at.row(qr, x), kf[x], s, 0, 0, 0);
       interleave<D / 16, 1, 0>();
-      asm volatile("" : "+v"(s), "+v"(row_at));
+      asm volatile("" : "+v"(s), "+v"(at.row_at));
       // p, with its sign bit set where dropout drops it
       float p[16], kept[16];
 #pragma unroll
       for (int x = 0; x < D / 16; ++x) {
-        const bf16x8 g = row_frag(gr, x);
+        const bf16x8 g = at.row(gr, x);
         bf16x8 v;
         if constexpr (VLDS)
-          v = row_frag(Vs + 32 * w * D, x);
+          v = at.row(Vs + 32 * w * D, x);
         else
           v = vf[x];
         dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g, v, dp, 0, 0, 0);
@@ -228,7 +183,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
       }
       bf16x8 pk[2] = {operand(kept), operand(kept + 8)};
       interleave<D / 16, VLDS ? 2 : 1, D == 128 ? 6 : 12>();
-      asm volatile("" : "+v"(dp), "+v"(pk[0]), "+v"(pk[1]), "+v"(col_at));
+      asm volatile("" : "+v"(dp), "+v"(pk[0]), "+v"(pk[1]), "+v"(at.col_at));
       float ds[16];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -245,17 +200,17 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
       for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
-          dva[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag(gr + 16 * s2 * D, db), pk[s2], dva[db], 0, 0, 0);
+          dva[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.columns(gr + 16 * s2 * D, db), pk[s2], dva[db], 0, 0, 0);
       bf16x8 dsk[2] = {operand(ds), operand(ds + 8)};
       interleave<D / 16, 2, D == 128 ? 6 : 12>();
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(dva[db]));
-      asm volatile("" : "+v"(dsk[0]), "+v"(dsk[1]), "+v"(col_at));
+      asm volatile("" : "+v"(dsk[0]), "+v"(dsk[1]), "+v"(at.col_at));
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
-          dka[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_frag(qr + 16 * s2 * D, db), dsk[s2], dka[db], 0, 0, 0);
+          dka[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.columns(qr + 16 * s2 * D, db), dsk[s2], dka[db], 0, 0, 0);
       interleave<D / 16, 2, 0>();
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(dka[db]));
@@ -285,12 +240,12 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
       const unsigned long long votes = __ballot(active);
       if (lane == 0) found[w] = __popcll(votes);
       __syncthreads();
-      int at = count + __popcll(votes & ((1ull << lane) - 1ull));
+      int slot = count + __popcll(votes & ((1ull << lane) - 1ull));
       for (int i = 0; i < kWaves; ++i) {
-        if (i < w) at += found[i];
+        if (i < w) slot += found[i];
         count += found[i];
       }
-      if (active) list[at] = e;
+      if (active) list[slot] = e;
       next += 64 * kWaves;
       __syncthreads();
     }

@@ -466,6 +466,7 @@ hipError_t make_items(const TrainArgs &a, int heads, int rows, int per_head, int
 template <typename T, int D>
 hipError_t forward(TrainArgs a, const TrainCall &c, hipStream_t s) {
   TRAIN_TRY(common_setup(a, c, s));
+  if constexpr (sizeof(T) == 2) return train_queries(D, false, a, c.heads, c.slots, static_cast<T *>(c.o), s);
   a.items = c.items;
   a.items_per_head = train_items_per_head(a.n, a.c_q, kRows);
   TRAIN_TRY(make_items(a, c.heads, kRows, a.items_per_head, c.items, s));
@@ -483,19 +484,23 @@ hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
   const int segments = (a.n + 32 * kMaskWords - 1) / (32 * kMaskWords);
   TRAIN_TRY(launch(train_masks_kernel, dim3(segments, a.c_q, c.heads), 256, s, a.n, a.c_q, a.sel_counts, a.sel_idx,
                    const_cast<uint32_t *>(a.masks), c.status));
+  if constexpr (sizeof(T) == 2) {
+    TRAIN_TRY(train_queries(D, true, a, c.heads, c.slots, static_cast<T *>(c.dq), s));
+    a.items = c.tiles;
+    a.items_per_head = train_items_per_head(a.n, a.c_q, kTrainKeyTile);
+    TRAIN_TRY(make_items(a, c.heads, kTrainKeyTile, a.items_per_head, c.tiles, s));
+    return train_keys(D, a, c.heads, train_key_splits(c.heads, a.n, a.c_q), c.parts, static_cast<T *>(c.dk),
+                      static_cast<T *>(c.dv), s);
+  }
   a.items = c.items;
   a.items_per_head = train_items_per_head(a.n, a.c_q, kRows);
   TRAIN_TRY(make_items(a, c.heads, kRows, a.items_per_head, c.items, s));
   const dim3 qgrid(static_cast<unsigned>(c.heads) * a.items_per_head);
   TRAIN_TRY(a.drop ? launch(train_queries_kernel<T, D, true, true>, qgrid, kThreads, s, a, static_cast<T *>(c.dq))
                    : launch(train_queries_kernel<T, D, true, false>, qgrid, kThreads, s, a, static_cast<T *>(c.dq)));
-  constexpr int tile = sizeof(T) == 2 ? kTrainKeyTile : kTile;
   a.items = c.tiles;
-  a.items_per_head = train_items_per_head(a.n, a.c_q, tile);
-  TRAIN_TRY(make_items(a, c.heads, tile, a.items_per_head, c.tiles, s));
-  if constexpr (sizeof(T) == 2)
-    return train_keys(D, a, c.heads, train_key_splits(c.heads, a.n, a.c_q), c.parts, static_cast<uint16_t *>(c.dk),
-                      static_cast<uint16_t *>(c.dv), s);
+  a.items_per_head = train_items_per_head(a.n, a.c_q, kTile);
+  TRAIN_TRY(make_items(a, c.heads, kTile, a.items_per_head, c.tiles, s));
   const dim3 kgrid(static_cast<unsigned>(c.heads) * ((a.n + kRows - 1) / kRows));
   return a.drop ? launch(train_keys_kernel<T, D, true>, kgrid, kThreads, s, a, static_cast<T *>(c.dk), static_cast<T *>(c.dv))
                 : launch(train_keys_kernel<T, D, false>, kgrid, kThreads, s, a, static_cast<T *>(c.dk), static_cast<T *>(c.dv));
@@ -513,8 +518,11 @@ size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, 
     return p;
   };
   const size_t H = heads;
-  char *items = take(H * train_items_per_head(n, c_q, kRows) * sizeof(int4));
-  char *tiles = take(H * train_items_per_head(n, c_q, kTile) * sizeof(int4));
+  const size_t slots = bf16 ? 2 * H * attn_items_per_head(n, c_q) : H * train_items_per_head(n, c_q, kRows);
+  char *items = take(slots * sizeof(int4));
+  const bool ordered = bf16 && attention_ordered(heads, n, d, c_q);
+  char *order = take(ordered ? attention_order_entries(heads, n, d, c_q) * sizeof(int2) : 0);
+  char *tiles = take(H * train_items_per_head(n, c_q, bf16 ? kTrainKeyTile : kTile) * sizeof(int4));
   char *words = take(H * n * 4 * sizeof(uint32_t));
   char *stats = take(H * (n + 1) * 2 * sizeof(float));
   char *masks = take(H * ((n + kTrainKeyBlock - 1) / kTrainKeyBlock) * c_q * (kTrainKeyBlock / 8));
@@ -524,7 +532,8 @@ size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, 
     a->words = reinterpret_cast<uint32_t *>(words);
     a->stats = reinterpret_cast<float *>(stats);
     a->masks = reinterpret_cast<uint32_t *>(masks);
-    c->items = reinterpret_cast<int4 *>(items);
+    c->items = c->slots.items = reinterpret_cast<int4 *>(items);
+    c->slots.order = ordered ? reinterpret_cast<int2 *>(order) : nullptr;
     c->tiles = reinterpret_cast<int4 *>(tiles);
     c->parts = reinterpret_cast<float *>(parts);
   }

@@ -232,6 +232,12 @@ struct AttnScratch {
   int2 *order;
   uint16_t *kv16;
 };
+// The work list, and the block order where the scratch holds one; *blocks: the
+// launch's blocks.
+hipError_t attention_list(int heads, int n, int d, int c_q, bool pair, const int32_t *offsets,
+                          const int32_t *sel_counts, const AttnScratch &w, hipStream_t s);
+hipError_t attention_plan(int heads, int n, int d, int c_q, const AttnScratch &w, int *blocks,
+                          hipStream_t s);
 hipError_t attention_run(int heads, int n, int d, bool bf16, const void *q,
                          const void *k, const void *v, void *o, int c_q,
                          const int32_t *offsets, const int32_t *perm,
@@ -278,13 +284,17 @@ struct TrainCall {
   int heads;
   const uint64_t *rng;
   void *o, *dq, *dk, *dv;
-  int4 *items, *tiles;
+  int4 *items, *tiles;     // items: fp32; tiles: the queries' of dK and dV
+  AttnScratch slots;       // bf16: the work slots of the forward and of dQ
   float *parts;            // sums of the query parts (train_key_splits > 1)
   int32_t *status;
 };
 constexpr int kTrainKeyBlock = 256;  // keys of a block and of a mask row
 constexpr int kTrainKeyTile = 64;    // queries of a tile (attention_keys.hip)
 int train_key_splits(int heads, int n, int c_q);
+// The forward into `o` (grad false), or dQ from a.stats (grad true).
+hipError_t train_queries(int d, bool grad, const TrainArgs &a, int heads, const AttnScratch &w,
+                         uint16_t *out, hipStream_t s);
 hipError_t train_keys(int d, const TrainArgs &a, int heads, int splits, float *parts, uint16_t *dk,
                       uint16_t *dv, hipStream_t s);
 int train_items_per_head(int n, int c_q, int rows);
