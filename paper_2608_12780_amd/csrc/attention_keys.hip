@@ -330,17 +330,24 @@ hipError_t run(const TrainArgs &a, int heads, int splits, float *parts, uint16_t
 
 }  // namespace
 
-// Parts of the query tiles, each with fp32 sums of its own that a second kernel
-// adds: as many as give the chip four blocks per CU, while a part keeps eight
-// tiles and the parts' sums no more than kMost parts.
+// Parts of the query tiles, each with fp32 sums of its own that a second kernel adds.
+// The chip holds one block per CU: as many parts, up to 16 of two tiles or more, as
+// make the launch's rounds shortest, a part costing about 2% of a round more (its
+// start, its sums).  3 heads x 2185 tokens (27 key blocks): TODO.
 int train_key_splits(int heads, int n, int c_q) {
-  constexpr int kMost = 16;
+  constexpr int kMost = 16, kCus = 256;
   const long long blocks = static_cast<long long>(heads) * ((n + kTrainKeyBlock - 1) / kTrainKeyBlock);
   const long long tiles = train_items_per_head(n, c_q, kTrainKeyTile);
-  long long want = (1024 + blocks - 1) / blocks;
-  if (want > tiles / 8) want = tiles / 8;
-  if (want > kMost) want = kMost;
-  return want < 1 ? 1 : static_cast<int>(want);
+  int best = 1;
+  double least = 0.0;
+  for (int s = 1; s <= kMost && (s == 1 || 2 * s <= tiles); ++s) {
+    const double rounds = static_cast<double>((blocks * s + kCus - 1) / kCus) * (1.0 / s + 0.02);
+    if (s == 1 || rounds < least) {
+      least = rounds;
+      best = s;
+    }
+  }
+  return best;
 }
 
 hipError_t train_keys(int d, const TrainArgs &a, int heads, int splits, float *parts, uint16_t *dk, uint16_t *dv, hipStream_t s) {

@@ -106,13 +106,19 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
   struct Idx {
     int a[NG], b[NG], own;
   };
-  auto load_idx = [&](int tile, Idx &ix) {
+  // one chunk's; a whole tile's rows lie at lane offsets from a scalar one
+  auto load_rows = [&](const __amdgpu_buffer_rsrc_t &sel, int count, int tile, int (&rows_of)[NG]) {
+    const bool whole = (tile + 1) * kBN <= count;
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
-      const int row = tile * kBN + 8 * w + RPL * i + lane / CH;
-      ix.a[i] = __builtin_amdgcn_raw_buffer_load_b32(rselA, min(row, ia.w - 1) * 4, 0, 0);
-      ix.b[i] = PAIRED ? __builtin_amdgcn_raw_buffer_load_b32(rselB, min(row, ib.w - 1) * 4, 0, 0) : 0;
+      const int row = 8 * w + RPL * i + lane / CH;
+      rows_of[i] = whole ? __builtin_amdgcn_raw_buffer_load_b32(sel, row * 4, tile * kBN * 4, 0)
+                         : __builtin_amdgcn_raw_buffer_load_b32(sel, min(tile * kBN + row, count - 1) * 4, 0, 0);
     }
+  };
+  auto load_idx = [&](int tile, Idx &ix) {
+    load_rows(rselA, ia.w, tile, ix.a);
+    if constexpr (PAIRED) load_rows(rselB, ib.w, tile, ix.b);
     ix.own = 0;
     if (DROP && w < (PAIRED ? 4 : 2))
       ix.own = w < 2 ? __builtin_amdgcn_raw_buffer_load_b32(rselA, min(tile * kBN + lane, ia.w - 1) * 4, 0, 0)
@@ -155,11 +161,9 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
     return s;
   };
   auto cut = [&](f32x16 &s, int from) {
-    if (from + 32 > r) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (from + 8 * (e >> 2) + 4 * hf + (e & 3) >= r) s[e] = -INFINITY;
-    }
+    for (int e = 0; e < 16; ++e)
+      if (from + 8 * (e >> 2) + 4 * hf + (e & 3) >= r) s[e] = -INFINITY;
   };
   auto add = [&](const uint16_t *tile, const bf16x8 (&p)[2]) {
 #pragma unroll
@@ -183,8 +187,10 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.row(kt + 32 * kb * D, x), qf[x], s[kb], 0, 0, 0);
     interleave<D / 8, 1, 0>();
     gather_k(kn, ix);
-    cut(s[0], tile * kBN);
-    cut(s[1], tile * kBN + 32);
+    if (tile * kBN + kBN > r) {
+      cut(s[0], tile * kBN);
+      cut(s[1], tile * kBN + 32);
+    }
     float mx0 = fmaxf(s[0][0], s[0][1]), mx1 = fmaxf(s[1][0], s[1][1]);
 #pragma unroll
     for (int e = 2; e < 16; e += 2) {
@@ -213,8 +219,7 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
     const float neg_m = -m_run;
     bf16x8 pk[2][2];
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    auto weights = [&](int kb) {
       float p[16];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -230,11 +235,20 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
       }
       pk[kb][0] = pack8(p);
       pk[kb][1] = pack8(p + 8);
-    }
-    l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    };
+    weights(0);
     gather_v(vn, ix);
+    asm volatile("" : "+v"(pk[0][0]), "+v"(pk[0][1]), "+v"(at.col_at));
+    // the second block's weights beside the first's product
     add(vt, pk[0]);
+    weights(1);
+    interleave<D / 16, 2, D == 128 ? 7 : 14>();
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(acc[db]));
+    asm volatile("" : "+v"(pk[1][0]), "+v"(pk[1][1]), "+v"(at.col_at));
     add(vt + 32 * D, pk[1]);
+    interleave<D / 16, 2, 0>();
+    l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
   };
 
   // In phases, each with matrix products next to the vector work of another block of
@@ -278,13 +292,13 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
     s[0] = scores(kt, 0);
     interleave<D / 16, 1, 0>();
     asm volatile("" : "+v"(s[0]), "+v"(at.row_at));
-    cut(s[0], tile * kBN);
+    if (tile * kBN + 32 > r) cut(s[0], tile * kBN);
     weights(0);
     gradient(0);
     s[1] = scores(kt, 1);
     interleave<D / 16, 1, D == 128 ? 5 : 10>();
     asm volatile("" : "+v"(s[1]), "+v"(dsk[0][0]), "+v"(dsk[0][1]), "+v"(at.row_at));
-    cut(s[1], tile * kBN + 32);
+    if (tile * kBN + 64 > r) cut(s[1], tile * kBN + 32);
     weights(1);
     gradient(1);
     add(kt, dsk[0]);

@@ -327,55 +327,81 @@ __global__ __launch_bounds__(kThreads) void train_keys_kernel(TrainArgs a, T *dk
   store_column<T, D>(dv + kj * D, dva, a.kept_scale, hf);
 }
 
-// Work items of `rows` queries: per head the chunks of every cluster in cluster
+// What the kernels read besides the call's arrays, made by one launch: small calls
+// are bound by their launches (2 heads x 256 tokens, d = 64: prepared in four, 13
+// us; in one, 4 us).  A block has one of the roles below, in this order.
+struct Prepare {
+  int heads, n, c_q;
+  int list_blocks, mask_blocks, word_blocks;  // the statistics' blocks come last
+  const int32_t *offsets, *sel_counts, *sel_idx;
+  // lists of work items of rows[i] queries
+  int4 *items[2];
+  int rows[2], per_head[2];
+  uint32_t *masks;
+  int32_t *status;
+  const uint64_t *rng;
+  uint32_t *words;
+  const void *o, *d_o;
+  const float *lse;
+  float *stats;
+};
+
+// Work items of `rows` queries of head h: the chunks of every cluster in cluster
 // order as (cluster, first row, rows, selected keys), then empty ones.
-__global__ __launch_bounds__(1024) void train_items_kernel(int n, int c_q, int rows, int per_head,
-                                                           const int32_t *__restrict__ offsets,
-                                                           const int32_t *__restrict__ sel_counts, int4 *items) {
+__device__ void prepare_items(const Prepare &p, int h, int rows, int per_head, int4 *items) {
+  constexpr int PER = kTrainMaxClusters / 256;
   __shared__ int first[kTrainMaxClusters + 1];
-  __shared__ int wtot[16];
-  const int h = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
-  const int32_t *off = offsets + static_cast<size_t>(h) * (c_q + 1);
-  auto count_of = [&](int c) { return min(max(off[c + 1] - off[c], 0), n); };
-  const int k = t < c_q ? (count_of(t) + rows - 1) / rows : 0;
-  const int incl = wave_incl_scan(k);
+  __shared__ int wtot[4];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const int32_t *off = p.offsets + static_cast<size_t>(h) * (p.c_q + 1);
+  auto count_of = [&](int c) { return min(max(off[c + 1] - off[c], 0), p.n); };
+  int k[PER], mine = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    k[i] = PER * t + i < p.c_q ? (count_of(PER * t + i) + rows - 1) / rows : 0;
+    mine += k[i];
+  }
+  const int incl = wave_incl_scan(mine);
   if (lane == 63) wtot[w] = incl;
   __syncthreads();
-  int base = incl - k;
-  for (int i = 0; i < w; ++i) base += wtot[i];
-  if (t < c_q) first[t] = base;
-  if (t == c_q - 1) first[c_q] = base + k;
+  int at = incl - mine;
+  for (int i = 0; i < w; ++i) at += wtot[i];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    first[PER * t + i] = at;  // clusters past c_q: the total
+    at += k[i];
+  }
+  if (t == 255) first[kTrainMaxClusters] = at;
   __syncthreads();
-  const int total = first[c_q];
-  for (int slot = t; slot < per_head; slot += 1024) {
+  const int total = first[p.c_q];
+  for (int slot = t; slot < per_head; slot += 256) {
     int4 it = make_int4(0, 0, 0, 0);
     if (slot < total) {
-      int lo = 0, hi = c_q;  // first[lo] <= slot < first[hi]
+      int lo = 0, hi = p.c_q;  // first[lo] <= slot < first[hi]
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         if (first[mid] <= slot) lo = mid; else hi = mid;
       }
       const int row0 = (slot - first[lo]) * rows;
       it = make_int4(lo, row0, min(rows, count_of(lo) - row0),
-                     min(max(sel_counts[static_cast<size_t>(h) * c_q + lo], 0), n));
+                     min(max(p.sel_counts[static_cast<size_t>(h) * p.c_q + lo], 0), p.n));
     }
     items[static_cast<size_t>(h) * per_head + slot] = it;
   }
 }
 
-// Key bits: masks[head][key / 256][cluster][8 words].  A block turns one cluster's list
-// into the bits of kMaskWords words in LDS; a list that is not strictly ascending
-// or leaves [0, n) is reported, and its bits are those that the search finds.
-constexpr int kMaskWords = 1024;
-__global__ __launch_bounds__(256) void train_masks_kernel(int n, int c_q, const int32_t *__restrict__ sel_counts,
-                                                          const int32_t *__restrict__ sel_idx, uint32_t *masks,
-                                                          int32_t *status) {
-  __shared__ uint32_t bits[kMaskWords];
-  const int c = blockIdx.y, h = blockIdx.z, t = threadIdx.x;
-  const int r = min(max(sel_counts[static_cast<size_t>(h) * c_q + c], 0), n);
-  const int32_t *sel = sel_idx + (static_cast<size_t>(h) * c_q + c) * n;
-  const int from = blockIdx.x * 32 * kMaskWords, to = min(from + 32 * kMaskWords, n);
-  for (int i = t; i < kMaskWords; i += 256) bits[i] = 0;
+// Key bits: masks[head][key / 256][cluster][8 words].  A block turns the part of one
+// cluster's list with keys in [from, from + 8192) into bits in LDS; a list that is
+// not strictly ascending or leaves [0, n) is reported, and its bits are those that
+// the search finds.
+constexpr int kMaskKeys = 32 * 256;  // a word per thread
+__device__ void prepare_masks(const Prepare &p, int h, int c, int from, int segments) {
+  __shared__ uint32_t bits[256];
+  const int t = threadIdx.x, n = p.n;
+  const int r = min(max(p.sel_counts[static_cast<size_t>(h) * p.c_q + c], 0), n);
+  const int32_t *sel = p.sel_idx + (static_cast<size_t>(h) * p.c_q + c) * n;
+  const int to = min(from + kMaskKeys, n);
+  bits[t] = 0;
   auto below = [&](int x) {  // entries below x
     int lo = 0, hi = r;
     while (lo < hi) {
@@ -384,61 +410,77 @@ __global__ __launch_bounds__(256) void train_masks_kernel(int n, int c_q, const 
     }
     return lo;
   };
-  const int lo = gridDim.x > 1 ? below(from) : 0, hi = gridDim.x > 1 ? below(to) : r;
+  const int lo = segments == 1 ? 0 : below(from), hi = segments == 1 ? r : below(to);
   __syncthreads();
+  bool bad = false;
+  auto check = [&](int e, int j) { bad = bad || j < 0 || j >= n || (e > 0 && sel[e - 1] >= j); };
+#pragma unroll 4
   for (int e = lo + t; e < hi; e += 256) {
     const int j = sel[e];
     if (j >= from && j < to) atomicOr(&bits[(j - from) >> 5], 1u << (j & 31));
+    if (segments == 1) check(e, j);
   }
-  if (status) {
-    bool bad = false;
-    for (int e = from + t; e < min(to, r); e += 256) {
-      const int j = sel[e];
-      bad = bad || j < 0 || j >= n || (e > 0 && sel[e - 1] >= j);
-    }
-    if (bad) atomicOr(status, kStatusBadSet);
+  if (segments > 1) {  // entries that no segment's search finds are seen here
+#pragma unroll 4
+    for (int e = from + t; e < min(to, r); e += 256) check(e, sel[e]);
   }
+  if (bad && p.status) atomicOr(p.status, kStatusBadSet);
   __syncthreads();
   constexpr int WORDS = kTrainKeyBlock / 32;
-  const int blocks = (n + kTrainKeyBlock - 1) / kTrainKeyBlock, b0 = from / kTrainKeyBlock;
-  for (int i = t; i < kMaskWords && b0 + i / WORDS < blocks; i += 256)
-    masks[((static_cast<size_t>(h) * blocks + b0 + i / WORDS) * c_q + c) * WORDS + i % WORDS] = bits[i];
+  const int blocks = (n + kTrainKeyBlock - 1) / kTrainKeyBlock, b = from / kTrainKeyBlock + t / WORDS;
+  if (b < blocks) p.masks[((static_cast<size_t>(h) * blocks + b) * p.c_q + c) * WORDS + t % WORDS] = bits[t];
 }
 
 // The rows' statistics for the gradients: (-lse in the exp2 domain, <do, o>).
 // A row without keys has lse = -inf: its probabilities are exp2(-inf) = 0.  Row n
 // of a head is one of no weight, for the rows that fill up a tile.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void train_stats_kernel(size_t rows, int n, const T *__restrict__ o, const T *__restrict__ d_o,
-                                                          const float *__restrict__ lse, float *stats) {
+__device__ void prepare_stats(const Prepare &p, size_t block) {
   constexpr int PER = 16 / sizeof(T), LANES = D / PER;
-  const size_t i = (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x) / LANES;
+  const T *o = static_cast<const T *>(p.o), *d_o = static_cast<const T *>(p.d_o);
+  const size_t i = (block * 256 + threadIdx.x) / LANES, n = p.n;
   const int x = threadIdx.x % LANES;
-  if (i >= rows) return;  // rows * LANES is a multiple of LANES: whole groups
+  if (i >= p.heads * n) return;  // whole groups of LANES
   float s = 0.0f;
 #pragma unroll
   for (int e = 0; e < PER; ++e) s = fmaf(load_elem(o, i * D + PER * x + e), load_elem(d_o, i * D + PER * x + e), s);
 #pragma unroll
   for (int k = LANES / 2; k > 0; k /= 2) s += __shfl_xor(s, k, LANES);
-  if (x == 0) {
-    float *head = stats + (i / n) * 2 * (n + 1);
-    head[i % n] = lse[i] == -INFINITY ? -INFINITY : -lse[i] * kLog2e;
-    head[n + 1 + i % n] = s;
-    if (i % n == 0) {
-      head[n] = -INFINITY;
-      head[2 * n + 1] = 0.0f;
-    }
+  if (x) return;
+  float *head = p.stats + i / n * 2 * (n + 1);
+  head[i % n] = p.lse[i] == -INFINITY ? -INFINITY : -p.lse[i] * kLog2e;
+  head[n + 1 + i % n] = s;
+  if (i % n == 0) {
+    head[n] = -INFINITY;
+    head[2 * n + 1] = 0.0f;
   }
 }
 
-// Dropout's words: of the queries, then of the keys, per head.
-__global__ __launch_bounds__(256) void train_words_kernel(int n, const uint64_t *__restrict__ rng, uint32_t *words) {
-  const int i = blockIdx.x * 256 + threadIdx.x, side = blockIdx.y, h = blockIdx.z;
-  if (i >= n) return;
-  const uint2 x = pair_word(Stream(rng), i, h, side);
-  uint32_t *at = words + (4 * static_cast<size_t>(h) + 2 * side) * n + i;
-  at[0] = x.x;
-  at[n] = x.y;
+template <typename T, int D>
+__global__ __launch_bounds__(256) void train_prepare_kernel(Prepare p) {
+  int b = static_cast<int>(blockIdx.x);
+  if (b < p.list_blocks) {
+    const int i = b / p.heads;
+    prepare_items(p, b % p.heads, p.rows[i], p.per_head[i], p.items[i]);
+    return;
+  }
+  b -= p.list_blocks;
+  if (b < p.mask_blocks) {
+    const int segments = (p.n + kMaskKeys - 1) / kMaskKeys, hc = b / segments;
+    prepare_masks(p, hc / p.c_q, hc % p.c_q, b % segments * kMaskKeys, segments);
+    return;
+  }
+  b -= p.mask_blocks;
+  if (b < p.word_blocks) {  // dropout's words: of the queries, then of the keys, per head
+    const int per = (p.n + 255) / 256, h = b / per / 2, side = b / per % 2, i = b % per * 256 + threadIdx.x;
+    if (i >= p.n) return;
+    const uint2 x = pair_word(Stream(p.rng), i, h, side);
+    uint32_t *at = p.words + (4 * static_cast<size_t>(h) + 2 * side) * p.n + i;
+    at[0] = x.x;
+    at[p.n] = x.y;
+    return;
+  }
+  prepare_stats<T, D>(p, static_cast<size_t>(b - p.word_blocks));
 }
 
 template <typename K, typename... A>
@@ -453,57 +495,79 @@ hipError_t launch(K kernel, dim3 grid, int threads, hipStream_t s, A... args) {
     if (e_ != hipSuccess) return e_;     \
   } while (0)
 
-hipError_t common_setup(const TrainArgs &a, const TrainCall &c, hipStream_t s) {
-  if (a.drop)
-    TRAIN_TRY(launch(train_words_kernel, dim3((a.n + 255) / 256, 2, c.heads), 256, s, a.n, c.rng, const_cast<uint32_t *>(a.words)));
-  return hipSuccess;
-}
-
-hipError_t make_items(const TrainArgs &a, int heads, int rows, int per_head, int4 *items, hipStream_t s) {
-  return launch(train_items_kernel, dim3(heads), 1024, s, a.n, a.c_q, rows, per_head, a.offsets, a.sel_counts, items);
+// grad: masks and statistics too.
+template <typename T, int D>
+hipError_t prepare(const TrainArgs &a, const TrainCall &c, bool grad, hipStream_t s) {
+  Prepare p{};
+  p.heads = c.heads;
+  p.n = a.n;
+  p.c_q = a.c_q;
+  p.offsets = a.offsets;
+  p.sel_counts = a.sel_counts;
+  p.sel_idx = a.sel_idx;
+  int lists = 0;
+  auto list = [&](int4 *items, int rows) {
+    p.items[lists] = items;
+    p.rows[lists] = rows;
+    p.per_head[lists++] = train_items_per_head(a.n, a.c_q, rows);
+  };
+  if (sizeof(T) == 4) list(c.items, kRows);
+  if (grad) list(c.tiles, sizeof(T) == 4 ? kTile : kTrainKeyTile);
+  p.list_blocks = lists * c.heads;
+  p.word_blocks = a.drop ? 2 * c.heads * ((a.n + 255) / 256) : 0;
+  p.rng = c.rng;
+  p.words = const_cast<uint32_t *>(a.words);
+  size_t stats = 0;
+  if (grad) {
+    p.mask_blocks = c.heads * a.c_q * ((a.n + kMaskKeys - 1) / kMaskKeys);
+    p.masks = const_cast<uint32_t *>(a.masks);
+    p.status = c.status;
+    p.o = c.o;
+    p.d_o = a.d_o;
+    p.lse = a.lse;
+    p.stats = const_cast<float *>(a.stats);
+    stats = (a.rows * (D * sizeof(T) / 16) + 255) / 256;
+  }
+  const size_t blocks = p.list_blocks + static_cast<size_t>(p.mask_blocks) + p.word_blocks + stats;
+  if (!blocks) return hipSuccess;
+  return launch(train_prepare_kernel<T, D>, dim3(static_cast<unsigned>(blocks)), 256, s, p);
 }
 
 template <typename T, int D>
 hipError_t forward(TrainArgs a, const TrainCall &c, hipStream_t s) {
-  TRAIN_TRY(common_setup(a, c, s));
-  if constexpr (sizeof(T) == 2) return train_queries(D, false, a, c.heads, c.slots, static_cast<T *>(c.o), s);
-  a.items = c.items;
-  a.items_per_head = train_items_per_head(a.n, a.c_q, kRows);
-  TRAIN_TRY(make_items(a, c.heads, kRows, a.items_per_head, c.items, s));
-  const dim3 grid(static_cast<unsigned>(c.heads) * a.items_per_head);
-  return a.drop ? launch(train_queries_kernel<T, D, false, true>, grid, kThreads, s, a, static_cast<T *>(c.o))
-                : launch(train_queries_kernel<T, D, false, false>, grid, kThreads, s, a, static_cast<T *>(c.o));
+  TRAIN_TRY((prepare<T, D>(a, c, false, s)));
+  if constexpr (sizeof(T) == 2) {
+    return train_queries(D, false, a, c.heads, c.slots, static_cast<T *>(c.o), s);
+  } else {
+    a.items = c.items;
+    a.items_per_head = train_items_per_head(a.n, a.c_q, kRows);
+    const dim3 grid(static_cast<unsigned>(c.heads) * a.items_per_head);
+    return a.drop ? launch(train_queries_kernel<T, D, false, true>, grid, kThreads, s, a, static_cast<T *>(c.o))
+                  : launch(train_queries_kernel<T, D, false, false>, grid, kThreads, s, a, static_cast<T *>(c.o));
+  }
 }
 
 template <typename T, int D>
 hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
-  TRAIN_TRY(common_setup(a, c, s));
-  const size_t rows = static_cast<size_t>(c.heads) * a.n, lanes = D * sizeof(T) / 16;
-  TRAIN_TRY(launch(train_stats_kernel<T, D>, dim3((rows * lanes + 255) / 256), 256, s, rows, a.n, static_cast<const T *>(c.o),
-                   static_cast<const T *>(a.d_o), a.lse, const_cast<float *>(a.stats)));
-  const int segments = (a.n + 32 * kMaskWords - 1) / (32 * kMaskWords);
-  TRAIN_TRY(launch(train_masks_kernel, dim3(segments, a.c_q, c.heads), 256, s, a.n, a.c_q, a.sel_counts, a.sel_idx,
-                   const_cast<uint32_t *>(a.masks), c.status));
+  TRAIN_TRY((prepare<T, D>(a, c, true, s)));
+  T *dq = static_cast<T *>(c.dq), *dk = static_cast<T *>(c.dk), *dv = static_cast<T *>(c.dv);
   if constexpr (sizeof(T) == 2) {
-    TRAIN_TRY(train_queries(D, true, a, c.heads, c.slots, static_cast<T *>(c.dq), s));
+    TRAIN_TRY(train_queries(D, true, a, c.heads, c.slots, dq, s));
     a.items = c.tiles;
     a.items_per_head = train_items_per_head(a.n, a.c_q, kTrainKeyTile);
-    TRAIN_TRY(make_items(a, c.heads, kTrainKeyTile, a.items_per_head, c.tiles, s));
-    return train_keys(D, a, c.heads, train_key_splits(c.heads, a.n, a.c_q), c.parts, static_cast<T *>(c.dk),
-                      static_cast<T *>(c.dv), s);
+    return train_keys(D, a, c.heads, train_key_splits(c.heads, a.n, a.c_q), c.parts, dk, dv, s);
+  } else {
+    a.items = c.items;
+    a.items_per_head = train_items_per_head(a.n, a.c_q, kRows);
+    const dim3 qgrid(static_cast<unsigned>(c.heads) * a.items_per_head);
+    TRAIN_TRY(a.drop ? launch(train_queries_kernel<T, D, true, true>, qgrid, kThreads, s, a, dq)
+                     : launch(train_queries_kernel<T, D, true, false>, qgrid, kThreads, s, a, dq));
+    a.items = c.tiles;
+    a.items_per_head = train_items_per_head(a.n, a.c_q, kTile);
+    const dim3 kgrid(static_cast<unsigned>(c.heads) * ((a.n + kRows - 1) / kRows));
+    return a.drop ? launch(train_keys_kernel<T, D, true>, kgrid, kThreads, s, a, dk, dv)
+                  : launch(train_keys_kernel<T, D, false>, kgrid, kThreads, s, a, dk, dv);
   }
-  a.items = c.items;
-  a.items_per_head = train_items_per_head(a.n, a.c_q, kRows);
-  TRAIN_TRY(make_items(a, c.heads, kRows, a.items_per_head, c.items, s));
-  const dim3 qgrid(static_cast<unsigned>(c.heads) * a.items_per_head);
-  TRAIN_TRY(a.drop ? launch(train_queries_kernel<T, D, true, true>, qgrid, kThreads, s, a, static_cast<T *>(c.dq))
-                   : launch(train_queries_kernel<T, D, true, false>, qgrid, kThreads, s, a, static_cast<T *>(c.dq)));
-  a.items = c.tiles;
-  a.items_per_head = train_items_per_head(a.n, a.c_q, kTile);
-  TRAIN_TRY(make_items(a, c.heads, kTile, a.items_per_head, c.tiles, s));
-  const dim3 kgrid(static_cast<unsigned>(c.heads) * ((a.n + kRows - 1) / kRows));
-  return a.drop ? launch(train_keys_kernel<T, D, true>, kgrid, kThreads, s, a, static_cast<T *>(c.dk), static_cast<T *>(c.dv))
-                : launch(train_keys_kernel<T, D, false>, kgrid, kThreads, s, a, static_cast<T *>(c.dk), static_cast<T *>(c.dv));
 }
 
 }  // namespace
