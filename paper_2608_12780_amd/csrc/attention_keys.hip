@@ -295,24 +295,6 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
     }
 }
 
-// The parts' sums in part order, scaled and rounded once.
-__global__ __launch_bounds__(256) void join_keys_kernel(size_t count, int splits, float scale_k, float scale_v,
-                                                        const float *__restrict__ parts, uint16_t *dk, uint16_t *dv) {
-  const size_t i = 4 * (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x);
-  if (i >= count) return;
-  const int v = blockIdx.y;
-  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int p = 0; p < splits; ++p) {
-    const float4 x = *reinterpret_cast<const float4 *>(parts + (2 * static_cast<size_t>(p) + v) * count + i);
-    s.x += x.x;
-    s.y += x.y;
-    s.z += x.z;
-    s.w += x.w;
-  }
-  const float f = v ? scale_v : scale_k;
-  *reinterpret_cast<uint2 *>((v ? dv : dk) + i) = make_uint2(pack_bf16(s.x * f, s.y * f), pack_bf16(s.z * f, s.w * f));
-}
-
 template <int D>
 hipError_t run(const TrainArgs &a, int heads, int splits, float *parts, uint16_t *dk, uint16_t *dv, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(heads) * splits * ((a.n + kTrainKeyBlock - 1) / kTrainKeyBlock));
@@ -320,35 +302,10 @@ hipError_t run(const TrainArgs &a, int heads, int splits, float *parts, uint16_t
     hipLaunchKernelGGL((grad_keys_kernel<D, true>), grid, dim3(kThreads), 0, s, a, splits, dk, dv, parts);
   else
     hipLaunchKernelGGL((grad_keys_kernel<D, false>), grid, dim3(kThreads), 0, s, a, splits, dk, dv, parts);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || splits == 1) return e;
-  const size_t count = a.rows * D;
-  hipLaunchKernelGGL(join_keys_kernel, dim3(static_cast<unsigned>((count / 4 + 255) / 256), 2), dim3(256), 0, s, count,
-                     splits, a.scale, a.kept_scale, parts, dk, dv);
   return hipGetLastError();
 }
 
 }  // namespace
-
-// Parts of the query tiles, each with fp32 sums of its own that a second kernel adds.
-// The chip holds one block per CU: as many parts, up to 16 of two tiles or more, as
-// make the launch's rounds shortest, a part costing about 2% of a round more (its
-// start, its sums).  3 heads x 2185 tokens (27 key blocks): TODO.
-int train_key_splits(int heads, int n, int c_q) {
-  constexpr int kMost = 16, kCus = 256;
-  const long long blocks = static_cast<long long>(heads) * ((n + kTrainKeyBlock - 1) / kTrainKeyBlock);
-  const long long tiles = train_items_per_head(n, c_q, kTrainKeyTile);
-  int best = 1;
-  double least = 0.0;
-  for (int s = 1; s <= kMost && (s == 1 || 2 * s <= tiles); ++s) {
-    const double rounds = static_cast<double>((blocks * s + kCus - 1) / kCus) * (1.0 / s + 0.02);
-    if (s == 1 || rounds < least) {
-      least = rounds;
-      best = s;
-    }
-  }
-  return best;
-}
 
 hipError_t train_keys(int d, const TrainArgs &a, int heads, int splits, float *parts, uint16_t *dk, uint16_t *dv, hipStream_t s) {
   return d == 128 ? run<128>(a, heads, splits, parts, dk, dv, s) : run<64>(a, heads, splits, parts, dk, dv, s);

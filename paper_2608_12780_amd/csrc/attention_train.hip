@@ -23,162 +23,114 @@ namespace scope {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kThreads = 256;               // four waves
-constexpr int kRows = 32 * kThreads / 64;   // rows (queries or keys) per block
+
+// fp32 inputs: fp32 matrix products, 16 x 16 results from 4 channels (or rows) per
+// instruction, so that inputs, weights and ds are not rounded.  They run at a
+// sixteenth of the bf16 rate and need little bandwidth: a wave owns 16 queries
+// (or keys), four a block, which leaves registers for three waves per SIMD to cover
+// the staging of tiles, and short work items for an even load.
+constexpr int kThreads = 256;
+constexpr int kRows = 16 * kThreads / 64;   // rows (queries or keys) per block
 constexpr int kTile = 32;                   // gathered rows per step
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// A wave's 32 x 32 matrix product in the tensors' type: bf16 operands of 16
-// channels per instruction, or fp32 operands (no rounding) of four times two.
-template <typename T>
-struct Mma;
-template <>
-struct Mma<uint16_t> {
-  typedef bf16x8 Frag;
-  static constexpr int kLane = 8;  // channels per lane and fragment
-  static constexpr int kPad = 32;
-  static __device__ __forceinline__ void product(f32x16 &acc, Frag a, Frag b) {
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
-  }
-};
-template <>
-struct Mma<float> {
-  typedef float4 Frag;
-  static constexpr int kLane = 4;
-  static constexpr int kPad = 4;
-  static __device__ __forceinline__ void product(f32x16 &acc, Frag a, Frag b) {
-    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, b.x, acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, b.y, acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, b.z, acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, b.w, acc, 0, 0, 0);
-  }
-};
-
-// Tile of kTile rows in LDS, and the two products that read it.
-template <typename T, int D>
+// Tile of kTile rows in LDS.  16 bytes of padding keep 16 rows' 16-byte reads, and
+// rows four apart, on distinct banks.
+template <int D>
 struct Tile {
-  typedef typename Mma<T>::Frag Frag;
-  static constexpr int kStride = D + Mma<T>::kPad;
-  static constexpr int kSteps = D / (2 * Mma<T>::kLane);
-  T x[kTile * kStride];
+  static constexpr int kStride = D + 4;
+  float x[kTile * kStride];
 
-  // this lane's fragments of a row of a tensor (zeros where there is none)
-  static __device__ __forceinline__ void fragments(Frag (&f)[kSteps], const T *row, bool valid, int hf) {
+  // rows 16 b .. of the tile . columns^T: element r of a lane is row 4 g + r
+  __device__ __forceinline__ f32x4 scores(const float4 (&f)[D / 16], int b, int l16, int g) const {
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-      f[s] = valid ? *reinterpret_cast<const Frag *>(row + Mma<T>::kLane * (2 * s + hf)) : Frag{};
-  }
-  // tile . columns^T: element e of a lane is row 8 (e / 4) + 4 hf + e % 4 of its column
-  __device__ __forceinline__ f32x16 scores(const Frag (&f)[kSteps], int l32, int hf) const {
-    f32x16 acc;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-      Mma<T>::product(acc, *reinterpret_cast<const Frag *>(&x[l32 * kStride + Mma<T>::kLane * (2 * s + hf)]), f[s]);
+    for (int s = 0; s < D / 16; ++s) {
+      const float4 t = *reinterpret_cast<const float4 *>(&x[(16 * b + l16) * kStride + 16 * s + 4 * g]);
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(t.x, f[s].x, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(t.y, f[s].y, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(t.z, f[s].z, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(t.w, f[s].w, acc, 0, 0, 0);
+    }
     return acc;
   }
+  // out += (rows 16 b .. of the tile)^T . w, w in the layout of scores(); row m of
+  // out[cb] is channel 64 (cb / 4) + 4 m + cb % 4, so that a lane reads 16 bytes
+  __device__ __forceinline__ void accumulate(f32x4 (&out)[D / 16], const float (&w)[4], int b, int l16, int g) const {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+        const float4 t = *reinterpret_cast<const float4 *>(&x[(16 * b + 4 * g + r) * kStride + 64 * c + 4 * l16]);
+        out[4 * c] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.x, w[r], out[4 * c], 0, 0, 0);
+        out[4 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.y, w[r], out[4 * c + 1], 0, 0, 0);
+        out[4 * c + 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.z, w[r], out[4 * c + 2], 0, 0, 0);
+        out[4 * c + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.w, w[r], out[4 * c + 3], 0, 0, 0);
+      }
+  }
 };
 
-// out += tile^T . w, w in the layout of scores()
+// This lane's fragments of a row (zeros where there is none), and its share of the
+// results times `f` into the row of its column.
 template <int D>
-__device__ __forceinline__ void accumulate_tile(const Tile<uint16_t, D> &t, f32x16 (&out)[D / 32],
-                                                const float (&w)[16], int lane) {
-  constexpr int S = Tile<uint16_t, D>::kStride;
-  // transposing reads, as the forward attention's V: row 4 (lane / 32) +
-  // (lane % 16) / 4 of a 16-row step, channels 16 ((lane / 16) % 2) + 4 (lane % 4)
-  const int at = (4 * (lane >> 5) + ((lane & 15) >> 2)) * S + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+__device__ __forceinline__ void load_row(float4 (&f)[D / 16], const float *row, bool valid, int g) {
 #pragma unroll
-  for (int s2 = 0; s2 < 2; ++s2) {
-    const bf16x8 b = as_bf16x8(make_uint4(pack_bf16(w[8 * s2 + 0], w[8 * s2 + 1]), pack_bf16(w[8 * s2 + 2], w[8 * s2 + 3]),
-                                          pack_bf16(w[8 * s2 + 4], w[8 * s2 + 5]), pack_bf16(w[8 * s2 + 6], w[8 * s2 + 7])));
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) {
-      const uint16_t *p = &t.x[16 * s2 * S + 32 * db + at];
-      const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(p)));
-      const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(p + 8 * S)));
-      out[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(make_uint4(lo.x, lo.y, hi.x, hi.y)), b, out[db], 0, 0, 0);
-    }
-  }
+  for (int s = 0; s < D / 16; ++s)
+    f[s] = valid ? *reinterpret_cast<const float4 *>(row + 16 * s + 4 * g) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 }
 template <int D>
-__device__ __forceinline__ void accumulate_tile(const Tile<float, D> &t, f32x16 (&out)[D / 32],
-                                                const float (&w)[16], int lane) {
-  const int l32 = lane & 31, hf = lane >> 5;
+__device__ __forceinline__ void store_row(float *row, const f32x4 (&acc)[D / 16], float f, int g) {
 #pragma unroll
-  for (int e = 0; e < 16; ++e)
+  for (int c = 0; c < D / 64; ++c)
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-      out[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(
-          t.x[(8 * (e >> 2) + 4 * hf + (e & 3)) * Tile<float, D>::kStride + 32 * db + l32], w[e], out[db], 0, 0, 0);
+    for (int r = 0; r < 4; ++r)
+      *reinterpret_cast<float4 *>(row + 64 * c + 4 * (4 * g + r)) =
+          make_float4(acc[4 * c][r] * f, acc[4 * c + 1][r] * f, acc[4 * c + 2][r] * f, acc[4 * c + 3][r] * f);
 }
 
-// 16 bytes of a row, `valid` or zeros.
-template <typename T>
-__device__ __forceinline__ uint4 row_chunk(const T *base, size_t row, int d, int chunk, bool valid) {
-  return valid ? *reinterpret_cast<const uint4 *>(base + row * d + chunk * (16 / sizeof(T))) : make_uint4(0, 0, 0, 0);
+__device__ __forceinline__ float4 row_chunk(const float *base, size_t row, int d, int chunk, bool valid) {
+  return valid ? *reinterpret_cast<const float4 *>(base + row * d + 4 * chunk) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 }
 
-// A lane's 16 rows of D x 32 results times `f`, into the row of its column.
-template <typename T, int D>
-__device__ __forceinline__ void store_column(T *row, const f32x16 (&acc)[D / 32], float f, int hf) {
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      T *at = row + 32 * db + 8 * i + 4 * hf;
-      const float a = acc[db][4 * i] * f, b = acc[db][4 * i + 1] * f, c = acc[db][4 * i + 2] * f, d = acc[db][4 * i + 3] * f;
-      if constexpr (sizeof(T) == 2)
-        *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
-      else
-        *reinterpret_cast<float4 *>(at) = make_float4(a, b, c, d);
-    }
-}
-
-__device__ __forceinline__ int row_of(int e, int hf) { return 8 * (e >> 2) + 4 * hf + (e & 3); }
-
-// One wave per 32 queries of a cluster, over the cluster's keys: the forward
+// One wave per 16 queries of a cluster, over the cluster's keys: the forward
 // (GRAD false) or dq (GRAD true).
-template <typename T, int D, bool GRAD, bool DROP>
-__global__ __launch_bounds__(kThreads) void train_queries_kernel(TrainArgs a, T *out) {
-  typedef Tile<T, D> TileT;
-  constexpr int CH = D * sizeof(T) / 16;              // 16-byte chunks of a row
-  constexpr int PER = kTile * CH / kThreads;          // of each tile per thread
-  static_assert(kTile * CH % kThreads == 0, "tile/threads mismatch");
-  __shared__ __attribute__((aligned(16))) TileT K, V;
+template <int D, bool GRAD, bool DROP>
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 3))) void train_queries_kernel(TrainArgs a, float *out) {
+  constexpr int CH = D / 4, PER = kTile * CH / kThreads;  // 16-byte chunks of a row; per thread and tile
+  __shared__ __attribute__((aligned(16))) Tile<D> K, V;
   __shared__ uint2 words[kTile];
   const int4 it = a.items[blockIdx.x];
   const int h = static_cast<int>(blockIdx.x) / a.items_per_head;
   const int c = it.x, row0 = it.y, rows = it.z, r = it.w;
   if (rows <= 0) return;
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6, l32 = lane & 31, hf = lane >> 5;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, l16 = lane & 15, g = lane >> 4;
   const size_t first = static_cast<size_t>(h) * a.n;
-  const T *k = static_cast<const T *>(a.k) + first * D, *v = static_cast<const T *>(a.v) + first * D;
-  const int ql = 32 * w + l32;
-  const bool valid = ql < rows;
-  size_t qi = first;
+  const float *k = static_cast<const float *>(a.k) + first * D, *v = static_cast<const float *>(a.v) + first * D;
+  const int ql = 16 * w + l16;
+  const bool valid = ql < rows, active = 16 * w < rows;
+  int qi = 0;
   if (valid) {
     const int pos = min(max(a.offsets[static_cast<size_t>(h) * (a.c_q + 1) + c] + row0 + ql, 0), a.n - 1);
-    qi += min(max(a.perm[first + pos], 0), a.n - 1);
+    qi = min(max(a.perm[first + pos], 0), a.n - 1);
   }
-  typename TileT::Frag qf[TileT::kSteps], gf[GRAD ? TileT::kSteps : 1];
-  TileT::fragments(qf, static_cast<const T *>(a.q) + qi * D, valid, hf);
+  float4 qf[D / 16], gf[GRAD ? D / 16 : 1];
+  load_row<D>(qf, static_cast<const float *>(a.q) + (first + qi) * D, valid, g);
   float neg_lse = -INFINITY, delta = 0.0f;
   if constexpr (GRAD) {
-    TileT::fragments(gf, static_cast<const T *>(a.d_o) + qi * D, valid, hf);
+    load_row<D>(gf, static_cast<const float *>(a.d_o) + (first + qi) * D, valid, g);
     if (valid) {
-      const float *st = a.stats + 2 * h * static_cast<size_t>(a.n + 1) + (qi - first);
+      const float *st = a.stats + 2 * h * static_cast<size_t>(a.n + 1) + qi;
       neg_lse = st[0];
       delta = st[a.n + 1];
     }
   }
   uint2 mine = make_uint2(0, 0);
   const uint32_t *wq = a.words + 4 * first, *wk = wq + 2 * static_cast<size_t>(a.n);
-  if (DROP && valid) mine = make_uint2(wq[qi - first], wq[qi - first + a.n]);
-  f32x16 acc[D / 32];
+  if (DROP && valid) mine = make_uint2(wq[qi], wq[qi + a.n]);
+  f32x4 acc[D / 16];
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[db][e] = 0.0f;
+  for (int cb = 0; cb < D / 16; ++cb) acc[cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m = -INFINITY, l = 0.0f;
   const int32_t *sel = a.sel_idx + (static_cast<size_t>(h) * a.c_q + c) * a.n;
   for (int k0 = 0; k0 < r; k0 += kTile) {
@@ -188,20 +140,27 @@ __global__ __launch_bounds__(kThreads) void train_queries_kernel(TrainArgs a, T 
       const int at = i * kThreads + t, row = at / CH, chunk = at % CH;
       const bool in = k0 + row < r;
       const int j = in ? min(max(sel[k0 + row], 0), a.n - 1) : 0;
-      *reinterpret_cast<uint4 *>(&K.x[row * TileT::kStride + chunk * (16 / sizeof(T))]) = row_chunk(k, j, D, chunk, in);
-      *reinterpret_cast<uint4 *>(&V.x[row * TileT::kStride + chunk * (16 / sizeof(T))]) = row_chunk(v, j, D, chunk, in);
+      *reinterpret_cast<float4 *>(&K.x[row * K.kStride + 4 * chunk]) = row_chunk(k, j, D, chunk, in);
+      *reinterpret_cast<float4 *>(&V.x[row * K.kStride + 4 * chunk]) = row_chunk(v, j, D, chunk, in);
       if (DROP && chunk == 0) words[row] = make_uint2(wk[j], wk[j + a.n]);
     }
     __syncthreads();
-    const f32x16 s = K.scores(qf, l32, hf);
-    float p[16];
+    if (!active) continue;
+    f32x4 s[2];
+    float p[2][4];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) s[b] = K.scores(qf, b, l16, g);
+    auto in_list = [&](int b, int e) { return k0 + 16 * b + 4 * g + e < r; };
     if constexpr (!GRAD) {
       float top = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        p[e] = k0 + row_of(e, hf) < r ? s[e] : -INFINITY;
-        top = fmaxf(top, p[e]);
-      }
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[b][e] = in_list(b, e) ? s[b][e] : -INFINITY;
+          top = fmaxf(top, p[b][e]);
+        }
+      top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       const float m_new = fmaxf(m, top * a.scale_log2);
       const float neg = m_new == -INFINITY ? 0.0f : -m_new;
@@ -209,122 +168,132 @@ __global__ __launch_bounds__(kThreads) void train_queries_kernel(TrainArgs a, T 
       m = m_new;
       l *= alpha;
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db)
+      for (int cb = 0; cb < D / 16; ++cb) acc[cb] *= alpha;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[db][e] *= alpha;
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], a.scale_log2, neg));
-        l += p[e];
-        if (DROP && !pair_kept(mine, words[row_of(e, hf)], a.drop)) p[e] = 0.0f;
-      }
-      accumulate_tile<D>(V, acc, p, lane);
+        for (int e = 0; e < 4; ++e) {
+          p[b][e] = __builtin_amdgcn_exp2f(fmaf(p[b][e], a.scale_log2, neg));
+          l += p[b][e];
+          if (DROP && !pair_kept(mine, words[16 * b + 4 * g + e], a.drop)) p[b][e] = 0.0f;
+        }
+#pragma unroll
+      for (int b = 0; b < 2; ++b) V.accumulate(acc, p[b], b, l16, g);
     } else {
-      const f32x16 dp = V.scores(gf, l32, hf);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        float g = dp[e];
-        if (DROP) g = pair_kept(mine, words[row_of(e, hf)], a.drop) ? g * a.kept_scale : 0.0f;
-        const float pe = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, neg_lse));
-        p[e] = k0 + row_of(e, hf) < r ? pe * (g - delta) : 0.0f;
+      for (int b = 0; b < 2; ++b) {
+        const f32x4 dp = V.scores(gf, b, l16, g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float x = dp[e];
+          if (DROP) x = pair_kept(mine, words[16 * b + 4 * g + e], a.drop) ? x * a.kept_scale : 0.0f;
+          const float pe = __builtin_amdgcn_exp2f(fmaf(s[b][e], a.scale_log2, neg_lse));
+          p[b][e] = in_list(b, e) ? pe * (x - delta) : 0.0f;
+        }
       }
-      accumulate_tile<D>(K, acc, p, lane);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) K.accumulate(acc, p[b], b, l16, g);
     }
   }
+  float f = a.scale;
   if constexpr (!GRAD) {
+    l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (!valid) return;
-    store_column<T, D>(out + qi * D, acc, l > 0.0f ? a.kept_scale / l : 0.0f, hf);
-    if (hf == 0) a.lse[qi] = l > 0.0f ? (m + __log2f(l)) * kLn2 : l == 0.0f ? -INFINITY : l;
-  } else {
-    if (!valid) return;
-    store_column<T, D>(out + qi * D, acc, a.scale, hf);
+    f = l > 0.0f ? a.kept_scale / l : 0.0f;
+    if (valid && g == 0) a.lse[first + qi] = l > 0.0f ? (m + __log2f(l)) * kLn2 : l == 0.0f ? -INFINITY : l;
   }
+  if (valid) store_row<D>(out + (first + qi) * D, acc, f, g);
 }
 
-// One wave per 32 keys, over the queries of every cluster that keeps any of the
-// block's keys: dk and dv.
-template <typename T, int D, bool DROP>
-__global__ __launch_bounds__(kThreads) void train_keys_kernel(TrainArgs a, T *dk, T *dv) {
-  typedef Tile<T, D> TileT;
-  constexpr int CH = D * sizeof(T) / 16;
-  constexpr int PER = kTile * CH / kThreads;
-  __shared__ __attribute__((aligned(16))) TileT Q, G;
+// One wave per 16 keys, over the queries of every cluster that keeps any of the
+// block's keys: dk and dv, or with several parts their sums over a part's tiles.
+template <int D, bool DROP>
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void train_keys_kernel(TrainArgs a, int splits, float *dk, float *dv, float *parts) {
+  constexpr int CH = D / 4, PER = kTile * CH / kThreads;
+  __shared__ __attribute__((aligned(16))) Tile<D> Q, G;
   __shared__ float2 stats[kTile];
   __shared__ uint2 words[kTile];
   const int blocks = (a.n + kRows - 1) / kRows;
-  const int h = static_cast<int>(blockIdx.x) / blocks, b = static_cast<int>(blockIdx.x) % blocks;
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6, l32 = lane & 31, hf = lane >> 5;
+  const int b = static_cast<int>(blockIdx.x) % blocks, part = static_cast<int>(blockIdx.x) / blocks % splits;
+  const int h = static_cast<int>(blockIdx.x) / blocks / splits;
+  const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const size_t first = static_cast<size_t>(h) * a.n;
-  const T *q = static_cast<const T *>(a.q), *g = static_cast<const T *>(a.d_o);
-  const int j = b * kRows + 32 * w + l32;
+  const float *q = static_cast<const float *>(a.q), *d_o = static_cast<const float *>(a.d_o);
+  const int j = b * kRows + 16 * w + l16;
   const bool valid = j < a.n;
   const size_t kj = first + (valid ? j : 0);
-  typename TileT::Frag kf[TileT::kSteps], vf[TileT::kSteps];
-  TileT::fragments(kf, static_cast<const T *>(a.k) + kj * D, valid, hf);
-  TileT::fragments(vf, static_cast<const T *>(a.v) + kj * D, valid, hf);
+  float4 kf[D / 16], vf[D / 16];
+  load_row<D>(kf, static_cast<const float *>(a.k) + kj * D, valid, g);
+  load_row<D>(vf, static_cast<const float *>(a.v) + kj * D, valid, g);
   uint2 mine = make_uint2(0, 0);
   const uint32_t *wq = a.words + 4 * first, *wk = wq + 2 * static_cast<size_t>(a.n);
   if (DROP) mine = make_uint2(wk[kj - first], wk[kj - first + a.n]);
-  f32x16 dka[D / 32], dva[D / 32];
+  f32x4 dka[D / 16], dva[D / 16];
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) dka[db][e] = dva[db][e] = 0.0f;
-  // the block's four words of each cluster, one per wave
+  for (int cb = 0; cb < D / 16; ++cb) dka[cb] = dva[cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  // the block's two words of each cluster, 16 bits a wave
   constexpr int WORDS = kTrainKeyBlock / 32, SHARE = kTrainKeyBlock / kRows;
-  const uint32_t *masks = a.masks + (static_cast<size_t>(h) * ((blocks + SHARE - 1) / SHARE) + b / SHARE) * a.c_q * WORDS +
+  const uint32_t *masks = a.masks + (static_cast<size_t>(h) * ((a.n + kTrainKeyBlock - 1) / kTrainKeyBlock) + b / SHARE) * a.c_q * WORDS +
                           kRows / 32 * (b % SHARE);
-  for (int i = 0; i < a.items_per_head; ++i) {
+  const int per = (a.items_per_head + splits - 1) / splits, end = min((part + 1) * per, a.items_per_head);
+  for (int i = part * per; i < end; ++i) {
     const int4 it = a.items[static_cast<size_t>(h) * a.items_per_head + i];
     const int c = it.x, row0 = it.y, rows = it.z;
     if (rows <= 0) break;
-    uint32_t any = 0, own = 0;
-    for (int x = 0; x < kRows / 32; ++x) {
-      const uint32_t m = masks[c * WORDS + x];
-      any |= m;
-      if (x == w) own = m;
-    }
-    if (!any) continue;
-    const bool kept = (own >> l32) & 1u;
+    const uint32_t m0 = masks[c * WORDS], m1 = masks[c * WORDS + 1];
+    if (!(m0 | m1)) continue;
+    const uint32_t own = (w & 2 ? m1 : m0) >> (16 * (w & 1)) & 0xFFFFu;
+    const bool kept = (own >> l16) & 1u;
     const int base = a.offsets[static_cast<size_t>(h) * (a.c_q + 1) + c] + row0;
     __syncthreads();
 #pragma unroll
     for (int x = 0; x < PER; ++x) {
       const int at = x * kThreads + t, row = at / CH, chunk = at % CH;
       const bool in = row < rows;
-      const size_t qi = first + (in ? min(max(a.perm[first + min(max(base + row, 0), a.n - 1)], 0), a.n - 1) : 0);
-      *reinterpret_cast<uint4 *>(&Q.x[row * TileT::kStride + chunk * (16 / sizeof(T))]) = row_chunk(q, qi, D, chunk, in);
-      *reinterpret_cast<uint4 *>(&G.x[row * TileT::kStride + chunk * (16 / sizeof(T))]) = row_chunk(g, qi, D, chunk, in);
+      const int qi = in ? min(max(a.perm[first + min(max(base + row, 0), a.n - 1)], 0), a.n - 1) : 0;
+      *reinterpret_cast<float4 *>(&Q.x[row * Q.kStride + 4 * chunk]) = row_chunk(q, first + qi, D, chunk, in);
+      *reinterpret_cast<float4 *>(&G.x[row * Q.kStride + 4 * chunk]) = row_chunk(d_o, first + qi, D, chunk, in);
       if (chunk == 0) {
-        const float *st = a.stats + 2 * h * static_cast<size_t>(a.n + 1) + (in ? qi - first : a.n);
+        const float *st = a.stats + 2 * h * static_cast<size_t>(a.n + 1) + (in ? qi : a.n);
         stats[row] = make_float2(st[0], st[a.n + 1]);
-        if (DROP) words[row] = make_uint2(wq[qi - first], wq[qi - first + a.n]);
+        if (DROP) words[row] = make_uint2(wq[qi], wq[qi + a.n]);
       }
     }
     __syncthreads();
     if (!own) continue;
-    const f32x16 s = Q.scores(kf, l32, hf), dp = G.scores(vf, l32, hf);
-    float p[16], ds[16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int row = row_of(e, hf);
-      const float2 st = stats[row];
-      float pe = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, st.x)), gp = dp[e];
-      p[e] = kept ? pe : 0.0f;
-      if (DROP) {
-        const bool keep = pair_kept(words[row], mine, a.drop);
-        gp = keep ? gp * a.kept_scale : 0.0f;
-        if (!keep) p[e] = 0.0f;
+    for (int qb = 0; qb < 2; ++qb) {
+      const f32x4 s = Q.scores(kf, qb, l16, g), dp = G.scores(vf, qb, l16, g);
+      float p[4], ds[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = 16 * qb + 4 * g + e;
+        const float2 st = stats[row];
+        const float pe = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, st.x));
+        float x = dp[e];
+        p[e] = kept ? pe : 0.0f;
+        if (DROP) {
+          const bool keep = pair_kept(words[row], mine, a.drop);
+          x = keep ? x * a.kept_scale : 0.0f;
+          if (!keep) p[e] = 0.0f;
+        }
+        ds[e] = kept ? pe * (x - st.y) : 0.0f;
       }
-      ds[e] = kept ? pe * (gp - st.y) : 0.0f;
+      G.accumulate(dva, p, qb, l16, g);
+      Q.accumulate(dka, ds, qb, l16, g);
     }
-    accumulate_tile<D>(G, dva, p, lane);
-    accumulate_tile<D>(Q, dka, ds, lane);
   }
   if (!valid) return;
-  store_column<T, D>(dk + kj * D, dka, a.scale, hf);
-  store_column<T, D>(dv + kj * D, dva, a.kept_scale, hf);
+  if (splits > 1) {
+    float *at = parts + 2 * static_cast<size_t>(part) * a.rows * D + kj * D;
+    store_row<D>(at, dka, 1.0f, g);
+    store_row<D>(at + a.rows * D, dva, 1.0f, g);
+  } else {
+    store_row<D>(dk + kj * D, dka, a.scale, g);
+    store_row<D>(dv + kj * D, dva, a.kept_scale, g);
+  }
 }
 
 // What the kernels read besides the call's arrays, made by one launch: small calls
@@ -483,6 +452,30 @@ __global__ __launch_bounds__(256) void train_prepare_kernel(Prepare p) {
   prepare_stats<T, D>(p, static_cast<size_t>(b - p.word_blocks));
 }
 
+// The parts' sums in part order, scaled and rounded once.
+template <typename T>
+__global__ __launch_bounds__(256) void join_parts_kernel(size_t count, int splits, float scale_k, float scale_v,
+                                                         const float *__restrict__ parts, T *dk, T *dv) {
+  const size_t i = 4 * (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x);
+  if (i >= count) return;
+  const int v = blockIdx.y;
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int p = 0; p < splits; ++p) {
+    const float4 x = *reinterpret_cast<const float4 *>(parts + (2 * static_cast<size_t>(p) + v) * count + i);
+    s.x += x.x;
+    s.y += x.y;
+    s.z += x.z;
+    s.w += x.w;
+  }
+  const float f = v ? scale_v : scale_k;
+  T *at = (v ? dv : dk) + i;
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16(s.x * f, s.y * f), pack_bf16(s.z * f, s.w * f));
+  else
+    *reinterpret_cast<float4 *>(at) = make_float4(s.x * f, s.y * f, s.z * f, s.w * f);
+}
+
 template <typename K, typename... A>
 hipError_t launch(K kernel, dim3 grid, int threads, hipStream_t s, A... args) {
   hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, args...);
@@ -494,6 +487,12 @@ hipError_t launch(K kernel, dim3 grid, int threads, hipStream_t s, A... args) {
     const hipError_t e_ = (x);           \
     if (e_ != hipSuccess) return e_;     \
   } while (0)
+
+template <typename T>
+hipError_t join_parts(size_t count, int splits, float scale_k, float scale_v, const float *parts, T *dk, T *dv, hipStream_t s) {
+  return launch(join_parts_kernel<T>, dim3(static_cast<unsigned>((count / 4 + 255) / 256), 2), 256, s, count, splits, scale_k,
+                scale_v, parts, dk, dv);
+}
 
 // grad: masks and statistics too.
 template <typename T, int D>
@@ -542,8 +541,8 @@ hipError_t forward(TrainArgs a, const TrainCall &c, hipStream_t s) {
     a.items = c.items;
     a.items_per_head = train_items_per_head(a.n, a.c_q, kRows);
     const dim3 grid(static_cast<unsigned>(c.heads) * a.items_per_head);
-    return a.drop ? launch(train_queries_kernel<T, D, false, true>, grid, kThreads, s, a, static_cast<T *>(c.o))
-                  : launch(train_queries_kernel<T, D, false, false>, grid, kThreads, s, a, static_cast<T *>(c.o));
+    return a.drop ? launch(train_queries_kernel<D, false, true>, grid, kThreads, s, a, static_cast<T *>(c.o))
+                  : launch(train_queries_kernel<D, false, false>, grid, kThreads, s, a, static_cast<T *>(c.o));
   }
 }
 
@@ -555,22 +554,45 @@ hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
     TRAIN_TRY(train_queries(D, true, a, c.heads, c.slots, dq, s));
     a.items = c.tiles;
     a.items_per_head = train_items_per_head(a.n, a.c_q, kTrainKeyTile);
-    return train_keys(D, a, c.heads, train_key_splits(c.heads, a.n, a.c_q), c.parts, dk, dv, s);
+    const int splits = train_key_splits(c.heads, a.n, kTrainKeyBlock, a.items_per_head);
+    TRAIN_TRY(train_keys(D, a, c.heads, splits, c.parts, dk, dv, s));
+    return splits > 1 ? join_parts(a.rows * D, splits, a.scale, a.kept_scale, c.parts, dk, dv, s) : hipSuccess;
   } else {
     a.items = c.items;
     a.items_per_head = train_items_per_head(a.n, a.c_q, kRows);
     const dim3 qgrid(static_cast<unsigned>(c.heads) * a.items_per_head);
-    TRAIN_TRY(a.drop ? launch(train_queries_kernel<T, D, true, true>, qgrid, kThreads, s, a, dq)
-                     : launch(train_queries_kernel<T, D, true, false>, qgrid, kThreads, s, a, dq));
+    TRAIN_TRY(a.drop ? launch(train_queries_kernel<D, true, true>, qgrid, kThreads, s, a, dq)
+                     : launch(train_queries_kernel<D, true, false>, qgrid, kThreads, s, a, dq));
     a.items = c.tiles;
     a.items_per_head = train_items_per_head(a.n, a.c_q, kTile);
-    const dim3 kgrid(static_cast<unsigned>(c.heads) * ((a.n + kRows - 1) / kRows));
-    return a.drop ? launch(train_keys_kernel<T, D, true>, kgrid, kThreads, s, a, dk, dv)
-                  : launch(train_keys_kernel<T, D, false>, kgrid, kThreads, s, a, dk, dv);
+    const int splits = train_key_splits(c.heads, a.n, kRows, a.items_per_head);
+    const dim3 kgrid(static_cast<unsigned>(c.heads) * splits * ((a.n + kRows - 1) / kRows));
+    TRAIN_TRY(a.drop ? launch(train_keys_kernel<D, true>, kgrid, kThreads, s, a, splits, dk, dv, c.parts)
+                     : launch(train_keys_kernel<D, false>, kgrid, kThreads, s, a, splits, dk, dv, c.parts));
+    return splits > 1 ? join_parts(a.rows * D, splits, a.scale, a.kept_scale, c.parts, dk, dv, s) : hipSuccess;
   }
 }
 
 }  // namespace
+
+// Parts of the query tiles, each with fp32 sums of its own that a second kernel adds.
+// The chip holds one block per CU: as many parts, up to 16 of two tiles or more, as
+// make the launch's rounds shortest, a part costing about 2% of a round more (its
+// start, its sums).  3 heads x 2185 tokens (27 key blocks): TODO.
+int train_key_splits(int heads, int n, int keys, int tiles) {
+  constexpr int kMost = 16, kCus = 256;
+  const long long blocks = static_cast<long long>(heads) * ((n + keys - 1) / keys);
+  int best = 1;
+  double least = 0.0;
+  for (int s = 1; s <= kMost && (s == 1 || 2 * s <= tiles); ++s) {
+    const double rounds = static_cast<double>((blocks * s + kCus - 1) / kCus) * (1.0 / s + 0.02);
+    if (s == 1 || rounds < least) {
+      least = rounds;
+      best = s;
+    }
+  }
+  return best;
+}
 
 int train_items_per_head(int n, int c_q, int rows) { return (n + rows - 1) / rows + c_q; }
 
@@ -590,7 +612,8 @@ size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, 
   char *words = take(H * n * 4 * sizeof(uint32_t));
   char *stats = take(H * (n + 1) * 2 * sizeof(float));
   char *masks = take(H * ((n + kTrainKeyBlock - 1) / kTrainKeyBlock) * c_q * (kTrainKeyBlock / 8));
-  const int splits = bf16 ? train_key_splits(heads, n, c_q) : 1;
+  const int splits = train_key_splits(heads, n, bf16 ? kTrainKeyBlock : kRows,
+                                      train_items_per_head(n, c_q, bf16 ? kTrainKeyTile : kTile));
   char *parts = take(splits > 1 ? H * n * d * splits * 2 * sizeof(float) : 0);
   if (a) {
     a->words = reinterpret_cast<uint32_t *>(words);

@@ -291,7 +291,8 @@ struct TrainCall {
 };
 constexpr int kTrainKeyBlock = 256;  // keys of a block and of a mask row
 constexpr int kTrainKeyTile = 64;    // queries of a tile (attention_keys.hip)
-int train_key_splits(int heads, int n, int c_q);
+// Parts that the query tiles are cut into for dK and dV, `keys` keys per block.
+int train_key_splits(int heads, int n, int keys, int tiles);
 // The forward into `o` (grad false), or dQ from a.stats (grad true).
 hipError_t train_queries(int d, bool grad, const TrainArgs &a, int heads, const AttnScratch &w,
                          uint16_t *out, hipStream_t s);
