@@ -376,8 +376,9 @@ int32_t scope_training_workspace_size(const scope_shape *shape, int32_t c_q,
  * fp32.  A cluster without keys gives O = 0 and lse = -inf.  Rows of queries in
  * no cluster are left as they were, in O and lse [heads][n].
  * S_c must be strictly ascending (as call 4 writes it): a key counts once.
- * Requirements and errors as call 5, and SCOPE_ERR_UNSUPPORTED for c_q > 1024;
- * the outputs must not overlap the inputs or each other.                    */
+ * Requirements and errors as call 5, and SCOPE_ERR_UNSUPPORTED for c_q > 1024 or
+ * fp32 rows with n * d * 4 >= 2^32; the outputs must not overlap the inputs or
+ * each other (SCOPE_ERR_INVALID_ARGUMENT).                                  */
 int32_t scope_sparse_attention_train(const scope_shape *shape, const void *q,
                                      const void *k, const void *v, int32_t c_q,
                                      const int32_t *offsets,

@@ -888,6 +888,14 @@ int32_t check_dropout(float p, const uint64_t *rng, uint32_t *drop) {
   return SCOPE_OK;
 }
 
+// check_attention, and what the training kernels ask for besides: their fp32 rows
+// too are addressed with 32-bit byte offsets.
+int32_t check_train(const scope_shape *s, int32_t c_q) {
+  if (c_q > scope::kTrainMaxClusters) return SCOPE_ERR_UNSUPPORTED;
+  if (static_cast<uint64_t>(s->n) * s->d * (s->dtype == SCOPE_BF16 ? 2 : 4) >= (1ull << 32)) return SCOPE_ERR_UNSUPPORTED;
+  return SCOPE_OK;
+}
+
 size_t train_ws(const scope_shape *s, int c_q) {
   return scope::train_workspace(s->heads, s->n, s->d, s->dtype == SCOPE_BF16, c_q, nullptr, nullptr, nullptr);
 }
@@ -987,6 +995,7 @@ int32_t scope_training_workspace_size(const scope_shape *shape, int32_t c_q, siz
   if (st) return st;
   if ((st = check_cq(shape, c_q))) return st;
   if (shape->d != 64 && shape->d != 128) return SCOPE_ERR_UNSUPPORTED;
+  if ((st = check_train(shape, c_q))) return st;
   if (!bytes) return SCOPE_ERR_INVALID_ARGUMENT;
   *bytes = train_ws(shape, c_q);
   return SCOPE_OK;
@@ -1000,7 +1009,7 @@ int32_t scope_sparse_attention_train(const scope_shape *shape, const void *q, co
                                      size_t ws_bytes, void *stream) {
   int32_t st = check_attention(shape, q, k, v, c_q, offsets, perm, sel_counts, sel_idx, scale, o);
   if (st) return st;
-  if (c_q > scope::kTrainMaxClusters) return SCOPE_ERR_UNSUPPORTED;
+  if ((st = check_train(shape, c_q))) return st;
   if (!lse || reinterpret_cast<uintptr_t>(lse) % 4) return SCOPE_ERR_INVALID_ARGUMENT;
   if (outputs_overlap(shape, 1, {o, q, k, v})) return SCOPE_ERR_INVALID_ARGUMENT;
   uint32_t drop = 0;
@@ -1026,7 +1035,7 @@ int32_t scope_sparse_attention_backward(
     int32_t *dev_status, void *stream) {
   int32_t st = check_attention(shape, q, k, v, c_q, offsets, perm, sel_counts, sel_idx, scale, o);
   if (st) return st;
-  if (c_q > scope::kTrainMaxClusters) return SCOPE_ERR_UNSUPPORTED;
+  if ((st = check_train(shape, c_q))) return st;
   if (!lse || reinterpret_cast<uintptr_t>(lse) % 4) return SCOPE_ERR_INVALID_ARGUMENT;
   for (const void *p : {d_o, static_cast<const void *>(dq), static_cast<const void *>(dk),
                         static_cast<const void *>(dv)})

@@ -93,6 +93,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
   // which give it no weight.
   struct Idx {
     int row[NG], own;   // gathered rows, and row `lane` for the statistics
+    int rows;
     uint32_t m;         // the wave's key bits of the tile's cluster
   };
   auto entry_of = [&](int i) {
@@ -110,6 +111,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
     }
     const int j = __builtin_amdgcn_raw_buffer_load_b32(rp, (e.x + min(lane, rows - 1)) * 4, 0, 0);
     ix.own = lane < rows ? j : a.n;
+    ix.rows = rows;
     ix.m = masks[c * kWaves + w];
   };
   auto gather = [&](uint16_t *q, uint16_t *g, const Idx &ix) {
@@ -123,7 +125,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
     if (w < (DROP ? 4 : 2)) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, q + kStats + 2 * kTQ * w, 4, ix.own * 4, 0, 0, 0);
   };
 
-  auto compute = [&](const uint16_t *qt, const uint16_t *gt, uint32_t m) {
+  auto compute = [&](const uint16_t *qt, const uint16_t *gt, int rows, uint32_t m) {
     const float *st = reinterpret_cast<const float *>(qt + kStats);
     // a key that the cluster does not keep has no weight, whatever its K and V
     // rows hold: the bits of its operands are cleared
@@ -138,6 +140,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
     // would be a register for each place and buffer instead of an offset).
 #pragma unroll
     for (int qb = 0; qb < kTQ / 32; ++qb) {
+      if (32 * qb >= rows) break;
       const uint16_t *qr = qt + 32 * qb * D, *gr = gt + 32 * qb * D;
       f32x16 s, dp;
       asm volatile("" : "+v"(at.row_at));
@@ -254,18 +257,21 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
     // computed; every wave's gathers land before the barrier
     Idx now{}, ahead{};
     uint32_t m = 0;
+    int rows = 0;
     load_idx(0, count, now);
     load_idx(1, count, ahead);
     if (count > 0) gather(Q0, G0, now);
     m = now.m;
+    rows = now.rows;
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
     __syncthreads();
     auto step = [&](int i, uint16_t *qc, uint16_t *gc, uint16_t *qn, uint16_t *gn) {
       now = ahead;
       if (i + 1 < count) gather(qn, gn, now);
       load_idx(i + 2, count, ahead);
-      if (m) compute(qc, gc, m);
+      if (m) compute(qc, gc, rows, m);
       m = now.m;
+      rows = now.rows;
       __builtin_amdgcn_s_waitcnt(0x0F70);
       __syncthreads();
     };

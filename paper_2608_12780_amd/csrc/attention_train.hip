@@ -34,41 +34,67 @@ constexpr int kRows = 16 * kThreads / 64;   // rows (queries or keys) per block
 constexpr int kTile = 32;                   // gathered rows per step
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// Tile of kTile rows in LDS.  16 bytes of padding keep 16 rows' 16-byte reads, and
-// rows four apart, on distinct banks.
+// Tiles of kTile gathered rows in LDS, written there by the buffer unit while the
+// tile before is computed; 16-byte slots are XOR-swizzled by the row, so that 16
+// rows' reads of a slot, and one row's of 16 slots, take distinct banks.
 template <int D>
-struct Tile {
-  static constexpr int kStride = D + 4;
-  float x[kTile * kStride];
-
-  // rows 16 b .. of the tile . columns^T: element r of a lane is row 4 g + r
-  __device__ __forceinline__ f32x4 scores(const float4 (&f)[D / 16], int b, int l16, int g) const {
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+struct TileF32 {
+  static constexpr int kFloats = kTile * D;
+  static constexpr int CH = D / 4;          // 16-byte chunks per row
+  static constexpr int RPL = 64 / CH;       // rows per gather load
+  static constexpr int NG = kTile / (kThreads / 64) / RPL;  // gather loads per wave and tile
+  int row_at, col_at;  // bytes: of row l16, chunk g; of row 4 g, chunk l16
+  __device__ __forceinline__ TileF32(int l16, int g)
+      : row_at(4 * D * l16 + 16 * (g ^ l16)), col_at(16 * D * g + 16 * (l16 ^ (4 * g))) {}
+  static __device__ __forceinline__ float4 at(const float *tile, int bytes) {
+    return *reinterpret_cast<const float4 *>(reinterpret_cast<const char *>(tile) + bytes);
+  }
+  // 16 rows of a tile . columns^T, of two tiles (or halves of one) at a time: one
+  // accumulator alone would wait for itself.  Element r of a lane is row 4 g + r.
+  __device__ __forceinline__ void scores(const float *t0, const float4 (&f0)[D / 16], f32x4 &s0, const float *t1,
+                                         const float4 (&f1)[D / 16], f32x4 &s1) const {
+    s0 = s1 = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
-      const float4 t = *reinterpret_cast<const float4 *>(&x[(16 * b + l16) * kStride + 16 * s + 4 * g]);
-      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(t.x, f[s].x, acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(t.y, f[s].y, acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(t.z, f[s].z, acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(t.w, f[s].w, acc, 0, 0, 0);
+      const float4 x = at(t0, row_at ^ (s << 6)), y = at(t1, row_at ^ (s << 6));
+      s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(x.x, f0[s].x, s0, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(y.x, f1[s].x, s1, 0, 0, 0);
+      s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(x.y, f0[s].y, s0, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(y.y, f1[s].y, s1, 0, 0, 0);
+      s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(x.z, f0[s].z, s0, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(y.z, f1[s].z, s1, 0, 0, 0);
+      s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(x.w, f0[s].w, s0, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(y.w, f1[s].w, s1, 0, 0, 0);
     }
-    return acc;
   }
   // out += (rows 16 b .. of the tile)^T . w, w in the layout of scores(); row m of
   // out[cb] is channel 64 (cb / 4) + 4 m + cb % 4, so that a lane reads 16 bytes
-  __device__ __forceinline__ void accumulate(f32x4 (&out)[D / 16], const float (&w)[4], int b, int l16, int g) const {
+  __device__ __forceinline__ void accumulate(const float *tile, f32x4 (&out)[D / 16], const float (&w)[4], int b) const {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
-        const float4 t = *reinterpret_cast<const float4 *>(&x[(16 * b + 4 * g + r) * kStride + 64 * c + 4 * l16]);
+        const float4 t = at(tile + (16 * b + r) * D + 64 * c, col_at ^ (r << 4));
         out[4 * c] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.x, w[r], out[4 * c], 0, 0, 0);
         out[4 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.y, w[r], out[4 * c + 1], 0, 0, 0);
         out[4 * c + 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.z, w[r], out[4 * c + 2], 0, 0, 0);
         out[4 * c + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.w, w[r], out[4 * c + 3], 0, 0, 0);
       }
   }
+  // this wave's rows of a tile, of the indices in `row`
+  static __device__ __forceinline__ void gather(const __amdgpu_buffer_rsrc_t &from, float *tile, const int (&row)[NG],
+                                                int w, int lane) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const int r0 = (RPL * NG) * w + RPL * i, r = r0 + lane / CH;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16, row[i] * (4 * D) + 16 * ((lane % CH) ^ (r & 15)), 0, 0, 0);
+    }
+  }
 };
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const void *p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), static_cast<short>(0), static_cast<int>(bytes), 0x00020000);
+}
 
 // This lane's fragments of a row (zeros where there is none), and its share of the
 // results times `f` into the row of its column.
@@ -88,25 +114,24 @@ __device__ __forceinline__ void store_row(float *row, const f32x4 (&acc)[D / 16]
           make_float4(acc[4 * c][r] * f, acc[4 * c + 1][r] * f, acc[4 * c + 2][r] * f, acc[4 * c + 3][r] * f);
 }
 
-__device__ __forceinline__ float4 row_chunk(const float *base, size_t row, int d, int chunk, bool valid) {
-  return valid ? *reinterpret_cast<const float4 *>(base + row * d + 4 * chunk) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-}
-
 // One wave per 16 queries of a cluster, over the cluster's keys: the forward
 // (GRAD false) or dq (GRAD true).
 template <int D, bool GRAD, bool DROP>
 __global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 3))) void train_queries_kernel(TrainArgs a, float *out) {
-  constexpr int CH = D / 4, PER = kTile * CH / kThreads;  // 16-byte chunks of a row; per thread and tile
-  __shared__ __attribute__((aligned(16))) Tile<D> K, V;
-  __shared__ uint2 words[kTile];
+__attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void train_queries_kernel(TrainArgs a, float *out) {
+  typedef TileF32<D> T;
+  // K tiles are followed by the keys' two dropout words (in the same array for the
+  // reason given in attention_keys.hip)
+  constexpr int kK = T::kFloats + (DROP ? 2 * 64 : 0);
+  __shared__ __attribute__((aligned(16))) float K0[kK], K1[kK], V0[T::kFloats], V1[T::kFloats];
   const int4 it = a.items[blockIdx.x];
   const int h = static_cast<int>(blockIdx.x) / a.items_per_head;
   const int c = it.x, row0 = it.y, rows = it.z, r = it.w;
   if (rows <= 0) return;
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6, l16 = lane & 15, g = lane >> 4;
+  const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const size_t first = static_cast<size_t>(h) * a.n;
-  const float *k = static_cast<const float *>(a.k) + first * D, *v = static_cast<const float *>(a.v) + first * D;
+  const T at(l16, g);
   const int ql = 16 * w + l16;
   const bool valid = ql < rows, active = 16 * w < rows;
   int qi = 0;
@@ -126,40 +151,51 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 3))) void train_queries_kernel(
     }
   }
   uint2 mine = make_uint2(0, 0);
-  const uint32_t *wq = a.words + 4 * first, *wk = wq + 2 * static_cast<size_t>(a.n);
-  if (DROP && valid) mine = make_uint2(wq[qi], wq[qi + a.n]);
+  if (DROP && valid) {
+    const uint32_t *wq = a.words + 4 * first + qi;
+    mine = make_uint2(wq[0], wq[a.n]);
+  }
   f32x4 acc[D / 16];
 #pragma unroll
   for (int cb = 0; cb < D / 16; ++cb) acc[cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m = -INFINITY, l = 0.0f;
-  const int32_t *sel = a.sel_idx + (static_cast<size_t>(h) * a.c_q + c) * a.n;
-  for (int k0 = 0; k0 < r; k0 += kTile) {
-    __syncthreads();
+
+  const uint32_t bytes = static_cast<uint32_t>(a.n) * (4 * D);
+  const __amdgpu_buffer_rsrc_t rk = resource(static_cast<const float *>(a.k) + first * D, bytes);
+  const __amdgpu_buffer_rsrc_t rv = resource(static_cast<const float *>(a.v) + first * D, bytes);
+  const __amdgpu_buffer_rsrc_t rs = resource(a.sel_idx + (static_cast<size_t>(h) * a.c_q + c) * a.n, r * 4);
+  const __amdgpu_buffer_rsrc_t rw = resource(a.words + 4 * first + (2 + (w & 1)) * static_cast<size_t>(a.n), DROP ? a.n * 4 : 0);
+  // rows past the end of the list repeat its last key, with no weight
+  struct Idx {
+    int row[T::NG], own;
+  };
+  auto load_idx = [&](int k0, Idx &ix) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int at = i * kThreads + t, row = at / CH, chunk = at % CH;
-      const bool in = k0 + row < r;
-      const int j = in ? min(max(sel[k0 + row], 0), a.n - 1) : 0;
-      *reinterpret_cast<float4 *>(&K.x[row * K.kStride + 4 * chunk]) = row_chunk(k, j, D, chunk, in);
-      *reinterpret_cast<float4 *>(&V.x[row * K.kStride + 4 * chunk]) = row_chunk(v, j, D, chunk, in);
-      if (DROP && chunk == 0) words[row] = make_uint2(wk[j], wk[j + a.n]);
-    }
-    __syncthreads();
-    if (!active) continue;
+    for (int i = 0; i < T::NG; ++i)
+      ix.row[i] = __builtin_amdgcn_raw_buffer_load_b32(rs, min(k0 + T::RPL * (T::NG * w + i) + lane / T::CH, r - 1) * 4, 0, 0);
+    ix.own = DROP && w < 2 ? __builtin_amdgcn_raw_buffer_load_b32(rs, min(k0 + lane, r - 1) * 4, 0, 0) : 0;
+  };
+  auto gather = [&](float *k, float *v, const Idx &ix) {
+    T::gather(rk, k, ix.row, w, lane);
+    T::gather(rv, v, ix.row, w, lane);
+    if (DROP && w < 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, k + T::kFloats + 64 * w, 4, ix.own * 4, 0, 0, 0);
+  };
+  auto compute = [&](int k0, const float *kt, const float *vt) {
+    const uint32_t *words = reinterpret_cast<const uint32_t *>(kt + T::kFloats) + 4 * g;
+    auto kept = [&](int b, int e) {
+      return pair_kept(mine, make_uint2(words[16 * b + e], words[64 + 16 * b + e]), a.drop);
+    };
     f32x4 s[2];
     float p[2][4];
+    at.scores(kt, qf, s[0], kt + 16 * D, qf, s[1]);
 #pragma unroll
-    for (int b = 0; b < 2; ++b) s[b] = K.scores(qf, b, l16, g);
-    auto in_list = [&](int b, int e) { return k0 + 16 * b + 4 * g + e < r; };
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (k0 + 16 * b + 4 * g + e >= r) s[b][e] = -INFINITY;
+    }
     if constexpr (!GRAD) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[b][e] = in_list(b, e) ? s[b][e] : -INFINITY;
-          top = fmaxf(top, p[b][e]);
-        }
+      float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       const float m_new = fmaxf(m, top * a.scale_log2);
@@ -173,27 +209,48 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 3))) void train_queries_kernel(
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[b][e] = __builtin_amdgcn_exp2f(fmaf(p[b][e], a.scale_log2, neg));
+          p[b][e] = __builtin_amdgcn_exp2f(fmaf(s[b][e], a.scale_log2, neg));
           l += p[b][e];
-          if (DROP && !pair_kept(mine, words[16 * b + 4 * g + e], a.drop)) p[b][e] = 0.0f;
+          if (DROP && !kept(b, e)) p[b][e] = 0.0f;
         }
 #pragma unroll
-      for (int b = 0; b < 2; ++b) V.accumulate(acc, p[b], b, l16, g);
+      for (int b = 0; b < 2; ++b) at.accumulate(vt, acc, p[b], b);
     } else {
+      f32x4 dp[2];
+      at.scores(vt, gf, dp[0], vt + 16 * D, gf, dp[1]);
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const f32x4 dp = V.scores(gf, b, l16, g);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float x = dp[e];
-          if (DROP) x = pair_kept(mine, words[16 * b + 4 * g + e], a.drop) ? x * a.kept_scale : 0.0f;
-          const float pe = __builtin_amdgcn_exp2f(fmaf(s[b][e], a.scale_log2, neg_lse));
-          p[b][e] = in_list(b, e) ? pe * (x - delta) : 0.0f;
+          const float x = DROP ? (kept(b, e) ? dp[b][e] * a.kept_scale : 0.0f) : dp[b][e];
+          p[b][e] = __builtin_amdgcn_exp2f(fmaf(s[b][e], a.scale_log2, neg_lse)) * (x - delta);
         }
       }
 #pragma unroll
-      for (int b = 0; b < 2; ++b) K.accumulate(acc, p[b], b, l16, g);
+      for (int b = 0; b < 2; ++b) at.accumulate(kt, acc, p[b], b);
     }
+  };
+  // one step: indices of the tile after next requested, the next tile gathered, this
+  // one computed; every wave's gathers land before the barrier
+  Idx now, ahead;
+  auto step = [&](int k0, const float *kc, const float *vc, float *kn, float *vn) {
+    if (k0 + kTile < r) gather(kn, vn, now);
+    load_idx(k0 + 2 * kTile, ahead);
+    if (active) compute(k0, kc, vc);
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+    __syncthreads();
+    now = ahead;
+  };
+  if (r > 0) {
+    load_idx(0, ahead);
+    load_idx(kTile, now);
+    gather(K0, V0, ahead);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);
+  __syncthreads();
+  for (int k0 = 0; k0 < r; k0 += 2 * kTile) {
+    step(k0, K0, V0, K1, V1);
+    if (k0 + kTile < r) step(k0 + kTile, K1, V1, K0, V0);
   }
   float f = a.scale;
   if constexpr (!GRAD) {
@@ -210,17 +267,20 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 3))) void train_queries_kernel(
 template <int D, bool DROP>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void train_keys_kernel(TrainArgs a, int splits, float *dk, float *dv, float *parts) {
-  constexpr int CH = D / 4, PER = kTile * CH / kThreads;
-  __shared__ __attribute__((aligned(16))) Tile<D> Q, G;
-  __shared__ float2 stats[kTile];
-  __shared__ uint2 words[kTile];
+  typedef TileF32<D> T;
+  constexpr int kList = 1024;  // active tiles listed at a time
+  constexpr int kQ = T::kFloats + 4 * 64;
+  // Q tiles are followed by their rows' statistics and dropout words
+  __shared__ __attribute__((aligned(16))) float Q0[kQ], Q1[kQ], G0[T::kFloats], G1[T::kFloats];
+  __shared__ int2 list[kList];
+  __shared__ int found[kThreads / 64];
   const int blocks = (a.n + kRows - 1) / kRows;
   const int b = static_cast<int>(blockIdx.x) % blocks, part = static_cast<int>(blockIdx.x) / blocks % splits;
   const int h = static_cast<int>(blockIdx.x) / blocks / splits;
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const size_t first = static_cast<size_t>(h) * a.n;
-  const float *q = static_cast<const float *>(a.q), *d_o = static_cast<const float *>(a.d_o);
+  const T at(l16, g);
   const int j = b * kRows + 16 * w + l16;
   const bool valid = j < a.n;
   const size_t kj = first + (valid ? j : 0);
@@ -228,68 +288,134 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void train_keys_kernel(Tra
   load_row<D>(kf, static_cast<const float *>(a.k) + kj * D, valid, g);
   load_row<D>(vf, static_cast<const float *>(a.v) + kj * D, valid, g);
   uint2 mine = make_uint2(0, 0);
-  const uint32_t *wq = a.words + 4 * first, *wk = wq + 2 * static_cast<size_t>(a.n);
-  if (DROP) mine = make_uint2(wk[kj - first], wk[kj - first + a.n]);
+  if (DROP) {
+    const uint32_t *wk = a.words + 4 * first + 2 * static_cast<size_t>(a.n) + (kj - first);
+    mine = make_uint2(wk[0], wk[a.n]);
+  }
   f32x4 dka[D / 16], dva[D / 16];
 #pragma unroll
   for (int cb = 0; cb < D / 16; ++cb) dka[cb] = dva[cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   // the block's two words of each cluster, 16 bits a wave
   constexpr int WORDS = kTrainKeyBlock / 32, SHARE = kTrainKeyBlock / kRows;
+  static_assert(kRows == 64, "two words per block");
   const uint32_t *masks = a.masks + (static_cast<size_t>(h) * ((a.n + kTrainKeyBlock - 1) / kTrainKeyBlock) + b / SHARE) * a.c_q * WORDS +
-                          kRows / 32 * (b % SHARE);
-  const int per = (a.items_per_head + splits - 1) / splits, end = min((part + 1) * per, a.items_per_head);
-  for (int i = part * per; i < end; ++i) {
-    const int4 it = a.items[static_cast<size_t>(h) * a.items_per_head + i];
-    const int c = it.x, row0 = it.y, rows = it.z;
-    if (rows <= 0) break;
-    const uint32_t m0 = masks[c * WORDS], m1 = masks[c * WORDS + 1];
-    if (!(m0 | m1)) continue;
-    const uint32_t own = (w & 2 ? m1 : m0) >> (16 * (w & 1)) & 0xFFFFu;
-    const bool kept = (own >> l16) & 1u;
-    const int base = a.offsets[static_cast<size_t>(h) * (a.c_q + 1) + c] + row0;
-    __syncthreads();
+                          2 * (b % SHARE);
+
+  const uint32_t bytes = static_cast<uint32_t>(a.n) * (4 * D);
+  const __amdgpu_buffer_rsrc_t rq = resource(static_cast<const float *>(a.q) + first * D, bytes);
+  const __amdgpu_buffer_rsrc_t rg = resource(static_cast<const float *>(a.d_o) + first * D, bytes);
+  const __amdgpu_buffer_rsrc_t rp = resource(a.perm + first, a.n * 4);
+  // plane w of the rows' values: statistics, then words
+  const __amdgpu_buffer_rsrc_t rs = w < 2 ? resource(a.stats + (2 * static_cast<size_t>(h) + w) * (a.n + 1), (a.n + 1) * 4)
+                                          : resource(a.words + (4 * static_cast<size_t>(h) + (w & 1)) * a.n, DROP ? a.n * 4 : 0);
+  // rows past a tile's end repeat its last one, with the statistics of row n
+  struct Idx {
+    int row[T::NG], own, rows;
+    uint32_t m;  // the wave's key bits of the tile's cluster
+  };
+  auto load_idx = [&](int i, int count, Idx &ix) {
+    if (i >= count) return;
+    const int2 e = list[i];
+    const int base = __builtin_amdgcn_readfirstlane(e.x), rows = __builtin_amdgcn_readfirstlane(e.y) & 255;
+    const int c = __builtin_amdgcn_readfirstlane(e.y) >> 8;
 #pragma unroll
-    for (int x = 0; x < PER; ++x) {
-      const int at = x * kThreads + t, row = at / CH, chunk = at % CH;
-      const bool in = row < rows;
-      const int qi = in ? min(max(a.perm[first + min(max(base + row, 0), a.n - 1)], 0), a.n - 1) : 0;
-      *reinterpret_cast<float4 *>(&Q.x[row * Q.kStride + 4 * chunk]) = row_chunk(q, first + qi, D, chunk, in);
-      *reinterpret_cast<float4 *>(&G.x[row * Q.kStride + 4 * chunk]) = row_chunk(d_o, first + qi, D, chunk, in);
-      if (chunk == 0) {
-        const float *st = a.stats + 2 * h * static_cast<size_t>(a.n + 1) + (in ? qi : a.n);
-        stats[row] = make_float2(st[0], st[a.n + 1]);
-        if (DROP) words[row] = make_uint2(wq[qi], wq[qi + a.n]);
-      }
-    }
-    __syncthreads();
-    if (!own) continue;
+    for (int x = 0; x < T::NG; ++x)
+      ix.row[x] = __builtin_amdgcn_raw_buffer_load_b32(rp, (base + min(T::RPL * (T::NG * w + x) + lane / T::CH, rows - 1)) * 4, 0, 0);
+    const int own = __builtin_amdgcn_raw_buffer_load_b32(rp, (base + min(lane, rows - 1)) * 4, 0, 0);
+    ix.own = lane < rows ? own : a.n;
+    ix.rows = rows;
+    ix.m = masks[c * WORDS + (w >> 1)] >> (16 * (w & 1)) & 0xFFFFu;
+  };
+  auto gather = [&](float *q, float *d_o, const Idx &ix) {
+    T::gather(rq, q, ix.row, w, lane);
+    T::gather(rg, d_o, ix.row, w, lane);
+    if (DROP || w < 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, q + T::kFloats + 64 * w, 4, ix.own * 4, 0, 0, 0);
+  };
+  auto compute = [&](const float *qt, const float *gt, int rows, uint32_t m) {
+    const float *st = qt + T::kFloats + 4 * g;
+    const bool selected = (m >> l16) & 1u;
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
-      const f32x4 s = Q.scores(kf, qb, l16, g), dp = G.scores(vf, qb, l16, g);
+      if (16 * qb >= rows) break;
+      f32x4 s, dp;
+      at.scores(qt + 16 * qb * D, kf, s, gt + 16 * qb * D, vf, dp);
       float p[4], ds[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int row = 16 * qb + 4 * g + e;
-        const float2 st = stats[row];
-        const float pe = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, st.x));
+        const int row = 16 * qb + e;
+        const float pe = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, st[row]));
         float x = dp[e];
-        p[e] = kept ? pe : 0.0f;
+        p[e] = selected ? pe : 0.0f;
         if (DROP) {
-          const bool keep = pair_kept(words[row], mine, a.drop);
-          x = keep ? x * a.kept_scale : 0.0f;
-          if (!keep) p[e] = 0.0f;
+          const bool kept = pair_kept(make_uint2(__float_as_uint(st[128 + row]), __float_as_uint(st[192 + row])), mine, a.drop);
+          x = kept ? x * a.kept_scale : 0.0f;
+          if (!kept) p[e] = 0.0f;
         }
-        ds[e] = kept ? pe * (x - st.y) : 0.0f;
+        ds[e] = selected ? pe * (x - st[64 + row]) : 0.0f;
       }
-      G.accumulate(dva, p, qb, l16, g);
-      Q.accumulate(dka, ds, qb, l16, g);
+      at.accumulate(gt, dva, p, qb);
+      at.accumulate(qt, dka, ds, qb);
+    }
+  };
+
+  const int per = (a.items_per_head + splits - 1) / splits;
+  int next = part * per;
+  const int end = min(next + per, a.items_per_head);
+  const int4 *items = a.items + static_cast<size_t>(h) * a.items_per_head;
+  while (next < end) {
+    // the tiles whose cluster keeps a key of the block
+    int count = 0;
+    while (next < end && count + kThreads <= kList) {
+      int2 e = make_int2(0, 0);
+      bool some = false;
+      if (next + t < end) {
+        const int4 it = items[next + t];
+        if (it.z > 0) {
+          some = (masks[it.x * WORDS] | masks[it.x * WORDS + 1]) != 0;
+          e = make_int2(a.offsets[static_cast<size_t>(h) * (a.c_q + 1) + it.x] + it.y, it.x << 8 | it.z);
+        }
+      }
+      const unsigned long long votes = __ballot(some);
+      if (lane == 0) found[w] = __popcll(votes);
+      __syncthreads();
+      int slot = count + __popcll(votes & ((1ull << lane) - 1ull));
+      for (int i = 0; i < kThreads / 64; ++i) {
+        if (i < w) slot += found[i];
+        count += found[i];
+      }
+      if (some) list[slot] = e;
+      next += kThreads;
+      __syncthreads();
+    }
+    count = __builtin_amdgcn_readfirstlane(count);
+    Idx now{}, ahead{};
+    load_idx(0, count, now);
+    load_idx(1, count, ahead);
+    if (count > 0) gather(Q0, G0, now);
+    uint32_t m = now.m;
+    int rows = now.rows;
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    __syncthreads();
+    auto step = [&](int i, const float *qc, const float *gc, float *qn, float *gn) {
+      now = ahead;
+      if (i + 1 < count) gather(qn, gn, now);
+      load_idx(i + 2, count, ahead);
+      if (m) compute(qc, gc, rows, m);
+      m = now.m;
+      rows = now.rows;
+      __builtin_amdgcn_s_waitcnt(0x0F70);
+      __syncthreads();
+    };
+    for (int i = 0; i < count; i += 2) {
+      step(i, Q0, G0, Q1, G1);
+      if (i + 1 < count) step(i + 1, Q1, G1, Q0, G0);
     }
   }
   if (!valid) return;
   if (splits > 1) {
-    float *at = parts + 2 * static_cast<size_t>(part) * a.rows * D + kj * D;
-    store_row<D>(at, dka, 1.0f, g);
-    store_row<D>(at + a.rows * D, dva, 1.0f, g);
+    float *to = parts + 2 * static_cast<size_t>(part) * a.rows * D + kj * D;
+    store_row<D>(to, dka, 1.0f, g);
+    store_row<D>(to + a.rows * D, dva, 1.0f, g);
   } else {
     store_row<D>(dk + kj * D, dka, a.scale, g);
     store_row<D>(dv + kj * D, dva, a.kept_scale, g);
