@@ -26,13 +26,14 @@ namespace {
 constexpr int kTQ = 64;            // queries per tile
 constexpr int kList = 1024;        // active tiles listed at a time
 
-constexpr int kWaves = kTrainKeyBlock / 32;  // a wave owns 32 keys
-constexpr int kThreads = 64 * kWaves;
+template <int D>
+constexpr int kWavesOf = train_key_block(D) / 32;  // a wave owns 32 keys
 
 template <int D, bool DROP>
-__global__ __launch_bounds__(kThreads)
+__global__ __launch_bounds__(64 * kWavesOf<D>)
 __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int splits, uint16_t *dk,
                                                                            uint16_t *dv, float *parts) {
+  constexpr int kKeys = train_key_block(D), kWaves = kWavesOf<D>;
   constexpr int CH = D / 8;              // 16-byte chunks per row
   constexpr int RPL = 64 / CH;           // rows per gather load
   constexpr int NG = kTQ / kWaves / RPL; // gather loads per wave, tile and matrix
@@ -43,10 +44,10 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
   __shared__ __attribute__((aligned(256))) uint16_t Q0[kStats + 8 * kTQ], Q1[kStats + 8 * kTQ], G0[kTQ * D], G1[kTQ * D];
   // d = 128: the block's V rows (each wave reads its own), for registers' sake
   constexpr bool VLDS = D == 128;
-  __shared__ __attribute__((aligned(16))) uint16_t Vs[VLDS ? kTrainKeyBlock * D : 8];
+  __shared__ __attribute__((aligned(16))) uint16_t Vs[VLDS ? kKeys * D : 8];
   __shared__ int2 list[kList];
   __shared__ int found[kWaves];
-  const int blocks = (a.n + kTrainKeyBlock - 1) / kTrainKeyBlock;
+  const int blocks = (a.n + kKeys - 1) / kKeys;
   const int kb = static_cast<int>(blockIdx.x) % blocks, part = static_cast<int>(blockIdx.x) / blocks % splits;
   const int h = static_cast<int>(blockIdx.x) / blocks / splits;
   const int t = threadIdx.x, lane = t & 63, l32 = lane & 31, hf = lane >> 5;
@@ -55,7 +56,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
 
   TileReader<D> at(lane);
   bf16x8 kf[D / 16], vf[VLDS ? 1 : D / 16];
-  const int own_row = 32 * w + l32, key = kb * kTrainKeyBlock + own_row;
+  const int own_row = 32 * w + l32, key = kb * kKeys + own_row;
   {
     const size_t from = (first + min(key, a.n - 1)) * D;
 #pragma unroll
@@ -87,7 +88,9 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
   const __amdgpu_buffer_rsrc_t rs = rsrc(w < 2 ? static_cast<const void *>(a.stats + (2 * static_cast<size_t>(h) + w) * (a.n + 1))
                                                : static_cast<const void *>(a.words + (4 * static_cast<size_t>(h) + (w & 1)) * a.n),
                                          w < 2 ? (a.n + 1) * 4 : DROP ? a.n * 4 : 0);
-  const uint32_t *masks = a.masks + (static_cast<size_t>(h) * blocks + kb) * a.c_q * (kTrainKeyBlock / 32);
+  constexpr int WORDS = kTrainKeyBlock / 32, SHARE = kTrainKeyBlock / kKeys;
+  const uint32_t *masks = a.masks + (static_cast<size_t>(h) * ((a.n + kTrainKeyBlock - 1) / kTrainKeyBlock) + kb / SHARE) * a.c_q * WORDS +
+                          kWaves * (kb % SHARE);
 
   // Rows past a tile's end repeat its last one, with the statistics of row n,
   // which give it no weight.
@@ -112,7 +115,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
     const int j = __builtin_amdgcn_raw_buffer_load_b32(rp, (e.x + min(lane, rows - 1)) * 4, 0, 0);
     ix.own = lane < rows ? j : a.n;
     ix.rows = rows;
-    ix.m = masks[c * kWaves + w];
+    ix.m = masks[c * WORDS + w];
   };
   auto gather = [&](uint16_t *q, uint16_t *g, const Idx &ix) {
 #pragma unroll
@@ -152,8 +155,8 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
             at.row(qr, x), kf[x], s, 0, 0, 0);
       interleave<D / 16, 1, 0>();
       asm volatile("" : "+v"(s), "+v"(at.row_at));
-      // p, with its sign bit set where dropout drops it
-      float p[16], kept[16];
+      // p, with its sign bit set where dropout drops it, and the kept ones' operands
+      float p[16];
 #pragma unroll
       for (int x = 0; x < D / 16; ++x) {
         const bf16x8 g = at.row(gr, x);
@@ -164,27 +167,39 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
           v = vf[x];
         dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g, v, dp, 0, 0, 0);
       }
+      bf16x8 pk[2];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r0 = 32 * qb + 8 * i + 4 * hf;
         const float4 nl = *reinterpret_cast<const float4 *>(&st[r0]);
         const float nls[4] = {nl.x, nl.y, nl.z, nl.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          kept[4 * i + j] = p[4 * i + j] = __builtin_amdgcn_exp2f(fmaf(s[4 * i + j], a.scale_log2, nls[j]));
-        if constexpr (DROP) {
-          const uint4 wx = *reinterpret_cast<const uint4 *>(&st[2 * kTQ + r0]);
-          const uint4 wy = *reinterpret_cast<const uint4 *>(&st[3 * kTQ + r0]);
-          const uint32_t wxs[4] = {wx.x, wx.y, wx.z, wx.w}, wys[4] = {wy.x, wy.y, wy.z, wy.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const bool k = pair_kept(make_uint2(wxs[j], wys[j]), mine, a.drop);
-            p[4 * i + j] = k ? p[4 * i + j] : -p[4 * i + j];
-            kept[4 * i + j] = k ? kept[4 * i + j] : 0.0f;
-          }
-        }
+        for (int j = 0; j < 4; ++j) p[4 * i + j] = __builtin_amdgcn_exp2f(fmaf(s[4 * i + j], a.scale_log2, nls[j]));
       }
-      bf16x8 pk[2] = {operand(kept), operand(kept + 8)};
+      if constexpr (DROP) {
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) {
+          float kept[8];
+#pragma unroll
+          for (int i = 2 * s2; i < 2 * s2 + 2; ++i) {
+            const int r0 = 32 * qb + 8 * i + 4 * hf;
+            const uint4 wx = *reinterpret_cast<const uint4 *>(&st[2 * kTQ + r0]);
+            const uint4 wy = *reinterpret_cast<const uint4 *>(&st[3 * kTQ + r0]);
+            const uint32_t wxs[4] = {wx.x, wx.y, wx.z, wx.w}, wys[4] = {wy.x, wy.y, wy.z, wy.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int e = 4 * i + j;
+              const bool k = pair_kept(make_uint2(wxs[j], wys[j]), mine, a.drop);
+              kept[4 * (i & 1) + j] = k ? p[e] : 0.0f;
+              p[e] = k ? p[e] : -p[e];
+            }
+          }
+          pk[s2] = operand(kept);
+        }
+      } else {
+        pk[0] = operand(p);
+        pk[1] = operand(p + 8);
+      }
       interleave<D / 16, VLDS ? 2 : 1, D == 128 ? 6 : 12>();
       asm volatile("" : "+v"(dp), "+v"(pk[0]), "+v"(pk[1]), "+v"(at.col_at));
       float ds[16];
@@ -234,9 +249,11 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
       if (next + t < end) {
         const int4 it = items[next + t];
         if (it.z > 0) {
-          const uint4 *m = reinterpret_cast<const uint4 *>(masks + it.x * (kTrainKeyBlock / 32));
-          const uint4 x = m[0], y = m[1];
-          active = ((x.x | x.y) | (x.z | x.w) | (y.x | y.y) | (y.z | y.w)) != 0;
+          const uint4 *m = reinterpret_cast<const uint4 *>(masks + it.x * WORDS);
+          uint32_t any = 0;
+#pragma unroll
+          for (int i = 0; i < kWaves / 4; ++i) any |= (m[i].x | m[i].y) | (m[i].z | m[i].w);
+          active = any != 0;
           e = make_int2(a.offsets[static_cast<size_t>(h) * (a.c_q + 1) + it.x] + it.y, it.x << 8 | it.z);
         }
       }
@@ -303,11 +320,11 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
 
 template <int D>
 hipError_t run(const TrainArgs &a, int heads, int splits, float *parts, uint16_t *dk, uint16_t *dv, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(heads) * splits * ((a.n + kTrainKeyBlock - 1) / kTrainKeyBlock));
+  const dim3 grid(static_cast<unsigned>(heads) * splits * ((a.n + train_key_block(D) - 1) / train_key_block(D)));
   if (a.drop)
-    hipLaunchKernelGGL((grad_keys_kernel<D, true>), grid, dim3(kThreads), 0, s, a, splits, dk, dv, parts);
+    hipLaunchKernelGGL((grad_keys_kernel<D, true>), grid, dim3(64 * kWavesOf<D>), 0, s, a, splits, dk, dv, parts);
   else
-    hipLaunchKernelGGL((grad_keys_kernel<D, false>), grid, dim3(kThreads), 0, s, a, splits, dk, dv, parts);
+    hipLaunchKernelGGL((grad_keys_kernel<D, false>), grid, dim3(64 * kWavesOf<D>), 0, s, a, splits, dk, dv, parts);
   return hipGetLastError();
 }
 

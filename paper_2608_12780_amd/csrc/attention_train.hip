@@ -680,7 +680,7 @@ hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
     TRAIN_TRY(train_queries(D, true, a, c.heads, c.slots, dq, s));
     a.items = c.tiles;
     a.items_per_head = train_items_per_head(a.n, a.c_q, kTrainKeyTile);
-    const int splits = train_key_splits(c.heads, a.n, kTrainKeyBlock, a.items_per_head);
+    const int splits = train_key_splits(c.heads, a.n, train_key_block(D), a.items_per_head);
     TRAIN_TRY(train_keys(D, a, c.heads, splits, c.parts, dk, dv, s));
     return splits > 1 ? join_parts(a.rows * D, splits, a.scale, a.kept_scale, c.parts, dk, dv, s) : hipSuccess;
   } else {
@@ -738,7 +738,7 @@ size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, 
   char *words = take(H * n * 4 * sizeof(uint32_t));
   char *stats = take(H * (n + 1) * 2 * sizeof(float));
   char *masks = take(H * ((n + kTrainKeyBlock - 1) / kTrainKeyBlock) * c_q * (kTrainKeyBlock / 8));
-  const int splits = train_key_splits(heads, n, bf16 ? kTrainKeyBlock : kRows,
+  const int splits = train_key_splits(heads, n, bf16 ? train_key_block(d) : kRows,
                                       train_items_per_head(n, c_q, bf16 ? kTrainKeyTile : kTile));
   char *parts = take(splits > 1 ? H * n * d * splits * 2 * sizeof(float) : 0);
   if (a) {

@@ -289,7 +289,9 @@ struct TrainCall {
   float *parts;            // sums of the query parts (train_key_splits > 1)
   int32_t *status;
 };
-constexpr int kTrainKeyBlock = 256;  // keys of a block and of a mask row
+constexpr int kTrainKeyBlock = 256;  // keys of a mask row
+// keys of a block of dK and dV, bf16
+constexpr int train_key_block(int d) { return d == 128 ? 256 : 128; }
 constexpr int kTrainKeyTile = 64;    // queries of a tile (attention_keys.hip)
 // Parts that the query tiles are cut into for dK and dV, `keys` keys per block.
 int train_key_splits(int heads, int n, int keys, int tiles);
