@@ -31,8 +31,7 @@ constexpr int kWavesOf = train_key_block(D) / 32;  // a wave owns 32 keys
 
 template <int D, bool DROP>
 __global__ __launch_bounds__(64 * kWavesOf<D>)
-__attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int splits, uint16_t *dk,
-                                                                           uint16_t *dv, float *parts) {
+__attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, uint16_t *dk, uint16_t *dv) {
   constexpr int kKeys = train_key_block(D), kWaves = kWavesOf<D>;
   constexpr int CH = D / 8;              // 16-byte chunks per row
   constexpr int RPL = 64 / CH;           // rows per gather load
@@ -47,7 +46,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
   __shared__ __attribute__((aligned(16))) uint16_t Vs[VLDS ? kKeys * D : 8];
   __shared__ int2 list[kList];
   __shared__ int found[kWaves];
-  const int blocks = (a.n + kKeys - 1) / kKeys;
+  const int splits = a.splits, blocks = (a.n + kKeys - 1) / kKeys;
   const int kb = static_cast<int>(blockIdx.x) % blocks, part = static_cast<int>(blockIdx.x) / blocks % splits;
   const int h = static_cast<int>(blockIdx.x) / blocks / splits;
   const int t = threadIdx.x, lane = t & 63, l32 = lane & 31, hf = lane >> 5;
@@ -306,7 +305,7 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
       const size_t at = (first + key) * D + 32 * db + 8 * i + 4 * hf;
       const f32x16 &x = dka[db], &y = dva[db];
       if (splits > 1) {
-        float *p = parts + static_cast<size_t>(part) * 2 * a.rows * D;
+        float *p = a.parts + static_cast<size_t>(part) * 2 * a.rows * D;
         *reinterpret_cast<float4 *>(p + at) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
         *reinterpret_cast<float4 *>(p + a.rows * D + at) = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
       } else {
@@ -319,19 +318,19 @@ __attribute__((amdgpu_waves_per_eu(2))) void grad_keys_kernel(TrainArgs a, int s
 }
 
 template <int D>
-hipError_t run(const TrainArgs &a, int heads, int splits, float *parts, uint16_t *dk, uint16_t *dv, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(heads) * splits * ((a.n + train_key_block(D) - 1) / train_key_block(D)));
+hipError_t run(const TrainArgs &a, int heads, uint16_t *dk, uint16_t *dv, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(heads) * a.splits * ((a.n + train_key_block(D) - 1) / train_key_block(D)));
   if (a.drop)
-    hipLaunchKernelGGL((grad_keys_kernel<D, true>), grid, dim3(64 * kWavesOf<D>), 0, s, a, splits, dk, dv, parts);
+    hipLaunchKernelGGL((grad_keys_kernel<D, true>), grid, dim3(64 * kWavesOf<D>), 0, s, a, dk, dv);
   else
-    hipLaunchKernelGGL((grad_keys_kernel<D, false>), grid, dim3(64 * kWavesOf<D>), 0, s, a, splits, dk, dv, parts);
+    hipLaunchKernelGGL((grad_keys_kernel<D, false>), grid, dim3(64 * kWavesOf<D>), 0, s, a, dk, dv);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t train_keys(int d, const TrainArgs &a, int heads, int splits, float *parts, uint16_t *dk, uint16_t *dv, hipStream_t s) {
-  return d == 128 ? run<128>(a, heads, splits, parts, dk, dv, s) : run<64>(a, heads, splits, parts, dk, dv, s);
+hipError_t train_keys(int d, const TrainArgs &a, int heads, uint16_t *dk, uint16_t *dv, hipStream_t s) {
+  return d == 128 ? run<128>(a, heads, dk, dv, s) : run<64>(a, heads, dk, dv, s);
 }
 
 }  // namespace scope

@@ -36,7 +36,7 @@ struct Tiles {
 };
 
 template <int D, bool GRAD, bool DROP, bool PAIRED>
-__device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const int4 &ia, const int4 &ib, uint16_t *out,
+__device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const int4 &ia, const int4 &ib, int part, uint16_t *out,
                                              typename Tiles<D, DROP>::K &K0, typename Tiles<D, DROP>::K &K1,
                                              typename Tiles<D, DROP>::V &V0, typename Tiles<D, DROP>::V &V1) {
   typedef Tiles<D, DROP> T;
@@ -85,8 +85,13 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
     for (int e = 0; e < 16; ++e) acc[db][e] = 0.0f;
   float m_run = -INFINITY, l_run = 0.0f;
 
-  const int ntA = (ia.w + kBN - 1) / kBN, ntB = PAIRED ? (ib.w + kBN - 1) / kBN : 0;
-  const int ntiles = ntA > ntB ? ntA : ntB, nt_own = (r + kBN - 1) / kBN;
+  // the part's tiles of each chunk's list
+  auto tiles_of = [&](int keys) { return ((keys + kBN - 1) / kBN + a.splits - 1) / a.splits; };
+  auto begin_of = [&](int keys) { return part * tiles_of(keys); };
+  auto count_of = [&](int keys) { return max(min((keys + kBN - 1) / kBN - begin_of(keys), tiles_of(keys)), 0); };
+  const int ntA = count_of(ia.w), ntB = PAIRED ? count_of(ib.w) : 0;
+  const int ntiles = ntA > ntB ? ntA : ntB, nt_own = count_of(r);
+  const int t0A = begin_of(ia.w), t0B = PAIRED ? begin_of(ib.w) : 0, t0_own = begin_of(r);
   auto rsrc = [](const void *p, int bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), static_cast<short>(0), bytes, 0x00020000);
   };
@@ -117,12 +122,12 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
     }
   };
   auto load_idx = [&](int tile, Idx &ix) {
-    load_rows(rselA, ia.w, tile, ix.a);
-    if constexpr (PAIRED) load_rows(rselB, ib.w, tile, ix.b);
+    load_rows(rselA, ia.w, t0A + tile, ix.a);
+    if constexpr (PAIRED) load_rows(rselB, ib.w, t0B + tile, ix.b);
     ix.own = 0;
     if (DROP && w < (PAIRED ? 4 : 2))
-      ix.own = w < 2 ? __builtin_amdgcn_raw_buffer_load_b32(rselA, min(tile * kBN + lane, ia.w - 1) * 4, 0, 0)
-                     : __builtin_amdgcn_raw_buffer_load_b32(rselB, min(tile * kBN + lane, ib.w - 1) * 4, 0, 0);
+      ix.own = w < 2 ? __builtin_amdgcn_raw_buffer_load_b32(rselA, min((t0A + tile) * kBN + lane, ia.w - 1) * 4, 0, 0)
+                     : __builtin_amdgcn_raw_buffer_load_b32(rselB, min((t0B + tile) * kBN + lane, ib.w - 1) * 4, 0, 0);
   };
   auto gather = [&](const __amdgpu_buffer_rsrc_t &rows_of, uint16_t *ta, uint16_t *tb, const Idx &ix) {
 #pragma unroll
@@ -325,9 +330,9 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
     }
     if (mine_too) {
       if constexpr (GRAD)
-        grad_tile(tile, kc[g], vc[g]);
+        grad_tile(t0_own + tile, kc[g], vc[g]);
       else
-        forward_tile(tile, kc[g], vc[g], kn, vn, now);
+        forward_tile(t0_own + tile, kc[g], vc[g], kn, vn, now);
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
     __syncthreads();
@@ -346,6 +351,20 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
     if (tile + 1 < ntiles) step(tile + 1, K1, V1, K0, V0);
   }
 
+  if (a.splits > 1) {  // the part's sums, and the forward's maximum and normaliser
+    float *to = a.parts + (static_cast<size_t>(part) * a.rows + first + qi) * D + 4 * hf;
+    const float l = l_run + __shfl_xor(l_run, 32);
+    if (!valid) return;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4 *>(to + 32 * db + 8 * i) =
+            make_float4(acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]);
+    if (!GRAD && hf == 0)
+      reinterpret_cast<float2 *>(a.parts + a.splits * a.rows * D)[part * a.rows + first + qi] = make_float2(m_run, l);
+    return;
+  }
   float f = a.scale;
   if constexpr (!GRAD) {
     // lanes l and l^32 hold the two halves of one query's row sum
@@ -373,8 +392,12 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void queries_kernel(TrainA
   __shared__ __attribute__((aligned(16))) typename T::K K1;
   __shared__ __attribute__((aligned(16))) typename T::V V0;
   __shared__ __attribute__((aligned(16))) typename T::V V1;
-  int item, half = 0;
-  if (order) {
+  int item, half = 0, part = 0;
+  if (a.splits > 1) {
+    const int b = static_cast<int>(blockIdx.x);
+    item = xcd_item(b % total_items, total_items);
+    part = b / total_items;
+  } else if (order) {
     const int2 e = order[blockIdx.x];  // (slot, 0: all of it, 1 or 2: a half)
     item = e.x;
     half = e.y;
@@ -387,9 +410,9 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void queries_kernel(TrainA
   if (half) take_half(&ia, &ib, half);
   if (ia.z <= 0) return;
   if (ib.z > 0)
-    queries_body<D, GRAD, DROP, true>(a, h, ia, ib, out, K0, K1, V0, V1);
+    queries_body<D, GRAD, DROP, true>(a, h, ia, ib, part, out, K0, K1, V0, V1);
   else
-    queries_body<D, GRAD, DROP, false>(a, h, ia, ib, out, K0, K1, V0, V1);
+    queries_body<D, GRAD, DROP, false>(a, h, ia, ib, part, out, K0, K1, V0, V1);
 }
 
 template <int D, bool GRAD>
@@ -405,15 +428,21 @@ hipError_t run(const TrainArgs &a, int total, int blocks, const AttnScratch &w, 
 
 }  // namespace
 
-hipError_t train_queries(int d, bool grad, const TrainArgs &args, int heads, const AttnScratch &w, uint16_t *out,
-                         hipStream_t s) {
+hipError_t train_queries(int d, bool grad, const TrainArgs &args, int heads, bool listed, const AttnScratch &scratch,
+                         uint16_t *out, hipStream_t s) {
   TrainArgs a = args;
+  AttnScratch w = scratch;
+  if (a.splits > 1) w.order = nullptr;
   a.items_per_head = attn_items_per_head(a.n, a.c_q);
-  hipError_t e = attention_list(heads, a.n, d, a.c_q, a.c_q > 1, a.offsets, a.sel_counts, w, s);
-  if (e != hipSuccess) return e;
-  int blocks = 0;
-  if ((e = attention_plan(heads, a.n, d, a.c_q, w, &blocks, s)) != hipSuccess) return e;
   const int total = heads * a.items_per_head;
+  int blocks = total * a.splits;
+  if (!listed) {
+    hipError_t e = attention_list(heads, a.n, d, a.c_q, a.c_q > 1, a.offsets, a.sel_counts, w, s);
+    if (e != hipSuccess) return e;
+    if (a.splits == 1 && (e = attention_plan(heads, a.n, d, a.c_q, w, &blocks, s)) != hipSuccess) return e;
+  } else {
+    w.order = nullptr;
+  }
   if (d == 128) return grad ? run<128, true>(a, total, blocks, w, out, s) : run<128, false>(a, total, blocks, w, out, s);
   return grad ? run<64, true>(a, total, blocks, w, out, s) : run<64, false>(a, total, blocks, w, out, s);
 }

@@ -13,6 +13,7 @@
 // the same bits on every run.
 #include <math.h>
 
+#include "attention_slots.h"
 #include "common.h"
 #include "kernels.h"
 #include "mfma.h"
@@ -124,8 +125,9 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void train_queries_kernel(
   // reason given in attention_keys.hip)
   constexpr int kK = T::kFloats + (DROP ? 2 * 64 : 0);
   __shared__ __attribute__((aligned(16))) float K0[kK], K1[kK], V0[T::kFloats], V1[T::kFloats];
-  const int4 it = a.items[blockIdx.x];
-  const int h = static_cast<int>(blockIdx.x) / a.items_per_head;
+  const int part = static_cast<int>(blockIdx.x) % a.splits, slot = static_cast<int>(blockIdx.x) / a.splits;
+  const int4 it = a.items[slot];
+  const int h = slot / a.items_per_head;
   const int c = it.x, row0 = it.y, rows = it.z, r = it.w;
   if (rows <= 0) return;
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
@@ -160,6 +162,9 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void train_queries_kernel(
   for (int cb = 0; cb < D / 16; ++cb) acc[cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m = -INFINITY, l = 0.0f;
 
+  // the part's keys, in whole tiles
+  const int per = ((r + kTile - 1) / kTile + a.splits - 1) / a.splits * kTile;
+  const int from = min(part * per, r), end = min(from + per, r);
   const uint32_t bytes = static_cast<uint32_t>(a.n) * (4 * D);
   const __amdgpu_buffer_rsrc_t rk = resource(static_cast<const float *>(a.k) + first * D, bytes);
   const __amdgpu_buffer_rsrc_t rv = resource(static_cast<const float *>(a.v) + first * D, bytes);
@@ -234,23 +239,32 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void train_queries_kernel(
   // one computed; every wave's gathers land before the barrier
   Idx now, ahead;
   auto step = [&](int k0, const float *kc, const float *vc, float *kn, float *vn) {
-    if (k0 + kTile < r) gather(kn, vn, now);
+    if (k0 + kTile < end) gather(kn, vn, now);
     load_idx(k0 + 2 * kTile, ahead);
     if (active) compute(k0, kc, vc);
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
     __syncthreads();
     now = ahead;
   };
-  if (r > 0) {
-    load_idx(0, ahead);
-    load_idx(kTile, now);
+  if (from < end) {
+    load_idx(from, ahead);
+    load_idx(from + kTile, now);
     gather(K0, V0, ahead);
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);
   __syncthreads();
-  for (int k0 = 0; k0 < r; k0 += 2 * kTile) {
+  for (int k0 = from; k0 < end; k0 += 2 * kTile) {
     step(k0, K0, V0, K1, V1);
-    if (k0 + kTile < r) step(k0 + kTile, K1, V1, K0, V0);
+    if (k0 + kTile < end) step(k0 + kTile, K1, V1, K0, V0);
+  }
+  if (a.splits > 1) {
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (!valid) return;
+    const size_t at_row = static_cast<size_t>(part) * a.rows + first + qi;
+    store_row<D>(a.parts + at_row * D, acc, 1.0f, g);
+    if (!GRAD && g == 0) reinterpret_cast<float2 *>(a.parts + a.splits * a.rows * D)[at_row] = make_float2(m, l);
+    return;
   }
   float f = a.scale;
   if constexpr (!GRAD) {
@@ -266,7 +280,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void train_queries_kernel(
 // block's keys: dk and dv, or with several parts their sums over a part's tiles.
 template <int D, bool DROP>
 __global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void train_keys_kernel(TrainArgs a, int splits, float *dk, float *dv, float *parts) {
+__attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void train_keys_kernel(TrainArgs a, float *dk, float *dv) {
   typedef TileF32<D> T;
   constexpr int kList = 1024;  // active tiles listed at a time
   constexpr int kQ = T::kFloats + 4 * 64;
@@ -274,7 +288,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void train_keys_kernel(Tra
   __shared__ __attribute__((aligned(16))) float Q0[kQ], Q1[kQ], G0[T::kFloats], G1[T::kFloats];
   __shared__ int2 list[kList];
   __shared__ int found[kThreads / 64];
-  const int blocks = (a.n + kRows - 1) / kRows;
+  const int splits = a.splits, blocks = (a.n + kRows - 1) / kRows;
   const int b = static_cast<int>(blockIdx.x) % blocks, part = static_cast<int>(blockIdx.x) / blocks % splits;
   const int h = static_cast<int>(blockIdx.x) / blocks / splits;
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
@@ -413,7 +427,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void train_keys_kernel(Tra
   }
   if (!valid) return;
   if (splits > 1) {
-    float *to = parts + 2 * static_cast<size_t>(part) * a.rows * D + kj * D;
+    float *to = a.parts + 2 * static_cast<size_t>(part) * a.rows * D + kj * D;
     store_row<D>(to, dka, 1.0f, g);
     store_row<D>(to + a.rows * D, dva, 1.0f, g);
   } else {
@@ -431,7 +445,7 @@ struct Prepare {
   const int32_t *offsets, *sel_counts, *sel_idx;
   // lists of work items of rows[i] queries
   int4 *items[2];
-  int rows[2], per_head[2];
+  int rows[2], per_head[2], stride[2];  // stride 2: work slots of one chunk
   uint32_t *masks;
   int32_t *status;
   const uint64_t *rng;
@@ -443,7 +457,7 @@ struct Prepare {
 
 // Work items of `rows` queries of head h: the chunks of every cluster in cluster
 // order as (cluster, first row, rows, selected keys), then empty ones.
-__device__ void prepare_items(const Prepare &p, int h, int rows, int per_head, int4 *items) {
+__device__ void prepare_items(const Prepare &p, int h, int rows, int per_head, int stride, int4 *items) {
   constexpr int PER = kTrainMaxClusters / 256;
   __shared__ int first[kTrainMaxClusters + 1];
   __shared__ int wtot[4];
@@ -481,7 +495,9 @@ __device__ void prepare_items(const Prepare &p, int h, int rows, int per_head, i
       it = make_int4(lo, row0, min(rows, count_of(lo) - row0),
                      min(max(p.sel_counts[static_cast<size_t>(h) * p.c_q + lo], 0), p.n));
     }
-    items[static_cast<size_t>(h) * per_head + slot] = it;
+    int4 *to = items + (static_cast<size_t>(h) * per_head + slot) * stride;
+    to[0] = it;
+    if (stride == 2) to[1] = make_int4(0, 0, 0, 0);
   }
 }
 
@@ -497,27 +513,44 @@ __device__ void prepare_masks(const Prepare &p, int h, int c, int from, int segm
   const int32_t *sel = p.sel_idx + (static_cast<size_t>(h) * p.c_q + c) * n;
   const int to = min(from + kMaskKeys, n);
   bits[t] = 0;
-  auto below = [&](int x) {  // entries below x
+  auto below = [&](int x) {  // entries below x, 64 places of the list at a time
     int lo = 0, hi = r;
     while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (sel[mid] < x) lo = mid + 1; else hi = mid;
+      const int step = (hi - lo + 63) / 64, at = lo + step * (t & 63) + step - 1;
+      const int less = __popcll(__ballot(at < hi && sel[min(at, hi - 1)] < x));
+      lo = min(lo + step * less, hi);
+      hi = step == 1 ? lo : min(lo + step - 1, hi);
     }
     return lo;
   };
   const int lo = segments == 1 ? 0 : below(from), hi = segments == 1 ? r : below(to);
   __syncthreads();
-  bool bad = false;
-  auto check = [&](int e, int j) { bad = bad || j < 0 || j >= n || (e > 0 && sel[e - 1] >= j); };
-#pragma unroll 4
-  for (int e = lo + t; e < hi; e += 256) {
-    const int j = sel[e];
-    if (j >= from && j < to) atomicOr(&bits[(j - from) >> 5], 1u << (j & 31));
-    if (segments == 1) check(e, j);
-  }
-  if (segments > 1) {  // entries that no segment's search finds are seen here
-#pragma unroll 4
-    for (int e = from + t; e < min(to, r); e += 256) check(e, sel[e]);
+  // A bound between two segments is found alike for both, so their ranges cover
+  // [below(0), below(n)) whatever the list holds: every entry of a bad list is seen.
+  bool bad = lo > 0 && from == 0;
+  bad = bad || (hi < r && to == n);
+  for (int e0 = lo + 8 * t; e0 < hi; e0 += 8 * 256) {
+    // eight neighbours per thread: most fall into one word, set at once
+    int before = e0 > 0 ? sel[e0 - 1] : -1, word = 0, j[8];
+    uint32_t acc = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) j[i] = sel[min(e0 + i, hi - 1)];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (e0 + i >= hi) break;
+      const bool here = j[i] >= from && j[i] < to;
+      bad = bad || !here || j[i] <= before;
+      before = j[i];
+      if (!here) continue;
+      const int at = (j[i] - from) >> 5;
+      if (at != word) {
+        if (acc) atomicOr(&bits[word], acc);
+        word = at;
+        acc = 0;
+      }
+      acc |= 1u << (j[i] & 31);
+    }
+    if (acc) atomicOr(&bits[word], acc);
   }
   if (bad && p.status) atomicOr(p.status, kStatusBadSet);
   __syncthreads();
@@ -536,9 +569,18 @@ __device__ void prepare_stats(const Prepare &p, size_t block) {
   const size_t i = (block * 256 + threadIdx.x) / LANES, n = p.n;
   const int x = threadIdx.x % LANES;
   if (i >= p.heads * n) return;  // whole groups of LANES
+  const uint4 vo = reinterpret_cast<const uint4 *>(o)[i * LANES + x], vg = reinterpret_cast<const uint4 *>(d_o)[i * LANES + x];
+  const uint32_t a[4] = {vo.x, vo.y, vo.z, vo.w}, b[4] = {vg.x, vg.y, vg.z, vg.w};
   float s = 0.0f;
 #pragma unroll
-  for (int e = 0; e < PER; ++e) s = fmaf(load_elem(o, i * D + PER * x + e), load_elem(d_o, i * D + PER * x + e), s);
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (sizeof(T) == 2) {
+      s = fmaf(__uint_as_float(a[e] << 16), __uint_as_float(b[e] << 16), s);
+      s = fmaf(__uint_as_float(a[e] & 0xFFFF0000u), __uint_as_float(b[e] & 0xFFFF0000u), s);
+    } else {
+      s = fmaf(__uint_as_float(a[e]), __uint_as_float(b[e]), s);
+    }
+  }
 #pragma unroll
   for (int k = LANES / 2; k > 0; k /= 2) s += __shfl_xor(s, k, LANES);
   if (x) return;
@@ -556,7 +598,7 @@ __global__ __launch_bounds__(256) void train_prepare_kernel(Prepare p) {
   int b = static_cast<int>(blockIdx.x);
   if (b < p.list_blocks) {
     const int i = b / p.heads;
-    prepare_items(p, b % p.heads, p.rows[i], p.per_head[i], p.items[i]);
+    prepare_items(p, b % p.heads, p.rows[i], p.per_head[i], p.stride[i], p.items[i]);
     return;
   }
   b -= p.list_blocks;
@@ -602,6 +644,45 @@ __global__ __launch_bounds__(256) void join_parts_kernel(size_t count, int split
     *reinterpret_cast<float4 *>(at) = make_float4(s.x * f, s.y * f, s.z * f, s.w * f);
 }
 
+// O and lse, or dQ, from the parts' sums.  A group of D / 4 lanes per query, in the
+// clusters' order: queries in no cluster are left as they were.
+template <typename T, int D, bool GRAD>
+__global__ __launch_bounds__(256) void join_queries_kernel(TrainArgs a, T *out) {
+  constexpr int LANES = D / 4;
+  const int h = blockIdx.y, pos = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, x = threadIdx.x % LANES;
+  const size_t first = static_cast<size_t>(h) * a.n;
+  const int32_t *off = a.offsets + static_cast<size_t>(h) * (a.c_q + 1);
+  if (pos < off[0] || pos >= min(off[a.c_q], a.n)) return;
+  const size_t row = first + min(max(a.perm[first + pos], 0), a.n - 1);
+  const float2 *ml = reinterpret_cast<const float2 *>(a.parts + a.splits * a.rows * D);
+  float top = 0.0f, l = 0.0f, f = a.scale;
+  if constexpr (!GRAD) {
+    top = -INFINITY;
+    for (int p = 0; p < a.splits; ++p) top = fmaxf(top, ml[p * a.rows + row].x);
+    if (top == -INFINITY) top = 0.0f;
+    for (int p = 0; p < a.splits; ++p) {
+      const float2 s = ml[p * a.rows + row];
+      l = fmaf(s.y, __builtin_amdgcn_exp2f(s.x - top), l);
+    }
+    f = l > 0.0f ? a.kept_scale / l : 0.0f;
+    if (x == 0) a.lse[row] = l > 0.0f ? (top + __log2f(l)) * kLn2 : l == 0.0f ? -INFINITY : l;
+  }
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int p = 0; p < a.splits; ++p) {
+    const float4 v = *reinterpret_cast<const float4 *>(a.parts + (p * a.rows + row) * D + 4 * x);
+    const float w = GRAD ? 1.0f : __builtin_amdgcn_exp2f(ml[p * a.rows + row].x - top);
+    s.x = fmaf(v.x, w, s.x);
+    s.y = fmaf(v.y, w, s.y);
+    s.z = fmaf(v.z, w, s.z);
+    s.w = fmaf(v.w, w, s.w);
+  }
+  T *to = out + row * D + 4 * x;
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(s.x * f, s.y * f), pack_bf16(s.z * f, s.w * f));
+  else
+    *reinterpret_cast<float4 *>(to) = make_float4(s.x * f, s.y * f, s.z * f, s.w * f);
+}
+
 template <typename K, typename... A>
 hipError_t launch(K kernel, dim3 grid, int threads, hipStream_t s, A... args) {
   hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, args...);
@@ -620,6 +701,45 @@ hipError_t join_parts(size_t count, int splits, float scale_k, float scale_v, co
                 scale_v, parts, dk, dv);
 }
 
+// Parts that each block's tiles are cut into, with fp32 sums of their own that a
+// second kernel adds: as many, up to 16 of `least` tiles or more, as make the
+// launch's rounds shortest; a part costs about 4% of a block more (its start, its
+// sums).  `resident`: the blocks that the chip holds at once.
+int parts_of(long long blocks, long long tiles, int least, int resident) {
+  constexpr int kMost = 16;
+  int best = 1;
+  double shortest = 0.0;
+  for (int s = 1; s <= kMost && (s == 1 || s * least <= tiles); ++s) {
+    const double rounds = static_cast<double>((blocks * s + resident - 1) / resident) * (1.0 / s + 0.04);
+    if (s == 1 || rounds < shortest) {
+      shortest = rounds;
+      best = s;
+    }
+  }
+  return best;
+}
+int key_splits(int heads, int n, int d, bool bf16, int c_q) {
+  const int keys = bf16 ? train_key_block(d) : kRows, tile = bf16 ? kTrainKeyTile : kTile;
+  return parts_of(static_cast<long long>(heads) * ((n + keys - 1) / keys), train_items_per_head(n, c_q, tile), 2,
+                  bf16 && d == 128 ? 256 : 512);
+}
+// The lists are on the device: clusters of a block's queries or fewer are taken to
+// fill a block each, larger ones half a block more than their queries do, and every
+// key to be selected.
+int query_splits(int heads, int n, int d, bool bf16, int c_q) {
+  const int rows = bf16 ? kBM : kRows, tile = bf16 ? kBN : kTile;
+  const long long chunks = n / rows + c_q / 2 > c_q ? n / rows + (c_q + 1) / 2 : c_q;
+  const int resident = bf16 && d == 128 ? 256 : 512;
+  // a block order of its own fills the chip better, where there are the blocks
+  if (bf16 && 2 * heads * chunks > resident && attention_ordered(heads, n, d, c_q)) return 1;
+  return parts_of(heads * chunks, n / tile, 4, resident);
+}
+// Whether the work slots of a bf16 call are listed with the rest: chunks alone, in
+// cluster order.  With so few no slots share a block and their order matters little.
+bool lists_slots(int heads, int n, int c_q) {
+  return static_cast<long long>(heads) * attn_items_per_head(n, c_q) <= 256;
+}
+
 // grad: masks and statistics too.
 template <typename T, int D>
 hipError_t prepare(const TrainArgs &a, const TrainCall &c, bool grad, hipStream_t s) {
@@ -631,13 +751,15 @@ hipError_t prepare(const TrainArgs &a, const TrainCall &c, bool grad, hipStream_
   p.sel_counts = a.sel_counts;
   p.sel_idx = a.sel_idx;
   int lists = 0;
-  auto list = [&](int4 *items, int rows) {
+  auto list = [&](int4 *items, int rows, int stride) {
     p.items[lists] = items;
     p.rows[lists] = rows;
+    p.stride[lists] = stride;
     p.per_head[lists++] = train_items_per_head(a.n, a.c_q, rows);
   };
-  if (sizeof(T) == 4) list(c.items, kRows);
-  if (grad) list(c.tiles, sizeof(T) == 4 ? kTile : kTrainKeyTile);
+  if (sizeof(T) == 4) list(c.items, kRows, 1);
+  else if (lists_slots(c.heads, a.n, a.c_q)) list(c.slots.items, kBM, 2);
+  if (grad) list(c.tiles, sizeof(T) == 4 ? kTile : kTrainKeyTile, 1);
   p.list_blocks = lists * c.heads;
   p.word_blocks = a.drop ? 2 * c.heads * ((a.n + 255) / 256) : 0;
   p.rng = c.rng;
@@ -658,67 +780,54 @@ hipError_t prepare(const TrainArgs &a, const TrainCall &c, bool grad, hipStream_
   return launch(train_prepare_kernel<T, D>, dim3(static_cast<unsigned>(blocks)), 256, s, p);
 }
 
+// The kernels by queries, and where they ran in parts the join.
 template <typename T, int D>
-hipError_t forward(TrainArgs a, const TrainCall &c, hipStream_t s) {
-  TRAIN_TRY((prepare<T, D>(a, c, false, s)));
+hipError_t queries(TrainArgs a, const TrainCall &c, bool grad, T *out, hipStream_t s) {
+  a.splits = query_splits(c.heads, a.n, D, sizeof(T) == 2, a.c_q);
   if constexpr (sizeof(T) == 2) {
-    return train_queries(D, false, a, c.heads, c.slots, static_cast<T *>(c.o), s);
+    TRAIN_TRY(train_queries(D, grad, a, c.heads, lists_slots(c.heads, a.n, a.c_q), c.slots, out, s));
   } else {
     a.items = c.items;
     a.items_per_head = train_items_per_head(a.n, a.c_q, kRows);
-    const dim3 grid(static_cast<unsigned>(c.heads) * a.items_per_head);
-    return a.drop ? launch(train_queries_kernel<D, false, true>, grid, kThreads, s, a, static_cast<T *>(c.o))
-                  : launch(train_queries_kernel<D, false, false>, grid, kThreads, s, a, static_cast<T *>(c.o));
+    const dim3 grid(static_cast<unsigned>(c.heads) * a.items_per_head * a.splits);
+    if (grad)
+      TRAIN_TRY(a.drop ? launch(train_queries_kernel<D, true, true>, grid, kThreads, s, a, out)
+                       : launch(train_queries_kernel<D, true, false>, grid, kThreads, s, a, out));
+    else
+      TRAIN_TRY(a.drop ? launch(train_queries_kernel<D, false, true>, grid, kThreads, s, a, out)
+                       : launch(train_queries_kernel<D, false, false>, grid, kThreads, s, a, out));
   }
+  if (a.splits == 1) return hipSuccess;
+  const dim3 grid((a.n + 1024 / D - 1) / (1024 / D), c.heads);
+  return grad ? launch(join_queries_kernel<T, D, true>, grid, 256, s, a, out)
+              : launch(join_queries_kernel<T, D, false>, grid, 256, s, a, out);
+}
+
+template <typename T, int D>
+hipError_t forward(const TrainArgs &a, const TrainCall &c, hipStream_t s) {
+  TRAIN_TRY((prepare<T, D>(a, c, false, s)));
+  return queries<T, D>(a, c, false, static_cast<T *>(c.o), s);
 }
 
 template <typename T, int D>
 hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
   TRAIN_TRY((prepare<T, D>(a, c, true, s)));
-  T *dq = static_cast<T *>(c.dq), *dk = static_cast<T *>(c.dk), *dv = static_cast<T *>(c.dv);
+  TRAIN_TRY((queries<T, D>(a, c, true, static_cast<T *>(c.dq), s)));
+  T *dk = static_cast<T *>(c.dk), *dv = static_cast<T *>(c.dv);
+  a.items = c.tiles;
+  a.items_per_head = train_items_per_head(a.n, a.c_q, sizeof(T) == 2 ? kTrainKeyTile : kTile);
+  a.splits = key_splits(c.heads, a.n, D, sizeof(T) == 2, a.c_q);
   if constexpr (sizeof(T) == 2) {
-    TRAIN_TRY(train_queries(D, true, a, c.heads, c.slots, dq, s));
-    a.items = c.tiles;
-    a.items_per_head = train_items_per_head(a.n, a.c_q, kTrainKeyTile);
-    const int splits = train_key_splits(c.heads, a.n, train_key_block(D), a.items_per_head);
-    TRAIN_TRY(train_keys(D, a, c.heads, splits, c.parts, dk, dv, s));
-    return splits > 1 ? join_parts(a.rows * D, splits, a.scale, a.kept_scale, c.parts, dk, dv, s) : hipSuccess;
+    TRAIN_TRY(train_keys(D, a, c.heads, dk, dv, s));
   } else {
-    a.items = c.items;
-    a.items_per_head = train_items_per_head(a.n, a.c_q, kRows);
-    const dim3 qgrid(static_cast<unsigned>(c.heads) * a.items_per_head);
-    TRAIN_TRY(a.drop ? launch(train_queries_kernel<D, true, true>, qgrid, kThreads, s, a, dq)
-                     : launch(train_queries_kernel<D, true, false>, qgrid, kThreads, s, a, dq));
-    a.items = c.tiles;
-    a.items_per_head = train_items_per_head(a.n, a.c_q, kTile);
-    const int splits = train_key_splits(c.heads, a.n, kRows, a.items_per_head);
-    const dim3 kgrid(static_cast<unsigned>(c.heads) * splits * ((a.n + kRows - 1) / kRows));
-    TRAIN_TRY(a.drop ? launch(train_keys_kernel<D, true>, kgrid, kThreads, s, a, splits, dk, dv, c.parts)
-                     : launch(train_keys_kernel<D, false>, kgrid, kThreads, s, a, splits, dk, dv, c.parts));
-    return splits > 1 ? join_parts(a.rows * D, splits, a.scale, a.kept_scale, c.parts, dk, dv, s) : hipSuccess;
+    const dim3 grid(static_cast<unsigned>(c.heads) * a.splits * ((a.n + kRows - 1) / kRows));
+    TRAIN_TRY(a.drop ? launch(train_keys_kernel<D, true>, grid, kThreads, s, a, dk, dv)
+                     : launch(train_keys_kernel<D, false>, grid, kThreads, s, a, dk, dv));
   }
+  return a.splits > 1 ? join_parts(a.rows * D, a.splits, a.scale, a.kept_scale, a.parts, dk, dv, s) : hipSuccess;
 }
 
 }  // namespace
-
-// Parts of the query tiles, each with fp32 sums of its own that a second kernel adds.
-// The chip holds one block per CU: as many parts, up to 16 of two tiles or more, as
-// make the launch's rounds shortest, a part costing about 2% of a round more (its
-// start, its sums).  3 heads x 2185 tokens (27 key blocks): TODO.
-int train_key_splits(int heads, int n, int keys, int tiles) {
-  constexpr int kMost = 16, kCus = 256;
-  const long long blocks = static_cast<long long>(heads) * ((n + keys - 1) / keys);
-  int best = 1;
-  double least = 0.0;
-  for (int s = 1; s <= kMost && (s == 1 || 2 * s <= tiles); ++s) {
-    const double rounds = static_cast<double>((blocks * s + kCus - 1) / kCus) * (1.0 / s + 0.02);
-    if (s == 1 || rounds < least) {
-      least = rounds;
-      best = s;
-    }
-  }
-  return best;
-}
 
 int train_items_per_head(int n, int c_q, int rows) { return (n + rows - 1) / rows + c_q; }
 
@@ -738,17 +847,17 @@ size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, 
   char *words = take(H * n * 4 * sizeof(uint32_t));
   char *stats = take(H * (n + 1) * 2 * sizeof(float));
   char *masks = take(H * ((n + kTrainKeyBlock - 1) / kTrainKeyBlock) * c_q * (kTrainKeyBlock / 8));
-  const int splits = train_key_splits(heads, n, bf16 ? train_key_block(d) : kRows,
-                                      train_items_per_head(n, c_q, bf16 ? kTrainKeyTile : kTile));
-  char *parts = take(splits > 1 ? H * n * d * splits * 2 * sizeof(float) : 0);
+  const size_t sk = key_splits(heads, n, d, bf16, c_q), sq = query_splits(heads, n, d, bf16, c_q);
+  const size_t by_keys = sk > 1 ? 2 * sk * d : 0, by_queries = sq > 1 ? sq * (d + 2) : 0;
+  char *parts = take(H * n * (by_keys > by_queries ? by_keys : by_queries) * sizeof(float));
   if (a) {
     a->words = reinterpret_cast<uint32_t *>(words);
     a->stats = reinterpret_cast<float *>(stats);
     a->masks = reinterpret_cast<uint32_t *>(masks);
+    a->parts = reinterpret_cast<float *>(parts);
     c->items = c->slots.items = reinterpret_cast<int4 *>(items);
     c->slots.order = ordered ? reinterpret_cast<int2 *>(order) : nullptr;
     c->tiles = reinterpret_cast<int4 *>(tiles);
-    c->parts = reinterpret_cast<float *>(parts);
   }
   return used;
 }

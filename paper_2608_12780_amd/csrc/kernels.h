@@ -276,6 +276,11 @@ struct TrainArgs {
   float *lse;
   const int4 *items;
   size_t rows;             // heads * n
+  // parts that a block's tiles are cut into, and with more than one their sums:
+  // dK and dV [part][2][rows][d]; O or dQ [part][rows][d], then of the forward the
+  // running maximum and normaliser [part][rows][2]
+  int splits;
+  float *parts;
   const uint32_t *words;   // dropout: [heads][query 0, query 1, key 0, key 1][n]
   const float *stats;      // [heads][-lse in the exp2 domain, <do, o>][n + 1]
   const uint32_t *masks;   // key bits: [heads][ceil(n / 256)][c_q][8]
@@ -286,7 +291,6 @@ struct TrainCall {
   void *o, *dq, *dk, *dv;
   int4 *items, *tiles;     // items: fp32; tiles: the queries' of dK and dV
   AttnScratch slots;       // bf16: the work slots of the forward and of dQ
-  float *parts;            // sums of the query parts (train_key_splits > 1)
   int32_t *status;
 };
 constexpr int kTrainKeyBlock = 256;  // keys of a mask row
@@ -296,10 +300,10 @@ constexpr int kTrainKeyTile = 64;    // queries of a tile (attention_keys.hip)
 // Parts that the query tiles are cut into for dK and dV, `keys` keys per block.
 int train_key_splits(int heads, int n, int keys, int tiles);
 // The forward into `o` (grad false), or dQ from a.stats (grad true).
-hipError_t train_queries(int d, bool grad, const TrainArgs &a, int heads, const AttnScratch &w,
-                         uint16_t *out, hipStream_t s);
-hipError_t train_keys(int d, const TrainArgs &a, int heads, int splits, float *parts, uint16_t *dk,
-                      uint16_t *dv, hipStream_t s);
+// listed: the work slots are there already.
+hipError_t train_queries(int d, bool grad, const TrainArgs &a, int heads, bool listed,
+                         const AttnScratch &w, uint16_t *out, hipStream_t s);
+hipError_t train_keys(int d, const TrainArgs &a, int heads, uint16_t *dk, uint16_t *dv, hipStream_t s);
 int train_items_per_head(int n, int c_q, int rows);
 // Lays the workspace out (base null: only its size).
 size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, TrainArgs *a,
