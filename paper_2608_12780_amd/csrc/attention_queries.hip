@@ -235,7 +235,10 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
           const int e = 4 * i + j;
           p[e] = __builtin_amdgcn_exp2f(fmaf(s[kb][e], a.scale_log2, neg_m));
           sum[j] += p[e];
-          if (DROP && !pair_kept(mine, kw[j], a.drop)) p[e] = 0.0f;
+          if constexpr (DROP) {
+            p[e] = pair_kept(mine, kw[j], a.drop) ? p[e] : 0.0f;
+            asm("" : "+v"(p[e]));  // or both are rounded and the bits selected
+          }
         }
       }
       pk[kb][0] = pack8(p);
@@ -384,7 +387,7 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
 
 template <int D, bool GRAD, bool DROP>
 __global__ __launch_bounds__(kNW * 64)
-__attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void queries_kernel(TrainArgs a, int total_items,
+__attribute__((amdgpu_waves_per_eu(D == 64 && !DROP ? 4 : 2))) void queries_kernel(TrainArgs a, int total_items,
                                                                          const int4 *__restrict__ items,
                                                                          const int2 *__restrict__ order, uint16_t *out) {
   typedef Tiles<D, DROP> T;
