@@ -13,7 +13,7 @@ LIB = os.path.join(PKG, "libscope.so")
 SOURCES = ["api.cpp", "kmeans.hip", "kmeans_mfma.hip", "kmeans_update.hip",
            "kmeans_codebook.hip", "kmeans_lloyd.hip", "score.hip",
            "select.hip",
-           "attention.hip", "attention_train.hip", "attention_queries.hip", "attention_keys.hip", "dropout.hip", "peaks.hip"]
+           "attention.hip", "attention_train.hip", "attention_queries.hip", "attention_keys.hip", "attention_order.hip", "dropout.hip", "peaks.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = [

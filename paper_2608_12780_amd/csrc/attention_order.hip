@@ -1,0 +1,156 @@
+// An order of the keys for dK and dV.
+//
+// The gradient kernel runs 32 keys of a wave against every query tile whose cluster
+// keeps one of them, so keys in token order waste what their neighbours' sets do not
+// share: on the sparse layer's own sets (5 heads x 32760 tokens, 128 clusters) 43%
+// of the products at 54% kept keys, 72% at 15%.  Keys that the same clusters keep
+// belong together.  A key's signature are its bits in 12 clusters, spread over the
+// list; keys are sorted by it, signatures in the order of the reflected Gray code,
+// where neighbours differ in one cluster.  A head uses the order where it leaves
+// fewer (wave, tile) pairs, by 3%; where sets follow the token order it does not.
+// The gradients are the same bit for bit in any order: every key's sums have their
+// own column of the matrix products and run over the same tiles, a tile that does
+// not keep the key adding zeros.  (So the order within a signature may vary.)
+#include "common.h"
+#include "kernels.h"
+
+namespace scope {
+
+namespace {
+
+constexpr int kBits = 12;
+static_assert(kOrderBins == 1 << kBits, "a bin per signature");
+constexpr int kWords = kTrainKeyBlock / 32;
+
+__device__ __forceinline__ size_t mask_row(const TrainArgs &a, int h, int block, int c) {
+  return ((static_cast<size_t>(h) * ((a.n + kTrainKeyBlock - 1) / kTrainKeyBlock) + block) * a.c_q + c) * kWords;
+}
+
+// A block's keys are counted and placed through its own bins in LDS: many keys share
+// a signature (5 heads x 32760, 15% kept: 131 us with global counters alone).
+constexpr int kSortThreads = 1024, kSortKeys = 4;  // keys per thread
+
+__global__ __launch_bounds__(kSortThreads) void order_count_kernel(TrainArgs a) {
+  __shared__ uint32_t count[kOrderBins];
+  const int h = blockIdx.y, t = threadIdx.x;
+  for (int i = t; i < kOrderBins; i += kSortThreads) count[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSortKeys; ++i) {
+    const int key = (blockIdx.x * kSortKeys + i) * kSortThreads + t;
+    if (key >= a.n) break;
+    uint32_t gray = 0;
+#pragma unroll
+    for (int x = 0; x < kBits; ++x) {
+      const int c = (2 * x + 1) * a.c_q / (2 * kBits);
+      const uint32_t w = a.masks[mask_row(a, h, key / kTrainKeyBlock, c) + key % kTrainKeyBlock / 32];
+      gray = 2 * gray + (w >> (key & 31) & 1u);
+    }
+    // the signature's place in the Gray code's sequence
+    uint32_t bin = gray;
+#pragma unroll
+    for (int s = 1; s < kBits; s *= 2) bin ^= bin >> s;
+    a.order.bin[static_cast<size_t>(h) * a.n + key] = static_cast<uint16_t>(bin);
+    atomicAdd(&count[bin], 1u);
+  }
+  __syncthreads();
+  for (int i = t; i < kOrderBins; i += kSortThreads)
+    if (count[i]) atomicAdd(&a.order.start[static_cast<size_t>(h) * kOrderBins + i], count[i]);
+}
+
+// Counts to first positions.
+__global__ __launch_bounds__(1024) void order_scan_kernel(TrainArgs a) {
+  __shared__ uint32_t wtot[16];
+  constexpr int PER = kOrderBins / 1024;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  uint32_t *start = a.order.start + static_cast<size_t>(blockIdx.x) * kOrderBins + PER * t;
+  uint32_t k[PER], mine = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) mine += k[i] = start[i];
+  const uint32_t incl = wave_incl_scan(mine);
+  if (lane == 63) wtot[w] = incl;
+  __syncthreads();
+  uint32_t at = incl - mine;
+  for (int i = 0; i < w; ++i) at += wtot[i];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    start[i] = at;
+    at += k[i];
+  }
+}
+
+__global__ __launch_bounds__(kSortThreads) void order_place_kernel(TrainArgs a) {
+  __shared__ uint32_t next[kOrderBins];
+  const int h = blockIdx.y, t = threadIdx.x;
+  const size_t first = static_cast<size_t>(h) * a.n;
+  for (int i = t; i < kOrderBins; i += kSortThreads) next[i] = 0;
+  __syncthreads();
+  int bin[kSortKeys];
+#pragma unroll
+  for (int i = 0; i < kSortKeys; ++i) {
+    const int key = (blockIdx.x * kSortKeys + i) * kSortThreads + t;
+    bin[i] = key < a.n ? a.order.bin[first + key] : -1;
+    if (bin[i] >= 0) atomicAdd(&next[bin[i]], 1u);
+  }
+  __syncthreads();
+  for (int i = t; i < kOrderBins; i += kSortThreads)
+    if (next[i]) next[i] = atomicAdd(&a.order.start[static_cast<size_t>(h) * kOrderBins + i], next[i]);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSortKeys; ++i) {
+    if (bin[i] < 0) continue;
+    const uint32_t at = atomicAdd(&next[bin[i]], 1u);
+    if (at < static_cast<uint32_t>(a.n)) a.order.key[first + at] = (blockIdx.x * kSortKeys + i) * kSortThreads + t;
+  }
+}
+
+// The key bits by position, and what both orders cost: (wave, tile) pairs.
+__global__ __launch_bounds__(256) void order_masks_kernel(TrainArgs a) {
+  const int b = blockIdx.x, h = blockIdx.y, t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const int pos = b * 256 + t;
+  const int key = pos < a.n ? a.order.key[static_cast<size_t>(h) * a.n + pos] : 0;
+  const uint32_t *from = a.masks + mask_row(a, h, key / kTrainKeyBlock, 0) + key % kTrainKeyBlock / 32;
+  const size_t row = mask_row(a, h, b, 0) + 2 * w;
+  const int32_t *off = a.offsets + static_cast<size_t>(h) * (a.c_q + 1);
+  unsigned long long by_key = 0, by_position = 0;
+  const int per = (a.c_q + gridDim.z - 1) / gridDim.z, c0 = blockIdx.z * per;
+#pragma unroll 4
+  for (int c = c0; c < min(c0 + per, a.c_q); ++c) {
+    const unsigned long long votes = __ballot(pos < a.n && (from[c * kWords] >> (key & 31) & 1u));
+    const uint32_t lo = static_cast<uint32_t>(votes), hi = static_cast<uint32_t>(votes >> 32);
+    if (lane == 0) *reinterpret_cast<uint2 *>(a.order.masks + row + c * kWords) = make_uint2(lo, hi);
+    const uint2 old = *reinterpret_cast<const uint2 *>(a.masks + row + c * kWords);
+    const unsigned long long tiles = (max(off[c + 1] - off[c], 0) + 31) / 32;
+    by_key += tiles * ((old.x != 0) + (old.y != 0));
+    by_position += tiles * ((lo != 0) + (hi != 0));
+  }
+  __shared__ unsigned long long sum[2];
+  if (t < 2) sum[t] = 0;
+  __syncthreads();
+  if (lane == 0) {
+    atomicAdd(&sum[0], by_key);
+    atomicAdd(&sum[1], by_position);
+  }
+  __syncthreads();
+  // spread over a head's slots: one counter for all blocks was most of the kernel
+  if (t < 2) atomicAdd(&a.order.cost[(static_cast<size_t>(h) * kOrderSlots + (b + blockIdx.z) % kOrderSlots) * 2 + t], sum[t]);
+}
+
+}  // namespace
+
+// Few keys or clusters leave little to gain over the launches (measured: TODO).
+bool train_orders_keys(int n, int c_q, bool bf16) { return bf16 && n >= 8192 && c_q >= 24; }
+
+// After the bins and costs have been cleared.
+hipError_t train_order(const TrainArgs &a, int heads, hipStream_t s) {
+  constexpr int kKeys = kSortThreads * kSortKeys;
+  const dim3 grid((a.n + kKeys - 1) / kKeys, heads);
+  hipLaunchKernelGGL(order_count_kernel, grid, dim3(kSortThreads), 0, s, a);
+  hipLaunchKernelGGL(order_scan_kernel, dim3(heads), dim3(1024), 0, s, a);
+  hipLaunchKernelGGL(order_place_kernel, grid, dim3(kSortThreads), 0, s, a);
+  // the clusters in eighths: its loads are scattered words
+  hipLaunchKernelGGL(order_masks_kernel, dim3((a.n + 255) / 256, heads, 8), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace scope

@@ -447,6 +447,7 @@ struct Prepare {
   int4 *items[2];
   int rows[2], per_head[2], stride[2];  // stride 2: work slots of one chunk
   uint32_t *masks;
+  KeyOrder order;  // its bins and costs are cleared
   int32_t *status;
   const uint64_t *rng;
   uint32_t *words;
@@ -598,6 +599,11 @@ __global__ __launch_bounds__(256) void train_prepare_kernel(Prepare p) {
   int b = static_cast<int>(blockIdx.x);
   if (b < p.list_blocks) {
     const int i = b / p.heads;
+    if (i == 0 && p.order.cost) {
+      const int h = b % p.heads;
+      for (int x = threadIdx.x; x < kOrderBins; x += 256) p.order.start[static_cast<size_t>(h) * kOrderBins + x] = 0;
+      if (threadIdx.x < 2 * kOrderSlots) p.order.cost[static_cast<size_t>(h) * 2 * kOrderSlots + threadIdx.x] = 0;
+    }
     prepare_items(p, b % p.heads, p.rows[i], p.per_head[i], p.stride[i], p.items[i]);
     return;
   }
@@ -768,6 +774,7 @@ hipError_t prepare(const TrainArgs &a, const TrainCall &c, bool grad, hipStream_
   if (grad) {
     p.mask_blocks = c.heads * a.c_q * ((a.n + kMaskKeys - 1) / kMaskKeys);
     p.masks = const_cast<uint32_t *>(a.masks);
+    p.order = a.order;
     p.status = c.status;
     p.o = c.o;
     p.d_o = a.d_o;
@@ -818,6 +825,7 @@ hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
   a.items_per_head = train_items_per_head(a.n, a.c_q, sizeof(T) == 2 ? kTrainKeyTile : kTile);
   a.splits = key_splits(c.heads, a.n, D, sizeof(T) == 2, a.c_q);
   if constexpr (sizeof(T) == 2) {
+    if (a.order.cost) TRAIN_TRY(train_order(a, c.heads, s));
     TRAIN_TRY(train_keys(D, a, c.heads, dk, dv, s));
   } else {
     const dim3 grid(static_cast<unsigned>(c.heads) * a.splits * ((a.n + kRows - 1) / kRows));
@@ -846,7 +854,14 @@ size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, 
   char *tiles = take(H * train_items_per_head(n, c_q, bf16 ? kTrainKeyTile : kTile) * sizeof(int4));
   char *words = take(H * n * 4 * sizeof(uint32_t));
   char *stats = take(H * (n + 1) * 2 * sizeof(float));
-  char *masks = take(H * ((n + kTrainKeyBlock - 1) / kTrainKeyBlock) * c_q * (kTrainKeyBlock / 8));
+  const size_t mask_bytes = H * ((n + kTrainKeyBlock - 1) / kTrainKeyBlock) * c_q * (kTrainKeyBlock / 8);
+  char *masks = take(mask_bytes);
+  const size_t ordered_keys = train_orders_keys(n, c_q, bf16) ? 1 : 0;
+  char *bin = take(ordered_keys * H * n * sizeof(uint16_t));
+  char *start = take(ordered_keys * H * kOrderBins * sizeof(uint32_t));
+  char *key = take(ordered_keys * H * n * sizeof(int32_t));
+  char *by_position = take(ordered_keys * mask_bytes);
+  char *cost = take(ordered_keys * H * 2 * kOrderSlots * sizeof(unsigned long long));
   const size_t sk = key_splits(heads, n, d, bf16, c_q), sq = query_splits(heads, n, d, bf16, c_q);
   const size_t by_keys = sk > 1 ? 2 * sk * d : 0, by_queries = sq > 1 ? sq * (d + 2) : 0;
   char *parts = take(H * n * (by_keys > by_queries ? by_keys : by_queries) * sizeof(float));
@@ -855,6 +870,9 @@ size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, 
     a->stats = reinterpret_cast<float *>(stats);
     a->masks = reinterpret_cast<uint32_t *>(masks);
     a->parts = reinterpret_cast<float *>(parts);
+    if (ordered_keys)
+      a->order = {reinterpret_cast<uint16_t *>(bin), reinterpret_cast<uint32_t *>(start), reinterpret_cast<int32_t *>(key),
+                  reinterpret_cast<uint32_t *>(by_position), reinterpret_cast<unsigned long long *>(cost)};
     c->items = c->slots.items = reinterpret_cast<int4 *>(items);
     c->slots.order = ordered ? reinterpret_cast<int2 *>(order) : nullptr;
     c->tiles = reinterpret_cast<int4 *>(tiles);

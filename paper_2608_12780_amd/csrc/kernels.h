@@ -266,6 +266,16 @@ size_t attention_order_entries(int heads, int n, int d, int c_q);
 // Attention for training (attention_train.hip).  TrainArgs goes to the kernels;
 // TrainCall holds what the host needs besides.
 constexpr int kTrainMaxClusters = 1024;
+// An order of the keys that brings together those that the same clusters keep, for
+// dK and dV (attention_order.hip); null: none.
+struct KeyOrder {
+  uint16_t *bin;               // [heads][n]
+  uint32_t *start;             // [heads][kOrderBins]
+  int32_t *key;                // [heads][n] the key at a position
+  uint32_t *masks;             // the key bits by position, as TrainArgs::masks
+  unsigned long long *cost;    // [heads][kOrderSlots][by key, by position]
+};
+constexpr int kOrderBins = 4096, kOrderSlots = 64;
 struct TrainArgs {
   int n, c_q, items_per_head;
   const void *q, *k, *v, *d_o;
@@ -284,6 +294,7 @@ struct TrainArgs {
   const uint32_t *words;   // dropout: [heads][query 0, query 1, key 0, key 1][n]
   const float *stats;      // [heads][-lse in the exp2 domain, <do, o>][n + 1]
   const uint32_t *masks;   // key bits: [heads][ceil(n / 256)][c_q][8]
+  KeyOrder order;
 };
 struct TrainCall {
   int heads;
@@ -303,6 +314,8 @@ int train_key_splits(int heads, int n, int keys, int tiles);
 // listed: the work slots are there already.
 hipError_t train_queries(int d, bool grad, const TrainArgs &a, int heads, bool listed,
                          const AttnScratch &w, uint16_t *out, hipStream_t s);
+bool train_orders_keys(int n, int c_q, bool bf16);
+hipError_t train_order(const TrainArgs &a, int heads, hipStream_t s);
 hipError_t train_keys(int d, const TrainArgs &a, int heads, uint16_t *dk, uint16_t *dv, hipStream_t s);
 int train_items_per_head(int n, int c_q, int rows);
 // Lays the workspace out (base null: only its size).
