@@ -20,10 +20,10 @@ namespace {
 
 constexpr int kBits = 12;
 static_assert(kOrderBins == 1 << kBits, "a bin per signature");
-constexpr int kWords = kTrainKeyBlock / 32;
+constexpr int kWords = kTrainMaskKeys / 32;
 
 __device__ __forceinline__ size_t mask_row(const TrainArgs &a, int h, int block, int c) {
-  return ((static_cast<size_t>(h) * ((a.n + kTrainKeyBlock - 1) / kTrainKeyBlock) + block) * a.c_q + c) * kWords;
+  return ((static_cast<size_t>(h) * ((a.n + kTrainMaskKeys - 1) / kTrainMaskKeys) + block) * a.c_q + c) * kWords;
 }
 
 // A block's keys are counted and placed through its own bins in LDS: many keys share
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(kSortThreads) void order_count_kernel(TrainArgs a) 
 #pragma unroll
     for (int x = 0; x < kBits; ++x) {
       const int c = (2 * x + 1) * a.c_q / (2 * kBits);
-      const uint32_t w = a.masks[mask_row(a, h, key / kTrainKeyBlock, c) + key % kTrainKeyBlock / 32];
+      const uint32_t w = a.masks[mask_row(a, h, key / kTrainMaskKeys, c) + key % kTrainMaskKeys / 32];
       gray = 2 * gray + (w >> (key & 31) & 1u);
     }
     // the signature's place in the Gray code's sequence
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void order_masks_kernel(TrainArgs a) {
   const int b = blockIdx.x, h = blockIdx.y, t = threadIdx.x, lane = t & 63, w = t >> 6;
   const int pos = b * 256 + t;
   const int key = pos < a.n ? a.order.key[static_cast<size_t>(h) * a.n + pos] : 0;
-  const uint32_t *from = a.masks + mask_row(a, h, key / kTrainKeyBlock, 0) + key % kTrainKeyBlock / 32;
+  const uint32_t *from = a.masks + mask_row(a, h, key / kTrainMaskKeys, 0) + key % kTrainMaskKeys / 32;
   const size_t row = mask_row(a, h, b, 0) + 2 * w;
   const int32_t *off = a.offsets + static_cast<size_t>(h) * (a.c_q + 1);
   unsigned long long by_key = 0, by_position = 0;
@@ -144,7 +144,7 @@ bool train_orders_keys(int n, int c_q, bool bf16) { return bf16 && n >= 8192 && 
 // After the bins and costs have been cleared.
 hipError_t train_order(const TrainArgs &a, int heads, hipStream_t s) {
   constexpr int kKeys = kSortThreads * kSortKeys;
-  const dim3 grid((a.n + kKeys - 1) / kKeys, heads);
+  const dim3 grid((a.n + kTrainKeyBlock - 1) / kTrainKeyBlock, heads);
   hipLaunchKernelGGL(order_count_kernel, grid, dim3(kSortThreads), 0, s, a);
   hipLaunchKernelGGL(order_scan_kernel, dim3(heads), dim3(1024), 0, s, a);
   hipLaunchKernelGGL(order_place_kernel, grid, dim3(kSortThreads), 0, s, a);

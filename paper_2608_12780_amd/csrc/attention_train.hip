@@ -310,9 +310,9 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void train_keys_kernel(Tra
 #pragma unroll
   for (int cb = 0; cb < D / 16; ++cb) dka[cb] = dva[cb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   // the block's two words of each cluster, 16 bits a wave
-  constexpr int WORDS = kTrainKeyBlock / 32, SHARE = kTrainKeyBlock / kRows;
+  constexpr int WORDS = kTrainMaskKeys / 32, SHARE = kTrainMaskKeys / kRows;
   static_assert(kRows == 64, "two words per block");
-  const uint32_t *masks = a.masks + (static_cast<size_t>(h) * ((a.n + kTrainKeyBlock - 1) / kTrainKeyBlock) + b / SHARE) * a.c_q * WORDS +
+  const uint32_t *masks = a.masks + (static_cast<size_t>(h) * ((a.n + kTrainMaskKeys - 1) / kTrainMaskKeys) + b / SHARE) * a.c_q * WORDS +
                           2 * (b % SHARE);
 
   const uint32_t bytes = static_cast<uint32_t>(a.n) * (4 * D);
@@ -555,8 +555,8 @@ __device__ void prepare_masks(const Prepare &p, int h, int c, int from, int segm
   }
   if (bad && p.status) atomicOr(p.status, kStatusBadSet);
   __syncthreads();
-  constexpr int WORDS = kTrainKeyBlock / 32;
-  const int blocks = (n + kTrainKeyBlock - 1) / kTrainKeyBlock, b = from / kTrainKeyBlock + t / WORDS;
+  constexpr int WORDS = kTrainMaskKeys / 32;
+  const int blocks = (n + kTrainMaskKeys - 1) / kTrainMaskKeys, b = from / kTrainMaskKeys + t / WORDS;
   if (b < blocks) p.masks[((static_cast<size_t>(h) * blocks + b) * p.c_q + c) * WORDS + t % WORDS] = bits[t];
 }
 
@@ -725,9 +725,9 @@ int parts_of(long long blocks, long long tiles, int least, int resident) {
   return best;
 }
 int key_splits(int heads, int n, int d, bool bf16, int c_q) {
-  const int keys = bf16 ? train_key_block(d) : kRows, tile = bf16 ? kTrainKeyTile : kTile;
+  const int keys = bf16 ? kTrainKeyBlock : kRows, tile = bf16 ? kTrainKeyTile : kTile;
   return parts_of(static_cast<long long>(heads) * ((n + keys - 1) / keys), train_items_per_head(n, c_q, tile), 2,
-                  bf16 && d == 128 ? 256 : 512);
+                  512);
 }
 // The lists are on the device: clusters of a block's queries or fewer are taken to
 // fill a block each, larger ones half a block more than their queries do, and every
@@ -854,7 +854,7 @@ size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, 
   char *tiles = take(H * train_items_per_head(n, c_q, bf16 ? kTrainKeyTile : kTile) * sizeof(int4));
   char *words = take(H * n * 4 * sizeof(uint32_t));
   char *stats = take(H * (n + 1) * 2 * sizeof(float));
-  const size_t mask_bytes = H * ((n + kTrainKeyBlock - 1) / kTrainKeyBlock) * c_q * (kTrainKeyBlock / 8);
+  const size_t mask_bytes = H * ((n + kTrainMaskKeys - 1) / kTrainMaskKeys) * c_q * (kTrainMaskKeys / 8);
   char *masks = take(mask_bytes);
   const size_t ordered_keys = train_orders_keys(n, c_q, bf16) ? 1 : 0;
   char *bin = take(ordered_keys * H * n * sizeof(uint16_t));

@@ -304,10 +304,9 @@ struct TrainCall {
   AttnScratch slots;       // bf16: the work slots of the forward and of dQ
   int32_t *status;
 };
-constexpr int kTrainKeyBlock = 256;  // keys of a mask row
-// keys of a block of dK and dV, bf16
-constexpr int train_key_block(int d) { return d == 128 ? 256 : 128; }
-constexpr int kTrainKeyTile = 64;    // queries of a tile (attention_keys.hip)
+constexpr int kTrainMaskKeys = 256;  // keys of a mask row
+constexpr int kTrainKeyBlock = 128;  // keys of a block of dK and dV (attention_keys.hip)
+constexpr int kTrainKeyTile = 32;    // queries of its tiles
 // Parts that the query tiles are cut into for dK and dV, `keys` keys per block.
 int train_key_splits(int heads, int n, int keys, int tiles);
 // The forward into `o` (grad false), or dQ from a.stats (grad true).
