@@ -138,13 +138,22 @@ __global__ __launch_bounds__(256) void order_masks_kernel(TrainArgs a) {
 
 }  // namespace
 
-// Few keys or clusters leave little to gain over the launches (measured: TODO).
-bool train_orders_keys(int n, int c_q, bool bf16) { return bf16 && n >= 8192 && c_q >= 24; }
+// The order takes four launches, 20 to 50 us, which few keys do not earn: the whole
+// backward pass with it for the time without, 8 heads, d = 128, 8 to 96 clusters:
+//   tokens             2048        4096        8192       16384 (4 heads)
+//   sets of whole groups of scattered keys, 20% kept
+//                 1.01-1.10   0.84-0.97   0.70-0.84   0.59-0.68
+//   each key at random, 50% kept
+//                 1.09-1.11   0.99-1.06   0.95-1.02   0.94-1.01
+//   sets of runs of 128 tokens, 30% kept (the order is found and not used)
+//                 1.13-1.19   1.09-1.12   1.04-1.07   1.03-1.04
+// Fewer than 8 clusters were not measured: such sets share most blocks of 32 keys.
+bool train_orders_keys(int n, int c_q, bool bf16) { return bf16 && n >= 8192 && c_q >= 8; }
 
 // After the bins and costs have been cleared.
 hipError_t train_order(const TrainArgs &a, int heads, hipStream_t s) {
   constexpr int kKeys = kSortThreads * kSortKeys;
-  const dim3 grid((a.n + kTrainKeyBlock - 1) / kTrainKeyBlock, heads);
+  const dim3 grid((a.n + kKeys - 1) / kKeys, heads);
   hipLaunchKernelGGL(order_count_kernel, grid, dim3(kSortThreads), 0, s, a);
   hipLaunchKernelGGL(order_scan_kernel, dim3(heads), dim3(1024), 0, s, a);
   hipLaunchKernelGGL(order_place_kernel, grid, dim3(kSortThreads), 0, s, a);
