@@ -45,8 +45,8 @@
  *    checked in the first update pass of calls 1 and 2.  Nothing aborts or
  *    prints.
  *  - Determinism: every output is bitwise reproducible run to run and
- *    independent of launch geometry; calls 1-4 are bit-exact with respect to
- *    the canonical arithmetic defined under each call.
+ *    independent of launch geometry (calls 6 and 7: see there); calls 1-4 are
+ *    bit-exact with respect to the canonical arithmetic defined under each call.
  */
 #ifndef SCOPE_H
 #define SCOPE_H
@@ -375,10 +375,15 @@ int32_t scope_training_workspace_size(const scope_shape *shape, int32_t c_q,
  * rounded (fp32 matrix products), unlike call 5's.  Sums and statistics are
  * fp32.  A cluster without keys gives O = 0 and lse = -inf.  Rows of queries in
  * no cluster are left as they were, in O and lse [heads][n].
- * S_c must be strictly ascending (as call 4 writes it): a key counts once.
- * Requirements and errors as call 5, and SCOPE_ERR_UNSUPPORTED for c_q > 1024 or
- * fp32 rows with n * d * 4 >= 2^32; the outputs must not overlap the inputs or
- * each other (SCOPE_ERR_INVALID_ARGUMENT).                                  */
+ * S_c must be strictly ascending (as call 4 writes it): a key counts once; perm
+ * must not hold a query twice.
+ * Requirements and errors as call 5, and SCOPE_ERR_UNSUPPORTED for c_q > 1024,
+ * rows of a head of 2^32 bytes or more, or so many heads and clusters that a
+ * launch would need 2^32 threads; the outputs must not overlap the inputs or each
+ * other (SCOPE_ERR_INVALID_ARGUMENT where O overlaps Q, K or V).
+ * Calls 6 and 7 repeat bit for bit.  Long sums may be cut into parts, whose
+ * number follows from heads, n, d, c_q and the dtype, so a head's last bits can
+ * differ between calls of different sizes.                                  */
 int32_t scope_sparse_attention_train(const scope_shape *shape, const void *q,
                                      const void *k, const void *v, int32_t c_q,
                                      const int32_t *offsets,
@@ -402,8 +407,10 @@ int32_t scope_sparse_attention_train(const scope_shape *shape, const void *q,
  * dQ for every query in a cluster (0 where its cluster keeps no key); rows of
  * queries in no cluster are left as they were and give no gradient.  Bad sets
  * cannot fault: a set that is not strictly ascending in [0, n) sets bit 3 of
- * dev_status (may be NULL) and its gradients are unspecified.  Requirements and
- * errors as call 6.                                                         */
+ * dev_status (may be NULL) and its gradients are unspecified.  Rows of K and V
+ * that no set holds are not read into any result; a non-finite row of Q or d_o
+ * may spread to dK and dV of keys that its cluster does not keep.  Requirements
+ * and errors as call 6; no gradient may overlap an input or another one.     */
 int32_t scope_sparse_attention_backward(
     const scope_shape *shape, const void *q, const void *k, const void *v,
     const void *o, const float *lse, const void *d_o, int32_t c_q,

@@ -893,6 +893,7 @@ int32_t check_dropout(float p, const uint64_t *rng, uint32_t *drop) {
 int32_t check_train(const scope_shape *s, int32_t c_q) {
   if (c_q > scope::kTrainMaxClusters) return SCOPE_ERR_UNSUPPORTED;
   if (static_cast<uint64_t>(s->n) * s->d * (s->dtype == SCOPE_BF16 ? 2 : 4) >= (1ull << 32)) return SCOPE_ERR_UNSUPPORTED;
+  if (!scope::train_launchable(s->heads, s->n, s->d, s->dtype == SCOPE_BF16, c_q)) return SCOPE_ERR_UNSUPPORTED;
   return SCOPE_OK;
 }
 

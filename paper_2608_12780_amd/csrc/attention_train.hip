@@ -837,6 +837,14 @@ hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
 
 }  // namespace
 
+bool train_launchable(int heads, int n, int d, bool bf16, int c_q) {
+  const uint64_t H = heads, chunks = bf16 ? attn_items_per_head(n, c_q) : train_items_per_head(n, c_q, kRows);
+  const uint64_t prepared = 2 * H + H * c_q * ((n + kMaskKeys - 1) / kMaskKeys) + 2 * H * ((n + 255) / 256) +
+                            (H * n * d * (bf16 ? 2 : 4) / 16 + 255) / 256;
+  const uint64_t keys = H * ((n + 63) / 64);
+  return prepared * 256 < (1ull << 32) && H * chunks * (bf16 ? 64 * kNW : kThreads) < (1ull << 32) && keys * 256 < (1ull << 32);
+}
+
 int train_items_per_head(int n, int c_q, int rows) { return (n + rows - 1) / rows + c_q; }
 
 size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, TrainArgs *a, TrainCall *c) {

@@ -317,6 +317,8 @@ bool train_orders_keys(int n, int c_q, bool bf16);
 hipError_t train_order(const TrainArgs &a, int heads, hipStream_t s);
 hipError_t train_keys(int d, const TrainArgs &a, int heads, uint16_t *dk, uint16_t *dv, hipStream_t s);
 int train_items_per_head(int n, int c_q, int rows);
+// Whether every launch stays below 2^32 threads.
+bool train_launchable(int heads, int n, int d, bool bf16, int c_q);
 // Lays the workspace out (base null: only its size).
 size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, TrainArgs *a,
                        TrainCall *c);

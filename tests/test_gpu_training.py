@@ -47,8 +47,8 @@ def run(x, p=0.0, rng=None, scale=0.0, attention=None):
     return dict(o=o, lse=lse, dq=dq, dk=dk, dv=dv)
 
 
-def check(x, got, p=0.0, rng=(0, 0), scale=None):
-    val, tol, held = R.reference(x, p, rng, scale, got["o"], got["lse"])
+def check(x, got, p=0.0, rng=(0, 0), scale=None, head=0):
+    val, tol, held = R.reference(x, p, rng, scale, got["o"], got["lse"], head)
     for a in ("o", "lse", "dq"):
         R.assert_within(a, got[a], val[a], tol[a], held)
         # rows of queries in no cluster stay as they were
@@ -92,6 +92,45 @@ def test_values_and_gradients(heads, n, d, dtype, c_q, keep, pattern, p):
     rng = (0x123456789AB, 77 + n)
     got = run(x, p, rng)
     check(x, got, p, rng)
+
+
+LARGE = [
+    # lists in several segments, keys run in an order of their own (random sets) or
+    # not (sets that follow the token order), lists cut into parts or not
+    (1, 9001, 64, "bf16", 30, 0.2, "", 0.1),
+    (2, 8200, 128, "bf16", 26, 0.5, "empty", 0.0),
+    (1, 8300, 128, "bf16", 40, 0.4, "prefix", 0.1),
+    (1, 9000, 128, "bf16", 300, 0.1, "", 0.0),
+    (1, 8193, 64, "bf16", 8, 0.3, "", 0.1),
+    (1, 4500, 128, "bf16", 1, 1.0, "", 0.0),       # dense, a block order of its own
+    (1, 5000, 64, "bf16", 1, 1.0, "", 0.1),
+    (2, 16400, 128, "bf16", 60, 0.3, "uncovered", 0.0),
+    (1, 8400, 128, "f32", 33, 0.3, "uncovered", 0.1),
+    (9, 1300, 64, "f32", 50, 0.3, "", 0.0),
+    (40, 700, 128, "bf16", 20, 0.5, "", 0.0),      # slots shared by two clusters
+]
+
+
+@pytest.mark.parametrize("heads,n,d,dtype,c_q,keep,pattern,p", LARGE)
+def test_large(heads, n, d, dtype, c_q, keep, pattern, p):
+    G.say(f"[training] {heads}x{n} d={d} {dtype} c_q={c_q} keep={keep} {pattern} p={p}")
+    x = R.make(heads, n, d, dtype, c_q, keep, 5, pattern)
+    got = run(x, p, (21, n))
+    # head by head: the reference holds several n x n arrays
+    for h in range(heads):
+        y = {a: t[h:h + 1] for a, t in x.items() if a != "dims"}
+        y["dims"] = (1, n, d, c_q, dtype)
+        check(y, {a: t[h:h + 1] for a, t in got.items()}, p, (21, n), head=h)
+
+
+def test_large_repeats_bit_for_bit():
+    """The keys' order is found with counters whose order varies; the results do not."""
+    x = R.make(2, 9000, 128, "bf16", 32, 0.3, 6)
+    first = run(x)
+    for _ in range(3):
+        again = run(x)
+        for name in first:
+            assert torch.equal(first[name], again[name]), name
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -299,6 +338,22 @@ def test_layer_trains_end_to_end():
     assert all(torch.isfinite(leaf.grad).all() for leaf in leaves[:3])
 
 
+def test_partition_layer_differentiates():
+    cfg = inputs.CONFIGS["tiny"]
+    x = inputs.generate(cfg)
+    sets = inputs.partition_sets(cfg, "4")
+    layer = G.make_partition_layer(cfg, sets, (8,) * 4, materialize=False)
+    q, k, v = (torch.from_numpy(a).cuda().requires_grad_() for a in (x.q, x.k, x.v))
+    y = layer.forward_train(q, k, v)
+    g = torch.randn_like(y)
+    y.backward(g)
+    case = case_of(layer, q.detach(), k.detach(), v.detach(), g)
+    got = run(case)
+    check(case, got)
+    for leaf, name in zip((q, k, v), ("dq", "dk", "dv")):
+        assert torch.equal(leaf.grad, got[name]), name
+
+
 def test_a_new_selection_before_the_backward_is_refused():
     layer, q, k, v, iq, ik = small_layer()
     qa = q.clone().requires_grad_()
@@ -340,6 +395,25 @@ def test_bad_sets_are_reported():
                    x["sel_counts"], sel)
         torch.cuda.synchronize()
         assert int(a.status.item()) == 8, (at, value)
+
+
+@pytest.mark.parametrize("at,value", [(0, -3), (1000, -3), (1000, 50000), (4499, 9000),
+                                      (2000, None), (4100, 10)])
+def test_bad_sets_of_several_segments_are_reported(at, value):
+    """Every second key of 9000; the segments' ends are searched for in the list."""
+    x = R.make(1, 9000, 64, "bf16", 30, 0.5, 1)
+    H, n, d, C, dtype = x["dims"]
+    a = TrainingAttention(H, n, d, C, dtype)
+    o, lse = (t.zero_() for t in a.outputs())
+    sel, counts = x["sel_idx"].clone(), x["sel_counts"].clone()
+    counts[0, 7] = 4500
+    sel[0, 7, :4500] = torch.arange(0, 9000, 2, dtype=sel.dtype, device=sel.device)
+    args = (x["q"], x["k"], x["v"], o, lse, x["d_o"], x["offsets"], x["perm"], counts)
+    a.backward(*args, sel)
+    assert int(a.status.item()) == 0
+    sel[0, 7, at] = sel[0, 7, at - 1] if value is None else value
+    a.backward(*args, sel)
+    assert int(a.status.item()) == 8
 
 
 def test_refusals():

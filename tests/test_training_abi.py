@@ -67,6 +67,8 @@ def test_refusals(kind):
     assert call(kind, sh=shape(d=96)) == UNSUPPORTED
     assert call(kind, sh=shape(dtype=7)) == UNSUPPORTED
     assert call(kind, sh=shape(heads=1, n=1 << 24)) == UNSUPPORTED   # 32-bit row offsets
+    assert call(kind, sh=shape(heads=1, n=1 << 23, dtype=B.F32)) == UNSUPPORTED
+    assert call(kind, sh=shape(heads=65535, n=512), c_q=512) == UNSUPPORTED  # 2^32 threads
     assert call(kind, sh=shape(heads=0)) == INVALID
     # outputs over inputs, also shifted
     out = "o" if kind == "train" else "dk"

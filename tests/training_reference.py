@@ -30,13 +30,13 @@ def threshold(p):
     return min(65535, round(float(np.float32(p)) * 65536))
 
 
-def keep_pairs(heads, n, p, seed, offset):
-    """[heads][n][n] bool: the pairs that attention dropout keeps."""
+def keep_pairs(heads, n, p, seed, offset, head=0):
+    """[heads][n][n] bool: the pairs that attention dropout keeps, from `head` on."""
     i = np.arange(n, dtype=np.uint64)
     lo, hi = np.full(n, offset & 0xFFFFFFFF, np.uint64), np.full(n, offset >> 32, np.uint64)
     out = np.empty((heads, n, n), bool)
     for h in range(heads):
-        a, b = (philox((i, np.full(n, 0x80000000 + 2 * h + side, np.uint64), lo, hi), seed)
+        a, b = (philox((i, np.full(n, 0x80000000 + 2 * (head + h) + side, np.uint64), lo, hi), seed)
                 for side in (0, 1))
         z = (a[0][:, None] ^ b[0][None]) * ((a[1][:, None] + b[1][None]) & M32)
         out[h] = ((((z >> np.uint64(32)) ^ z) & M32) >> np.uint64(16)) >= np.uint64(threshold(p))
@@ -112,7 +112,7 @@ def allowed(x):
 
 # --- forward and backward with error bounds ---------------------------------------
 
-def reference(x, p=0.0, rng=(0, 0), scale=None, o=None, lse=None):
+def reference(x, p=0.0, rng=(0, 0), scale=None, o=None, lse=None, head=0):
     """(values, bounds): dicts of float64 tensors for o and lse, and given the
     kernel's o and lse (which the gradients start from) dq, dk and dv.
 
@@ -135,7 +135,7 @@ def reference(x, p=0.0, rng=(0, 0), scale=None, o=None, lse=None):
     ok, held = (torch.from_numpy(a).to(dev) for a in allowed(x))
     m = torch.ones(H, n, n, dtype=torch.float64, device=dev)
     if threshold(p):
-        m = torch.from_numpy(keep_pairs(H, n, p, *rng)).to(dev) * (65536.0 / (65536 - threshold(p)))
+        m = torch.from_numpy(keep_pairs(H, n, p, *rng, head)).to(dev) * (65536.0 / (65536 - threshold(p)))
     T = lambda t: t.transpose(1, 2).contiguous()
     mm = torch.matmul
     s = mm(q, T(k)) * scale
