@@ -12,6 +12,20 @@
 // The forward's normaliser sums the weights in fp32 before they are rounded to bf16
 // for the product with V (the inference attention sums the rounded ones): lse is an
 // fp32 result, and 2 to 3 keys of weight would leave rounded sums 2^-9 off.
+//
+// Bound by the matrix pipe and the vector instructions together, 5 heads x 32760,
+// 128 clusters, 53% of the keys kept, d = 128: forward 1.56 to 1.84 ms (0.79 to 0.93
+// PFLOP/s; matrix pipe 51% busy, vector 51%; the inference attention, which sums the
+// rounded weights with the matrix product, 1.54 to 1.57), dQ 2.15 to 2.19 ms (1.0
+// PFLOP/s of its three products; 57% and 45%).  dQ dense, 3 heads x 32760: 2.18 ms,
+// 1.14 PFLOP/s.
+//
+// ds is rounded to bf16 for its product with K, like the weights for theirs.  A
+// row's ds sum to zero without dropout, so dQ is a difference of larger sums and
+// keeps more of that rounding than dK and dV do: a relative error of 3.2e-3 in the
+// norm where dQ rounded once from fp32 has 1.7e-3.  A second bf16 term of ds would
+// take a third more matrix products than the 24 of a tile's half; taking the
+// rounding's row sum times the mean selected key out again leaves 2.8e-3.
 #include "attention_slots.h"
 #include "attention_tile.h"
 #include "common.h"
@@ -221,7 +235,8 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
         for (int e = 0; e < 16; ++e) acc[db][e] *= alpha;
       m_run = m_new;
     }
-    const float neg_m = -m_run;
+    // no logit above -inf so far: weights of 0, where inf - inf would be NaN
+    const float neg_m = m_run == -INFINITY ? 0.0f : -m_run;
     bf16x8 pk[2][2];
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     auto weights = [&](int kb) {
@@ -385,6 +400,9 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
                      pack_bf16(acc[db][4 * i + 2] * f, acc[db][4 * i + 3] * f));
 }
 
+// d = 128: the tiles' LDS leaves a CU one block.  d = 64: two, within 128 registers (dQ
+// spills 9 of them): 8 heads x 19721, 18% kept, 289 us for 328 with one block of 170
+// registers.  Dropout's words would spill far more: 8 x 8000 504 us for one block's 317.
 template <int D, bool GRAD, bool DROP>
 __global__ __launch_bounds__(kNW * 64)
 __attribute__((amdgpu_waves_per_eu(D == 64 && !DROP ? 4 : 2))) void queries_kernel(TrainArgs a, int total_items,

@@ -175,6 +175,39 @@ def test_unselected_rows_are_not_read_into_results(dtype, d):
         assert torch.equal(got[a], want[a]), a
 
 
+@pytest.mark.parametrize("heads,n,d,dtype", [(3, 2185, 128, "bf16"), (2, 600, 64, "bf16"),
+                                             (40, 700, 64, "bf16"), (3, 2185, 128, "f32")])
+@pytest.mark.parametrize("first_half", [False, True])
+@pytest.mark.parametrize("p", [0.0, 0.1])
+def test_logits_of_minus_infinity_have_no_weight(heads, n, d, dtype, first_half, p):
+    """2^70 times -2^70 leaves fp32: the logits of one half of the keys are -inf, those
+    of the other half have a factor of zero there.  Whole tiles and parts of a list,
+    and the lists of clusters 2 and 3, hold nothing else.  The result is that of sets
+    without these keys, for which the products are in range."""
+    x = R.make(heads, n, d, dtype, 6, 0.7, 13)
+    half = n // 2
+    lost = torch.arange(n, device="cuda") < half
+    lost = lost if first_half else ~lost
+    x["q"][:, :, 0] = 2.0 ** 70
+    x["k"][:, :, 0] = torch.where(lost, -2.0 ** 70, 0.0).to(x["k"].dtype)
+    rest = dict(x, sel_idx=x["sel_idx"].clone(), sel_counts=x["sel_counts"].clone())
+    for h in range(heads):
+        for c in range(6):
+            keys = x["sel_idx"][h, c, :int(x["sel_counts"][h, c])].long()
+            if c in (2, 3):
+                keys = keys[lost[keys]]
+                x["sel_counts"][h, c] = len(keys)
+                x["sel_idx"][h, c, :len(keys)] = keys.int()
+            keys = keys[~lost[keys]]
+            rest["sel_counts"][h, c] = len(keys)
+            rest["sel_idx"][h, c, :len(keys)] = keys.int()
+    got = run(x, p, (6, 7))
+    for h in range(heads) if heads < 10 else (0, heads - 1):
+        y = {a: t[h:h + 1] for a, t in rest.items() if a != "dims"}
+        y["dims"] = (1, n, d, 6, dtype)
+        check(y, {a: t[h:h + 1] for a, t in got.items()}, p, (6, 7), head=h)
+
+
 def test_repeats_bit_for_bit_and_across_workspaces():
     x = R.make(3, 1500, 128, "bf16", 24, 0.5, 2)
     first = run(x, 0.1, (1, 2))
@@ -253,6 +286,32 @@ def test_other_stream():
     assert torch.equal(o[:], want["o"]) and torch.equal(lse, want["lse"])
     for got, name in zip(grads, ("dq", "dk", "dv")):
         assert torch.equal(got, want[name]), name
+
+
+def test_two_calls_at_once():
+    """Two objects on two streams, several times over, against each alone."""
+    xs = [R.make(2, 1800, 128, "bf16", 20, 0.5, 11), R.make(3, 1100, 64, "f32", 9, 0.4, 12)]
+    want = [run(x, 0.1, (3, 4)) for x in xs]
+    attentions = [TrainingAttention(*x["dims"][:4], x["dims"][4]) for x in xs]
+    outs = [(a.outputs(), a.gradients()) for a in attentions]
+    for (o, lse), grads in outs:
+        for t in (o, lse, *grads):
+            t.zero_()
+    rngs = [rng_of(3, 4) for _ in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for x, a, (out, grads), rng, s in zip(xs, attentions, outs, rngs, streams):
+            qkv = (x["q"], x["k"], x["v"])
+            a.forward(*qkv, *R.sets(x), 0.0, 0.1, rng, into=out, stream=s)
+            a.backward(*qkv, *out, x["d_o"], *R.sets(x), 0.0, 0.1, rng, into=grads, stream=s)
+    torch.cuda.synchronize()
+    for x, w, ((o, lse), (dq, dk, dv)) in zip(xs, want, outs):
+        held = R.allowed(x)[1]
+        rows = torch.from_numpy(held).cuda()
+        for name, t in dict(o=o, lse=lse, dq=dq).items():
+            assert torch.equal(t[rows], w[name][rows]), name
+        assert torch.equal(dk, w["dk"]) and torch.equal(dv, w["dv"])
 
 
 def test_captured_and_replayed_with_new_masks():
@@ -352,6 +411,26 @@ def test_partition_layer_differentiates():
     check(case, got)
     for leaf, name in zip((q, k, v), ("dq", "dk", "dv")):
         assert torch.equal(leaf.grad, got[name]), name
+
+
+def test_attention_twice_and_an_expanded_gradient():
+    """One layer's attention used twice before the backward passes; the output's
+    gradient is an expanded scalar."""
+    layer, q, k, v, iq, ik = small_layer()
+    layer.forward(q, k, v, iq, ik)
+    g = torch.ones_like(q)
+    scales = (0.0, 0.05)
+    want = []
+    for scale in scales:
+        leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+        layer.attention(*leaves, scale=scale).backward(g)
+        want.append([t.grad for t in leaves])
+    both = [[t.clone().requires_grad_() for t in (q, k, v)] for _ in scales]
+    outs = [layer.attention(*leaves, scale=scale) for leaves, scale in zip(both, scales)]
+    (outs[0].sum() + outs[1].sum()).backward()
+    for leaves, grads in zip(both, want):
+        for leaf, grad in zip(leaves, grads):
+            assert torch.equal(leaf.grad, grad)
 
 
 def test_a_new_selection_before_the_backward_is_refused():
