@@ -29,8 +29,10 @@
  *    shape (fp32 or bf16).  All other arrays are dense, row-major, with the
  *    shapes given per argument, heads outermost.
  *  - Workspace: calls that need scratch take `workspace` (256-byte aligned)
- *    of at least scope_workspace_size() bytes.  One workspace serves every
- *    call, but two calls that may run concurrently need two workspaces.
+ *    of at least scope_workspace_size() bytes, calls 6 and 7 of at least
+ *    scope_training_workspace_size().  One workspace serves every call, but
+ *    two calls that may run concurrently (replays of captured graphs among
+ *    them) need two workspaces.  Nothing in it outlives its call.
  *  - Errors: argument checks run before any GPU work and return
  *    SCOPE_ERR_INVALID_ARGUMENT (bad value), SCOPE_ERR_UNSUPPORTED (valid but
  *    outside what the kernels implement) or SCOPE_ERR_WORKSPACE; nothing is

@@ -15,12 +15,12 @@
 //
 // Bound by the matrix products it runs, which with sparse sets are more than those
 // that count: a wave computes a tile if its cluster keeps one of its 32 keys, and a
-// block takes the time of its busiest waves.  Dense (3 heads x 32760, d = 128) 3.0
-// ms, 1100 TFLOP/s.  Two blocks share a CU (d = 64: three), so that one computes
+// block takes the time of its busiest waves.  Dense (3 heads x 32760, d = 128) 3.04
+// ms, 1.08 PFLOP/s of its four products, matrix pipe 52% busy.  Two blocks share a CU (d = 64: three), so that one computes
 // where the other's waves have nothing to do or wait: blocks of 256 keys and tiles
 // of 64 queries, one block per CU, took 2.9 ms dense, but on the sparse layer's own
 // sets 5.09 for 4.79 ms (5 heads x 32760, 54% of the keys kept) and 3.38 for 3.22
-// (15%); d = 64, 8 heads x 19721, 1040 for 794 us.
+// (15%); d = 64, 8 heads x 19721, 1040 for 804 us.
 #include "attention_tile.h"
 #include "common.h"
 #include "kernels.h"

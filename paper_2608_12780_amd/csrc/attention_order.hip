@@ -3,7 +3,8 @@
 // The gradient kernel runs 32 keys of a wave against every query tile whose cluster
 // keeps one of them, so keys in token order waste what their neighbours' sets do not
 // share: on the sparse layer's own sets (5 heads x 32760 tokens, 128 clusters) 43%
-// of the products at 54% kept keys, 72% at 15%.  Keys that the same clusters keep
+// of the products at 54% kept keys, 72% at 15% (dK and dV take 5.44 ms for 4.79 in
+// the order below, 4.88 for 3.22).  Keys that the same clusters keep
 // belong together.  A key's signature are its bits in 12 clusters, spread over the
 // list; keys are sorted by it, signatures in the order of the reflected Gray code,
 // where neighbours differ in one cluster.  A head uses the order where it leaves

@@ -7,10 +7,12 @@
 //   dq_i  = scale sum_j ds_ij k_j, dk_j = scale sum_i ds_ij q_i,
 //   dv_j  = sum_i p_ij m_ij do_i
 // The gradients recompute p from lse, so nothing of size n^2 is stored.  dq runs
-// over a cluster's gathered keys like the forward, one wave per 32 queries; dk
-// and dv run over the clusters' queries, one wave per 32 keys, with a bit for
-// each (cluster, key), so every sum has one owner and a fixed order: no atomics,
-// the same bits on every run.
+// over a cluster's gathered keys like the forward, a wave per 32 queries (fp32: 16);
+// dk and dv run over the clusters' queries, a wave per 32 keys (fp32: 16), with a
+// bit for each (cluster, key), so every sum has one owner and a fixed order: no
+// atomics on results, the same bits on every run.  S and dP are computed for either
+// side, seven products where five are needed; one pass for all three would add dq
+// from every block of keys, in an order that varies or through memory of its own.
 #include <math.h>
 
 #include "attention_slots.h"
@@ -28,8 +30,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // fp32 inputs: fp32 matrix products, 16 x 16 results from 4 channels (or rows) per
 // instruction, so that inputs, weights and ds are not rounded.  They run at a
 // sixteenth of the bf16 rate and need little bandwidth: a wave owns 16 queries
-// (or keys), four a block, which leaves registers for three waves per SIMD to cover
-// the staging of tiles, and short work items for an even load.
+// (or keys), four waves a block, which makes short work items for an even load and
+// leaves two blocks a CU (d = 64: four) to cover the staging of tiles.  Bound by the
+// matrix pipe, 73 to 76% busy: 4 heads x 6417 tokens, d = 128, 53% of the keys kept,
+// dq 740 to 766 us (88 TFLOP/s of the products that count), dk and dv 1270 to 1300.
 constexpr int kThreads = 256;
 constexpr int kRows = 16 * kThreads / 64;   // rows (queries or keys) per block
 constexpr int kTile = 32;                   // gathered rows per step
@@ -710,7 +714,9 @@ hipError_t join_parts(size_t count, int splits, float scale_k, float scale_v, co
 // Parts that each block's tiles are cut into, with fp32 sums of their own that a
 // second kernel adds: as many, up to 16 of `least` tiles or more, as make the
 // launch's rounds shortest; a part costs about 4% of a block more (its start, its
-// sums).  `resident`: the blocks that the chip holds at once.
+// sums).  `resident`: the blocks that the chip holds at once.  3 heads x 2185 tokens,
+// d = 128: dq in parts 43 us and their join 5, dk and dv 47 and 10; the largest cases,
+// whose blocks fill the chip many times, stay whole or take two parts.
 int parts_of(long long blocks, long long tiles, int least, int resident) {
   constexpr int kMost = 16;
   int best = 1;

@@ -307,8 +307,6 @@ struct TrainCall {
 constexpr int kTrainMaskKeys = 256;  // keys of a mask row
 constexpr int kTrainKeyBlock = 128;  // keys of a block of dK and dV (attention_keys.hip)
 constexpr int kTrainKeyTile = 32;    // queries of its tiles
-// Parts that the query tiles are cut into for dK and dV, `keys` keys per block.
-int train_key_splits(int heads, int n, int keys, int tiles);
 // The forward into `o` (grad false), or dQ from a.stats (grad true).
 // listed: the work slots are there already.
 hipError_t train_queries(int d, bool grad, const TrainArgs &a, int heads, bool listed,

@@ -21,7 +21,8 @@ class TrainingAttention:
     """Attention over given clusters and key sets with the rows' log-sum-exp
     (call 6) and its gradients (call 7), on buffers allocated once.  `dropout`
     drops attention probabilities; `rng` is an int64 tensor (seed, offset) on
-    the GPU, the same in backward as in forward."""
+    the GPU, the same in backward as in forward.  Calls that may run at once
+    (streams, replays of captured graphs) need an object each."""
 
     def __init__(self, heads, n, d, c_q, dtype="bf16", device="cuda"):
         self.heads, self.n, self.d, self.c_q = int(heads), int(n), int(d), int(c_q)
@@ -149,7 +150,9 @@ class _Differentiable:
     def attention(self, q, k, v, scale=0.0, dropout=0.0, rng=None):
         """Attention over the clusters and key sets that the layer holds (calls
         6 and 7), differentiable in q, k and v.  They must not be rewritten (a
-        new clustering or selection) before the backward pass has run."""
+        new clustering or selection) before the backward pass has run.  To
+        capture a graph, call `training_attention`'s forward and backward:
+        they allocate nothing when given their outputs."""
         return _AttentionFunction.apply(
             q, k, v, self, (self.offsets, self.perm, self.sel_counts, self.sel_idx), float(scale),
             float(dropout), rng)
