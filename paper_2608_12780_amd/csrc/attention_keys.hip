@@ -32,7 +32,6 @@ namespace scope {
 namespace {
 
 constexpr int kList = 1024;        // active tiles listed at a time
-static_assert(kOrderSlots == 64, "a slot per lane");
 static_assert(kTrainKeyTile == 32, "a tile is one matrix product's rows");
 
 constexpr int kWaves = kTrainKeyBlock / 32;  // a wave owns 32 keys
@@ -64,13 +63,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 && !DROP ? 3 : 2))) void grad_keys_ke
   TileReader<D> at(lane);
   bf16x8 kf[D / 16], vf[VLDS ? 1 : D / 16];
   const int own_row = 32 * w + l32, place = kb * kTrainKeyBlock + own_row;
-  // by position where that leaves 3% fewer (wave, tile) pairs
-  bool by_position = false;
-  if (a.order.cost) {
-    const unsigned long long *cost = a.order.cost + (static_cast<size_t>(h) * kOrderSlots + lane) * 2;
-    const unsigned long long by_key = wave_sum(cost[0]);
-    by_position = wave_sum(cost[1]) + by_key / 32 < by_key;
-  }
+  const bool by_position = keys_by_position(a.order, h, lane);
   const int key = place >= a.n ? a.n : by_position ? a.order.key[first + place] : place;
   {
     const size_t from = (first + min(key, a.n - 1)) * D;

@@ -1,6 +1,6 @@
 // An order of the keys for dK and dV.
 //
-// The gradient kernel runs 32 keys of a wave against every query tile whose cluster
+// The gradient kernels run the 32 keys of a wave (fp32: 16) against every query tile whose cluster
 // keeps one of them, so keys in token order waste what their neighbours' sets do not
 // share: on the sparse layer's own sets (5 heads x 32760 tokens, 128 clusters) 43%
 // of the products at 54% kept keys, 72% at 15% (dK and dV take 5.44 ms for 4.79 in
@@ -148,8 +148,14 @@ __global__ __launch_bounds__(256) void order_masks_kernel(TrainArgs a) {
 //                 1.09-1.11   0.99-1.06   0.95-1.02   0.94-1.01
 //   sets of runs of 128 tokens, 30% kept (the order is found and not used)
 //                 1.13-1.19   1.09-1.12   1.04-1.07   1.03-1.04
+// fp32, whose products take longer, 4 heads (up to 2048: 8), 8 to 64 clusters:
+//   tokens             1024        2048        4096        8192
+//   groups        0.93-1.02   0.75-0.97   0.68-0.91   0.62-0.68
+//   random        1.04-1.08   1.00-1.04   1.01-1.02   1.00-1.02
+//   runs          1.09-1.10   1.04-1.06   1.04-1.05   1.01-1.02
+// and 1.03 at 6417 tokens with 53% of scattered keys kept, so fp32 has the same bound.
 // Fewer than 8 clusters were not measured: such sets share most blocks of 32 keys.
-bool train_orders_keys(int n, int c_q, bool bf16) { return bf16 && n >= 8192 && c_q >= 8; }
+bool train_orders_keys(int n, int c_q) { return n >= 8192 && c_q >= 8; }
 
 // After the bins and costs have been cleared.
 hipError_t train_order(const TrainArgs &a, int heads, hipStream_t s) {

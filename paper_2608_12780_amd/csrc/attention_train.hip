@@ -16,6 +16,7 @@
 #include <math.h>
 
 #include "attention_slots.h"
+#include "attention_tile.h"
 #include "common.h"
 #include "kernels.h"
 #include "mfma.h"
@@ -299,8 +300,10 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void train_keys_kernel(Tra
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const size_t first = static_cast<size_t>(h) * a.n;
   const T at(l16, g);
-  const int j = b * kRows + 16 * w + l16;
-  const bool valid = j < a.n;
+  const bool by_position = keys_by_position(a.order, h, lane);
+  const int place = b * kRows + 16 * w + l16;
+  const bool valid = place < a.n;
+  const int j = valid && by_position ? a.order.key[first + place] : place;
   const size_t kj = first + (valid ? j : 0);
   float4 kf[D / 16], vf[D / 16];
   load_row<D>(kf, static_cast<const float *>(a.k) + kj * D, valid, g);
@@ -316,7 +319,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void train_keys_kernel(Tra
   // the block's two words of each cluster, 16 bits a wave
   constexpr int WORDS = kTrainMaskKeys / 32, SHARE = kTrainMaskKeys / kRows;
   static_assert(kRows == 64, "two words per block");
-  const uint32_t *masks = a.masks + (static_cast<size_t>(h) * ((a.n + kTrainMaskKeys - 1) / kTrainMaskKeys) + b / SHARE) * a.c_q * WORDS +
+  const uint32_t *masks = (by_position ? a.order.masks : a.masks) + (static_cast<size_t>(h) * ((a.n + kTrainMaskKeys - 1) / kTrainMaskKeys) + b / SHARE) * a.c_q * WORDS +
                           2 * (b % SHARE);
 
   const uint32_t bytes = static_cast<uint32_t>(a.n) * (4 * D);
@@ -830,8 +833,8 @@ hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
   a.items = c.tiles;
   a.items_per_head = train_items_per_head(a.n, a.c_q, sizeof(T) == 2 ? kTrainKeyTile : kTile);
   a.splits = key_splits(c.heads, a.n, D, sizeof(T) == 2, a.c_q);
+  if (a.order.cost) TRAIN_TRY(train_order(a, c.heads, s));
   if constexpr (sizeof(T) == 2) {
-    if (a.order.cost) TRAIN_TRY(train_order(a, c.heads, s));
     TRAIN_TRY(train_keys(D, a, c.heads, dk, dv, s));
   } else {
     const dim3 grid(static_cast<unsigned>(c.heads) * a.splits * ((a.n + kRows - 1) / kRows));
@@ -870,7 +873,7 @@ size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, 
   char *stats = take(H * (n + 1) * 2 * sizeof(float));
   const size_t mask_bytes = H * ((n + kTrainMaskKeys - 1) / kTrainMaskKeys) * c_q * (kTrainMaskKeys / 8);
   char *masks = take(mask_bytes);
-  const size_t ordered_keys = train_orders_keys(n, c_q, bf16) ? 1 : 0;
+  const size_t ordered_keys = train_orders_keys(n, c_q) ? 1 : 0;
   char *bin = take(ordered_keys * H * n * sizeof(uint16_t));
   char *start = take(ordered_keys * H * kOrderBins * sizeof(uint32_t));
   char *key = take(ordered_keys * H * n * sizeof(int32_t));

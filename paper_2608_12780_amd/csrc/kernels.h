@@ -311,7 +311,7 @@ constexpr int kTrainKeyTile = 32;    // queries of its tiles
 // listed: the work slots are there already.
 hipError_t train_queries(int d, bool grad, const TrainArgs &a, int heads, bool listed,
                          const AttnScratch &w, uint16_t *out, hipStream_t s);
-bool train_orders_keys(int n, int c_q, bool bf16);
+bool train_orders_keys(int n, int c_q);
 hipError_t train_order(const TrainArgs &a, int heads, hipStream_t s);
 hipError_t train_keys(int d, const TrainArgs &a, int heads, uint16_t *dk, uint16_t *dv, hipStream_t s);
 int train_items_per_head(int n, int c_q, int rows);

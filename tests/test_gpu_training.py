@@ -107,6 +107,8 @@ LARGE = [
     (2, 16400, 128, "bf16", 60, 0.3, "uncovered", 0.0),
     (1, 8400, 128, "f32", 33, 0.3, "uncovered", 0.1),
     (9, 1300, 64, "f32", 50, 0.3, "", 0.0),
+    (2, 8192, 64, "f32", 24, 0.2, "", 0.1),
+    (1, 8255, 128, "f32", 9, 0.4, "empty", 0.0),
     (40, 700, 128, "bf16", 20, 0.5, "", 0.0),      # slots shared by two clusters
 ]
 
@@ -123,9 +125,10 @@ def test_large(heads, n, d, dtype, c_q, keep, pattern, p):
         check(y, {a: t[h:h + 1] for a, t in got.items()}, p, (21, n), head=h)
 
 
-def test_large_repeats_bit_for_bit():
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_repeats_bit_for_bit(dtype):
     """The keys' order is found with counters whose order varies; the results do not."""
-    x = R.make(2, 9000, 128, "bf16", 32, 0.3, 6)
+    x = R.make(2, 9000, 128, dtype, 32, 0.3, 6)
     first = run(x)
     for _ in range(3):
         again = run(x)
