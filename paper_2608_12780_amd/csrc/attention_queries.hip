@@ -8,7 +8,7 @@
 // while the tile before is computed.  The gradient recomputes p from the row's
 // log-sum-exp and needs no second pass over the keys:
 //   S^T = K_tile . Q^T, dP^T = V_tile . dO^T, ds = p (m dP - D),
-//   dQ^T += K_tile^T . ds^T
+//   dQ^T += K_tile^T . ds^T    (ds in two terms, below)
 // The forward's normaliser sums the weights in fp32 before they are rounded to bf16
 // for the product with V (the inference attention sums the rounded ones): lse is an
 // fp32 result, and 2 to 3 keys of weight would leave rounded sums 2^-9 off.
@@ -16,16 +16,16 @@
 // Bound by the matrix pipe and the vector instructions together, 5 heads x 32760,
 // 128 clusters, 53% of the keys kept, d = 128: forward 1.56 to 1.84 ms (0.79 to 0.93
 // PFLOP/s; matrix pipe 51% busy, vector 51%; the inference attention, which sums the
-// rounded weights with the matrix product, 1.54 to 1.57), dQ 2.15 to 2.19 ms (1.0
-// PFLOP/s of its three products; 57% and 45%).  dQ dense, 3 heads x 32760: 2.18 ms,
-// 1.14 PFLOP/s.
+// rounded weights with the matrix product, 1.54 to 1.57), dQ 2.6 to 2.9 ms (1.0 to
+// 1.1 PFLOP/s of its four products; 60% and 49%).  dQ dense, 3 heads x 32760: 2.7 to
+// 2.8 ms, 1.2 PFLOP/s.
 //
-// ds is rounded to bf16 for its product with K, like the weights for theirs.  A
-// row's ds sum to zero without dropout, so dQ is a difference of larger sums and
-// keeps more of that rounding than dK and dV do: a relative error of 3.2e-3 in the
-// norm where dQ rounded once from fp32 has 1.7e-3.  A second bf16 term of ds would
-// take a third more matrix products than the 24 of a tile's half; taking the
-// rounding's row sum times the mean selected key out again leaves 2.8e-3.
+// dQ's ds are two bf16 terms, the second what rounding the first left: a row's ds
+// sum to zero, so dQ is a difference of larger sums and keeps more of their rounding
+// than dK and dV do.  With one term it was off by 3.2e-3 in the norm where a dQ
+// computed in fp32 and rounded once has 1.7e-3; with two it has 1.7e-3.  They take a
+// third more matrix products, the whole backward pass 3% (d = 64) to 11% (dense) more
+// time.  Taking the rounding's row sum times the mean key out again left 2.8e-3.
 #include "attention_slots.h"
 #include "attention_tile.h"
 #include "common.h"
@@ -191,6 +191,17 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
       for (int db = 0; db < D / 32; ++db)
         acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.columns(tile + 16 * s2 * D, db), p[s2], acc[db], 0, 0, 0);
   };
+  // of two terms
+  auto add2 = [&](const uint16_t *tile, const bf16x8 (&p)[2], const bf16x8 (&rest)[2]) {
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        const bf16x8 k = at.columns(tile + 16 * s2 * D, db);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, p[s2], acc[db], 0, 0, 0);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, rest[s2], acc[db], 0, 0, 0);
+      }
+  };
 
   auto forward_tile = [&](int tile, const uint16_t *kt, const uint16_t *vt, typename T::K &kn, typename T::V &vn,
                           const Idx &ix) {
@@ -279,7 +290,7 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
   auto grad_tile = [&](int tile, const uint16_t *kt, const uint16_t *vt) {
     f32x16 s[2], dp[2];
     float p[2][16];
-    bf16x8 dsk[2][2];
+    bf16x8 dsk[2][2], rest[2][2];
     auto weights = [&](int kb) {  // p, negative where dropped, beside dP^T
       f32x16 x;
 #pragma unroll
@@ -311,6 +322,19 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
       }
       dsk[kb][0] = pack8(ds);
       dsk[kb][1] = pack8(ds + 8);
+      // what the rounding left
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint4 u = __builtin_bit_cast(uint4, dsk[kb][i]);
+        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          ds[8 * i + 2 * j] -= __uint_as_float(x[j] << 16);
+          ds[8 * i + 2 * j + 1] -= __uint_as_float(x[j] & 0xFFFF0000u);
+        }
+      }
+      rest[kb][0] = pack8(ds);
+      rest[kb][1] = pack8(ds + 8);
     };
     s[0] = scores(kt, 0);
     interleave<D / 16, 1, 0>();
@@ -320,17 +344,27 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
     gradient(0);
     s[1] = scores(kt, 1);
     interleave<D / 16, 1, D == 128 ? 5 : 10>();
-    asm volatile("" : "+v"(s[1]), "+v"(dsk[0][0]), "+v"(dsk[0][1]), "+v"(at.row_at));
+    asm volatile("" : "+v"(s[1]), "+v"(dsk[0][0]), "+v"(dsk[0][1]), "+v"(rest[0][0]), "+v"(rest[0][1]), "+v"(at.row_at));
+    // d = 64 has registers for one block of keys' ds (kept over the next block's
+    // weights they spilled 32 more: dQ of 8 heads x 19721 568 us for 351)
+    if constexpr (D == 64) {
+      add2(kt, dsk[0], rest[0]);
+      interleave<D / 8, 1, 0>();
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(acc[db]));
+    }
     if (tile * kBN + 64 > r) cut(s[1], tile * kBN + 32);
     weights(1);
     gradient(1);
-    add(kt, dsk[0]);
-    interleave<D / 16, 2, D == 128 ? 5 : 10>();
+    if constexpr (D == 128) {
+      add2(kt, dsk[0], rest[0]);
+      interleave<D / 8, 1, 4>();
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(acc[db]));
-    asm volatile("" : "+v"(dsk[1][0]), "+v"(dsk[1][1]), "+v"(at.col_at));
-    add(kt + 32 * D, dsk[1]);
-    interleave<D / 16, 2, 0>();
+      for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(acc[db]));
+    }
+    asm volatile("" : "+v"(dsk[1][0]), "+v"(dsk[1][1]), "+v"(rest[1][0]), "+v"(rest[1][1]), "+v"(at.col_at));
+    add2(kt + 32 * D, dsk[1], rest[1]);
+    interleave<D / 8, 1, 0>();
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(acc[db]));
     asm volatile("" : "+v"(at.row_at), "+v"(at.col_at));
@@ -401,8 +435,8 @@ __device__ __forceinline__ void queries_body(const TrainArgs &a, int h, const in
 }
 
 // d = 128: the tiles' LDS leaves a CU one block.  d = 64: two, within 128 registers (dQ
-// spills 9 of them): 8 heads x 19721, 18% kept, 289 us for 328 with one block of 170
-// registers.  Dropout's words would spill far more: 8 x 8000 504 us for one block's 317.
+// spills 9 of them): 8 heads x 19721, 18% kept, 335 to 351 us for 418 with one block.
+// Dropout's words would spill far more: 8 x 8000 504 us for 317 (ds in one term).
 template <int D, bool GRAD, bool DROP>
 __global__ __launch_bounds__(kNW * 64)
 __attribute__((amdgpu_waves_per_eu(D == 64 && !DROP ? 4 : 2))) void queries_kernel(TrainArgs a, int total_items,

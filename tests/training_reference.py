@@ -126,7 +126,8 @@ def reference(x, p=0.0, rng=(0, 0), scale=None, o=None, lse=None, head=0):
              for the sum, and half a step of the output
       ds     p's error times |dp - D|, p times the errors of the sums dp and D,
              b for ds as an operand
-      dq, dk sums of the ds' errors, (terms + 8) u for the sum, half a step."""
+      dq, dk sums of the ds' errors, (terms + 8) u for the sum, half a step; dq's
+             ds are two operands, the second the first's rounding error, so b^2"""
     H, n, d, _, dtype = x["dims"]
     dev = x["q"].device
     b, half = (HALF_STEP["bf16"], HALF_STEP["bf16"]) if dtype == "bf16" else (0.0, U)
@@ -164,9 +165,10 @@ def reference(x, p=0.0, rng=(0, 0), scale=None, o=None, lse=None, head=0):
         D, e_D = torch.where(live, D, 0.0), torch.where(live, e_D, 0.0)
         ds = prob * (dp - D)
         e_ds = ds.abs() * (rel + b) + prob * (e_dp + e_D + 4 * U * (dp.abs() + D.abs()))
+        e_dq = ds.abs() * (rel + b * b) + prob * (e_dp + e_D + 4 * U * (dp.abs() + D.abs()))
         per_key = ok.sum(1).double()
         val["dq"] = scale * mm(ds, k)
-        tol["dq"] = scale * mm(e_ds + (terms + 8)[..., None] * U * ds.abs(), k.abs()) + half * val["dq"].abs()
+        tol["dq"] = scale * mm(e_dq + (terms + 8)[..., None] * U * ds.abs(), k.abs()) + half * val["dq"].abs()
         val["dk"] = scale * mm(T(ds), q)
         tol["dk"] = scale * mm(T(e_ds) + (per_key + 8)[..., None] * U * T(ds.abs()), q.abs()) + half * val["dk"].abs()
         pm = prob * m
