@@ -404,8 +404,8 @@ int32_t scope_sparse_attention_train(const scope_shape *shape, const void *q,
  *   dQ_i = scale sum_j ds_ij k_j, dK_j = scale sum_i ds_ij q_i,
  *   dV_j = sum_i p_ij m_ij d_o_i,
  * j over S_c and i over the queries whose cluster keeps j.  Types as call 6:
- * for bf16 inputs p and ds enter the matrix products rounded to bf16, every sum
- * is fp32.  dK and dV are written for every key (0 where no cluster keeps it),
+ * for bf16 inputs p, and ds for dK, enter the matrix products rounded to bf16, ds
+ * for dQ as two bf16 terms; every sum is fp32.  dK and dV are written for every key (0 where no cluster keeps it),
  * dQ for every query in a cluster (0 where its cluster keeps no key); rows of
  * queries in no cluster are left as they were and give no gradient.  Bad sets
  * cannot fault: a set that is not strictly ascending in [0, n) sets bit 3 of
