@@ -405,9 +405,10 @@ int32_t scope_sparse_attention_train(const scope_shape *shape, const void *q,
  *   dV_j = sum_i p_ij m_ij d_o_i,
  * j over S_c and i over the queries whose cluster keeps j.  Types as call 6:
  * for bf16 inputs p, and ds for dK, enter the matrix products rounded to bf16, ds
- * for dQ as two bf16 terms; every sum is fp32.  dK and dV are written for every key (0 where no cluster keeps it),
- * dQ for every query in a cluster (0 where its cluster keeps no key); rows of
- * queries in no cluster are left as they were and give no gradient.  Bad sets
+ * for dQ as two bf16 terms; every sum is fp32.  dK and dV are written for every
+ * key (0 where no cluster keeps it), dQ for every query in a cluster (0 where its
+ * cluster keeps no key); rows of queries in no cluster are left as they were and
+ * give no gradient.  Bad sets
  * cannot fault: a set that is not strictly ascending in [0, n) sets bit 3 of
  * dev_status (may be NULL) and its gradients are unspecified.  Rows of K and V
  * that no set holds are not read into any result; a non-finite row of Q or d_o
