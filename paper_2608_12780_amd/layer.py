@@ -12,9 +12,17 @@ and residual, and ScopeLayer.forward_train runs the layer with both.
 """
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import binding as B
+
+
+def _allocating_on(stream):
+    """Where a call allocates what it runs `stream` on: memory that torch's
+    allocator gives out for another stream may still be in use there."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 class TrainingAttention:
@@ -50,7 +58,8 @@ class TrainingAttention:
                 rng=None, into=None, stream=None):
         """Returns (out, lse): `into`, or the buffers this object holds."""
         if into is None:
-            self._out = into = self._out or self.outputs()
+            with _allocating_on(stream):
+                self._out = into = self._out or self.outputs()
         B.scope_sparse_attention_train(self.shape, q, k, v, self.c_q, offsets, perm, sel_counts,
                                        sel_idx, scale, dropout, rng, *into, self.workspace, stream)
         return into
@@ -59,7 +68,8 @@ class TrainingAttention:
                  dropout=0.0, rng=None, into=None, stream=None):
         """Returns (dq, dk, dv): `into`, or the buffers this object holds."""
         if into is None:
-            self._grads = into = self._grads or self.gradients()
+            with _allocating_on(stream):
+                self._grads = into = self._grads or self.gradients()
         B.scope_sparse_attention_backward(self.shape, q, k, v, out, lse, d_out, self.c_q, offsets,
                                           perm, sel_counts, sel_idx, scale, dropout, rng, *into,
                                           self.workspace, self.status, stream)
@@ -124,7 +134,10 @@ def dropout(x, p, rng, residual=None, out=None, stream=None):
     if out is None and stream is None and torch.is_grad_enabled() and (
             x.requires_grad or residual is not None and residual.requires_grad):
         return _DropoutFunction.apply(x, residual, p, rng)
-    y = torch.empty_like(x) if out is None else out
+    y = out
+    if y is None:
+        with _allocating_on(stream):
+            y = torch.empty_like(x)
     B.scope_dropout(x, residual, p, rng, y, stream)
     return y
 

@@ -1,0 +1,66 @@
+"""Calls of the training operators that their documentation allows, in the ways
+programs make them: buffers that a call allocates, streams, autograd's gradients
+and shapes."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+from paper_2608_12780_amd import binding as B  # noqa: E402
+from paper_2608_12780_amd.layer import TrainingAttention, dropout  # noqa: E402
+
+import gpu_harness as G  # noqa: E402
+import training_reference as R  # noqa: E402
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.lib()
+
+
+def rng_of(seed, offset):
+    return torch.tensor([seed, offset], dtype=torch.int64, device="cuda")
+
+
+def freed_block(like):
+    """The address of a block that the current stream's pool has just got back;
+    work queued on that stream could still be using it."""
+    t = torch.empty_like(like)
+    at = t.data_ptr()
+    del t
+    assert torch.empty_like(like).data_ptr() == at  # what an allocation here would get
+    return at
+
+
+def test_dropout_allocates_on_the_stream_it_runs_on():
+    x = torch.randn(3_000_001, device="cuda")
+    want = dropout(x, 0.2, rng_of(1, 2))
+    rng, s = rng_of(1, 2), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    at = freed_block(x)
+    y = dropout(x, 0.2, rng, stream=s)
+    s.synchronize()
+    assert y.data_ptr() != at
+    assert torch.equal(y, want)
+
+
+def test_held_buffers_are_allocated_on_the_stream_of_their_first_call():
+    x = R.make(2, 3001, 64, "bf16", 5, 0.5, 3)
+    a = TrainingAttention(2, 3001, 64, 5, "bf16")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    qkv = (x["q"], x["k"], x["v"])
+    at = freed_block(x["q"])
+    o, lse = a.forward(*qkv, *R.sets(x), stream=s)
+    assert o.data_ptr() != at
+    at = freed_block(x["q"])
+    grads = a.backward(*qkv, o, lse, x["d_o"], *R.sets(x), stream=s)
+    s.synchronize()
+    assert at not in [t.data_ptr() for t in grads]
+    want = TrainingAttention(2, 3001, 64, 5, "bf16")
+    out = want.forward(*qkv, *R.sets(x))
+    for got, ref in zip((o, lse, *grads), (*out, *want.backward(*qkv, *out, x["d_o"], *R.sets(x)))):
+        assert torch.equal(got, ref)
