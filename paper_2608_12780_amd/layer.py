@@ -127,13 +127,18 @@ class _DropoutFunction(torch.autograd.Function):
 
 def dropout(x, p, rng, residual=None, out=None, stream=None):
     """x / (1 - p) where kept, else 0, plus `residual` (call 8), into `out` or a
-    new tensor; differentiable in x and residual where neither out nor stream
-    is given.  `rng` is an int64 tensor (seed, offset) on the GPU."""
+    new tensor; differentiable in x and residual, except into `out`, which is
+    refused where a gradient is asked for.  `rng` is an int64 tensor (seed,
+    offset) on the GPU."""
     if residual is not None and residual.shape != x.shape:
         raise ValueError(f"residual is {tuple(residual.shape)}, x {tuple(x.shape)}")
-    if out is None and stream is None and torch.is_grad_enabled() and (
-            x.requires_grad or residual is not None and residual.requires_grad):
-        return _DropoutFunction.apply(x, residual, p, rng)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad
+                                       for t in (x, residual, out)):
+        if out is not None:
+            raise ValueError("dropout into `out` is not differentiable: leave `out` away, or call "
+                             "it under torch.no_grad()")
+        with _allocating_on(stream):  # the function runs on the current stream
+            return _DropoutFunction.apply(x, residual, p, rng)
     y = out
     if y is None:
         with _allocating_on(stream):

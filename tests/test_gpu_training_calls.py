@@ -64,3 +64,34 @@ def test_held_buffers_are_allocated_on_the_stream_of_their_first_call():
     out = want.forward(*qkv, *R.sets(x))
     for got, ref in zip((o, lse, *grads), (*out, *want.backward(*qkv, *out, x["d_o"], *R.sets(x)))):
         assert torch.equal(got, ref)
+
+
+@pytest.mark.parametrize("of_residual", [False, True])
+def test_dropout_on_a_stream_is_differentiable(of_residual):
+    x, res = torch.randn(2, 1001, device="cuda").unbind()
+    leaf = (res if of_residual else x).clone().requires_grad_()
+    args = (x, leaf) if of_residual else (leaf, res)
+    rng, s = rng_of(4, 5), torch.cuda.Stream()
+    g = torch.randn_like(x)
+    s.wait_stream(torch.cuda.current_stream())
+    y = dropout(args[0], 0.3, rng, residual=args[1], stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    y.backward(g)
+    keep = torch.from_numpy(R.keep_elements(1001, 0.3, 4, 5)).cuda()
+    factor = 65536.0 / (65536 - R.threshold(0.3))
+    assert torch.equal(y, torch.where(keep, x * factor, 0.0) + res)
+    assert torch.equal(leaf.grad, g if of_residual else torch.where(keep, g * factor, 0.0))
+
+
+def test_dropout_into_a_buffer_refuses_to_lose_a_gradient():
+    x, out = torch.randn(2, 100, device="cuda").unbind()
+    leaf = x.clone().requires_grad_()
+    for kw in (dict(), dict(residual=x), dict(stream=torch.cuda.current_stream())):
+        with pytest.raises(ValueError, match="not differentiable"):
+            dropout(leaf, 0.1, rng_of(1, 1), out=out, **kw)
+    with pytest.raises(ValueError, match="not differentiable"):
+        dropout(x, 0.1, rng_of(1, 1), residual=leaf, out=out)
+    want = dropout(x, 0.1, rng_of(1, 1))
+    with torch.no_grad():
+        assert torch.equal(dropout(leaf, 0.1, rng_of(1, 1), out=out), want)
+    assert torch.equal(dropout(x, 0.1, rng_of(1, 1), out=out), want)
