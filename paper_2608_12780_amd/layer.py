@@ -97,9 +97,12 @@ class _AttentionFunction(torch.autograd.Function):
             raise RuntimeError("the layer's clusters or key sets changed between this attention "
                                "and its backward pass")
         attention = ctx.owner.training_attention()
-        grads = attention.backward(q, k, v, out, lse, d_out.contiguous(), offsets, perm,
-                                   sel_counts, sel_idx, ctx.scale, ctx.dropout,
-                                   rng[0] if rng else None, into=attention.gradients())
+        d_out = d_out.contiguous()
+        if d_out.data_ptr() % 16:  # a piece of another tensor's gradient
+            d_out = d_out.clone()
+        grads = attention.backward(q, k, v, out, lse, d_out, offsets, perm, sel_counts, sel_idx,
+                                   ctx.scale, ctx.dropout, rng[0] if rng else None,
+                                   into=attention.gradients())
         return (*grads, None, None, None, None, None)
 
 

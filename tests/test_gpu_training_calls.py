@@ -8,7 +8,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from paper_2608_12780_amd import binding as B  # noqa: E402
-from paper_2608_12780_amd.layer import TrainingAttention, dropout  # noqa: E402
+from paper_2608_12780_amd.layer import DenseAttention, TrainingAttention, dropout  # noqa: E402
 
 import gpu_harness as G  # noqa: E402
 import training_reference as R  # noqa: E402
@@ -95,3 +95,35 @@ def test_dropout_into_a_buffer_refuses_to_lose_a_gradient():
     with torch.no_grad():
         assert torch.equal(dropout(leaf, 0.1, rng_of(1, 1), out=out), want)
     assert torch.equal(dropout(x, 0.1, rng_of(1, 1), out=out), want)
+
+
+def dense_case(dtype, heads=2, n=150, d=64):
+    x = R.make(heads, n, d, dtype, 1, 1.0, 6)
+    dense = DenseAttention(heads, n, d, dtype)
+    x.update({a: getattr(dense, a) for a in R.SETS})
+    return dense, x, [x[a].clone().requires_grad_() for a in "qkv"]
+
+
+def want_gradients(x):
+    """(dq, dk, dv) of the calls themselves."""
+    H, n, d, C, dtype = x["dims"]
+    a = TrainingAttention(H, n, d, C, dtype)
+    qkv = (x["q"], x["k"], x["v"])
+    return a.backward(*qkv, *a.forward(*qkv, *R.sets(x)), x["d_o"], *R.sets(x))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("before", [1, 3, 8])
+def test_gradient_of_a_piece_at_any_offset(dtype, before):
+    """The gradient behind torch.cat with a piece of odd length is a contiguous view
+    that starts off the 16 bytes that the gradient call asks for."""
+    dense, x, leaves = dense_case(dtype)
+    out = dense.attention(*leaves)
+    whole = torch.cat((torch.zeros(before, dtype=out.dtype, device="cuda"), out.flatten()))
+    seen = []
+    whole.register_hook(lambda g: seen.append(g[before:].data_ptr() % 16))
+    whole.backward(torch.cat((torch.ones(before, device="cuda").to(out.dtype),
+                              x["d_o"].flatten())))
+    assert seen == [before * out.element_size() % 16]
+    for leaf, want in zip(leaves, want_gradients(x)):
+        assert torch.equal(leaf.grad, want)
