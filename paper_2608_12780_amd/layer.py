@@ -103,6 +103,9 @@ class _AttentionFunction(torch.autograd.Function):
         grads = attention.backward(q, k, v, out, lse, d_out, offsets, perm, sel_counts, sel_idx,
                                    ctx.scale, ctx.dropout, rng[0] if rng else None,
                                    into=attention.gradients())
+        # each of its input's shape, which may name [heads][n][d] in other ways
+        grads = [g.view(x.shape) if need else None
+                 for g, x, need in zip(grads, (q, k, v), ctx.needs_input_grad)]
         return (*grads, None, None, None, None, None)
 
 
@@ -174,6 +177,11 @@ class _Differentiable:
         new clustering or selection) before the backward pass has run.  To
         capture a graph, call `training_attention`'s forward and backward:
         they allocate nothing when given their outputs."""
+        count = self.heads * self.n * self.d
+        for t, name in ((q, "q"), (k, "k"), (v, "v")):
+            if torch.is_grad_enabled() and t.requires_grad and t.numel() != count:
+                raise ValueError(f"{name} needs {count} elements for its gradient, "
+                                 f"has {t.numel()}")
         return _AttentionFunction.apply(
             q, k, v, self, (self.offsets, self.perm, self.sel_counts, self.sel_idx), float(scale),
             float(dropout), rng)

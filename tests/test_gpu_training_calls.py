@@ -127,3 +127,43 @@ def test_gradient_of_a_piece_at_any_offset(dtype, before):
     assert seen == [before * out.element_size() % 16]
     for leaf, want in zip(leaves, want_gradients(x)):
         assert torch.equal(leaf.grad, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_have_their_inputs_shapes(dtype):
+    """[heads][n][d] under other shapes, one for each input."""
+    dense, x, _ = dense_case(dtype)
+    shapes = ((1, 2, 150, 64), (300, 64), (2 * 150 * 64,))
+    leaves = [x[a].reshape(shape).clone().requires_grad_() for a, shape in zip("qkv", shapes)]
+    out = dense.attention(*leaves)
+    assert out.shape == (2, 150, 64)
+    out.backward(x["d_o"])
+    for leaf, want in zip(leaves, want_gradients(x)):
+        assert torch.equal(leaf.grad, want.view_as(leaf))
+
+
+@pytest.mark.parametrize("only", range(3))
+def test_gradients_of_some_inputs(only):
+    dense, x, leaves = dense_case("bf16")
+    for i, leaf in enumerate(leaves):
+        leaf.requires_grad_(i == only)
+    dense.attention(*leaves).backward(x["d_o"])
+    for i, (leaf, want) in enumerate(zip(leaves, want_gradients(x))):
+        assert torch.equal(leaf.grad, want) if i == only else leaf.grad is None
+
+
+def test_larger_inputs_have_no_gradient():
+    """More than heads x n x d elements: their first ones are attended to, as the
+    calls do, but a gradient of all of them is refused before anything runs."""
+    dense, x, _ = dense_case("f32")
+    with torch.no_grad():
+        want = dense.attention(x["q"], x["k"], x["v"])
+    for i, name in enumerate("qkv"):
+        args = [x[a] for a in "qkv"]
+        args[i] = torch.cat((args[i], torch.ones_like(args[i])))
+        assert torch.equal(dense.attention(*args), want)
+        args[i].requires_grad_()
+        with pytest.raises(ValueError, match=f"{name} needs 19200 elements"):
+            dense.attention(*args)
+        with torch.no_grad():
+            assert torch.equal(dense.attention(*args), want)
