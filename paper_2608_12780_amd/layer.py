@@ -30,17 +30,26 @@ class TrainingAttention:
     (call 6) and its gradients (call 7), on buffers allocated once.  `dropout`
     drops attention probabilities; `rng` is an int64 tensor (seed, offset) on
     the GPU, the same in backward as in forward.  Calls that may run at once
-    (streams, replays of captured graphs) need an object each."""
+    (streams, replays of captured graphs) need an object each.  With
+    workspace=False it holds no workspace: every call takes one from torch's
+    allocator, for the stream it runs on, and gives it back."""
 
-    def __init__(self, heads, n, d, c_q, dtype="bf16", device="cuda"):
+    def __init__(self, heads, n, d, c_q, dtype="bf16", device="cuda", workspace=True):
         self.heads, self.n, self.d, self.c_q = int(heads), int(n), int(d), int(c_q)
         self.dtype = B.BF16 if dtype == "bf16" else B.F32
         self.tdtype = torch.bfloat16 if self.dtype == B.BF16 else torch.float32
         self.shape = B.make_shape(heads, n, d, self.dtype, _dummy_ranges(self.d))
         self.device = torch.device(device)
-        self.workspace = B.alloc_training_workspace(self.shape, self.c_q, device)
+        self.workspace = (B.alloc_training_workspace(self.shape, self.c_q, device) if workspace
+                          else None)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self._out = self._grads = None
+
+    def _scratch(self, stream):
+        if self.workspace is not None:
+            return self.workspace
+        with _allocating_on(stream):
+            return B.alloc_training_workspace(self.shape, self.c_q, self.device)
 
     def _rows(self):
         return torch.empty(self.heads, self.n, self.d, dtype=self.tdtype, device=self.device)
@@ -61,7 +70,8 @@ class TrainingAttention:
             with _allocating_on(stream):
                 self._out = into = self._out or self.outputs()
         B.scope_sparse_attention_train(self.shape, q, k, v, self.c_q, offsets, perm, sel_counts,
-                                       sel_idx, scale, dropout, rng, *into, self.workspace, stream)
+                                       sel_idx, scale, dropout, rng, *into,
+                                       self._scratch(stream), stream)
         return into
 
     def backward(self, q, k, v, out, lse, d_out, offsets, perm, sel_counts, sel_idx, scale=0.0,
@@ -72,14 +82,14 @@ class TrainingAttention:
                 self._grads = into = self._grads or self.gradients()
         B.scope_sparse_attention_backward(self.shape, q, k, v, out, lse, d_out, self.c_q, offsets,
                                           perm, sel_counts, sel_idx, scale, dropout, rng, *into,
-                                          self.workspace, self.status, stream)
+                                          self._scratch(stream), self.status, stream)
         return into
 
 
 class _AttentionFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, owner, sets, scale, dropout, rng):
-        attention = owner.training_attention()
+        attention = owner.autograd_attention()
         # the mask belongs to the values that rng holds now
         rng = rng.clone() if rng is not None else None
         out, lse = attention.forward(q, k, v, *sets, scale, dropout, rng,
@@ -96,7 +106,7 @@ class _AttentionFunction(torch.autograd.Function):
         if ctx.owner.selection != ctx.selection:
             raise RuntimeError("the layer's clusters or key sets changed between this attention "
                                "and its backward pass")
-        attention = ctx.owner.training_attention()
+        attention = ctx.owner.autograd_attention()
         d_out = d_out.contiguous()
         if d_out.data_ptr() % 16:  # a piece of another tensor's gradient
             d_out = d_out.clone()
@@ -161,14 +171,27 @@ class _Differentiable:
 
     # counts what rewrites the clusters or key sets that a backward pass reads
     selection = 0
-    _training = None
+    _training = _autograd = None
+
+    def _calls(self, workspace):
+        return TrainingAttention(self.heads, self.n, self.d, self.offsets.shape[1] - 1,
+                                 "bf16" if self.dtype == B.BF16 else "f32", self.offsets.device,
+                                 workspace)
+
+    def autograd_attention(self):
+        """The training calls that `attention` makes, with a workspace for each:
+        one that the layer held would be written by calls on several streams at
+        once, and would be memory for every layer of a model."""
+        if self._autograd is None:
+            self._autograd = self._calls(workspace=False)
+        return self._autograd
 
     def training_attention(self):
-        """The training calls' buffers, made on the first use."""
+        """The training calls on buffers held by the layer, made on the first use;
+        its status is that of `attention`'s calls too."""
         if self._training is None:
-            self._training = TrainingAttention(
-                self.heads, self.n, self.d, self.offsets.shape[1] - 1,
-                "bf16" if self.dtype == B.BF16 else "f32", self.offsets.device)
+            self._training = self._calls(workspace=True)
+            self._training.status = self.autograd_attention().status
         return self._training
 
     def attention(self, q, k, v, scale=0.0, dropout=0.0, rng=None):

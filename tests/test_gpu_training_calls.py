@@ -167,3 +167,73 @@ def test_larger_inputs_have_no_gradient():
             dense.attention(*args)
         with torch.no_grad():
             assert torch.equal(dense.attention(*args), want)
+
+
+@pytest.fixture
+def workspaces(monkeypatch):
+    """(call, address, stream) of every training call's workspace."""
+    seen = []
+
+    def watch(name, at):
+        call = getattr(B, name)
+
+        def watched(*args):
+            seen.append((name[23:], args[at].data_ptr(), torch.cuda.current_stream().cuda_stream))
+            return call(*args)
+        monkeypatch.setattr(B, name, watched)
+    watch("scope_sparse_attention_train", 14)
+    watch("scope_sparse_attention_backward", 17)
+    return seen
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_layers_attention_on_two_streams(dtype, workspaces):
+    """Forward and backward passes of one layer on two streams at once, each with a
+    workspace that the other stream's calls do not write."""
+    dense, x, _ = dense_case(dtype, 3, 1500)
+    cases = [dict(x, q=x["q"] * (1 + i / 4), d_o=x["d_o"] * (1 - i / 4)) for i in range(2)]
+    want = [want_gradients(y) for y in cases]
+    del workspaces[:]
+    streams = [torch.cuda.Stream() for _ in cases]
+    leaves = [[[y[a].clone().requires_grad_() for a in "qkv"] for y in cases] for _ in range(6)]
+    dense.autograd_attention()
+    torch.cuda.synchronize()
+    for turn in leaves:
+        for s, y, own in zip(streams, cases, turn):
+            with torch.cuda.stream(s):
+                dense.attention(*own).backward(y["d_o"])
+    torch.cuda.synchronize()
+    assert len(workspaces) == 24
+    of = [{at for _, at, stream in workspaces if stream == s.cuda_stream} for s in streams]
+    assert of[0] and of[1] and not of[0] & of[1]
+    for turn in leaves:
+        for own, grads in zip(turn, want):
+            for leaf, grad in zip(own, grads):
+                assert torch.equal(leaf.grad, grad)
+
+
+def test_layers_hold_no_workspace_for_autograd():
+    """Forward and backward of several layers leave no more memory than one does."""
+    held = []
+    x = R.make(4, 2048, 64, "bf16", 1, 1.0, 6)
+    layers = [DenseAttention(4, 2048, 64, "bf16") for _ in range(3)]
+    layers[0].training_attention()
+    size = layers[0].training_attention().workspace.numel()
+    leaves = [x[a].requires_grad_() for a in "qkv"]
+    for layer in layers[1:]:
+        layer.attention(*leaves).backward(x["d_o"])
+        for leaf in leaves:
+            leaf.grad = None
+        held.append(torch.cuda.memory_allocated())
+    assert held[1] - held[0] < size / 4
+
+
+def test_status_of_autograds_calls_is_the_layers():
+    dense, x, leaves = dense_case("bf16")
+    y = dense.attention(*leaves)
+    dense.sel_idx[0, 0, 7] = 3          # not ascending
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    dense.attention(*leaves).sum().backward()
+    assert int(dense.training_attention().status.item()) == 8
+    assert int(dense.autograd_attention().status.item()) == 8
