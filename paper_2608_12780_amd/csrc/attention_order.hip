@@ -9,9 +9,11 @@
 // list; keys are sorted by it, signatures in the order of the reflected Gray code,
 // where neighbours differ in one cluster.  A head uses the order where it leaves
 // fewer (wave, tile) pairs, by 3%; where sets follow the token order it does not.
-// The gradients are the same bit for bit in any order: every key's sums have their
+// Finite gradients are the same bit for bit in any order: every key's sums have their
 // own column of the matrix products and run over the same tiles, a tile that does
-// not keep the key adding zeros.  (So the order within a signature may vary.)
+// not keep the key adding zeros.  A NaN or infinity in Q or dO makes NaN of such a
+// zero, in the keys that share a wave; so the order is the same on every run as well:
+// the sort is stable, keys of one signature ascend.
 #include "common.h"
 #include "kernels.h"
 
@@ -27,9 +29,14 @@ __device__ __forceinline__ size_t mask_row(const TrainArgs &a, int h, int block,
   return ((static_cast<size_t>(h) * ((a.n + kTrainMaskKeys - 1) / kTrainMaskKeys) + block) * a.c_q + c) * kWords;
 }
 
-// A block's keys are counted and placed through its own bins in LDS: many keys share
-// a signature (5 heads x 32760, 15% kept: 131 us with global counters alone).
-constexpr int kSortThreads = 1024, kSortKeys = 4;  // keys per thread
+// A block counts its keys by signature in LDS; its counts become the places where
+// its keys of a signature start.
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSortKeys = 4;  // keys per thread
+static_assert(kOrderKeys == kSortThreads * kSortKeys, "keys of a block");
+
+__device__ __forceinline__ uint32_t *starts_of(const TrainArgs &a, int h, int block, int blocks) {
+  return a.order.start + (static_cast<size_t>(h) * blocks + block) * kOrderBins;
+}
 
 __global__ __launch_bounds__(kSortThreads) void order_count_kernel(TrainArgs a) {
   __shared__ uint32_t count[kOrderBins];
@@ -55,53 +62,92 @@ __global__ __launch_bounds__(kSortThreads) void order_count_kernel(TrainArgs a) 
     atomicAdd(&count[bin], 1u);
   }
   __syncthreads();
-  for (int i = t; i < kOrderBins; i += kSortThreads)
-    if (count[i]) atomicAdd(&a.order.start[static_cast<size_t>(h) * kOrderBins + i], count[i]);
+  uint32_t *to = starts_of(a, h, blockIdx.x, gridDim.x);
+  for (int i = t; i < kOrderBins; i += kSortThreads) to[i] = count[i];
 }
 
-// Counts to first positions.
-__global__ __launch_bounds__(1024) void order_scan_kernel(TrainArgs a) {
+// Counts to first positions: signature by signature, in each block by block.
+__global__ __launch_bounds__(1024) void order_scan_kernel(TrainArgs a, int blocks) {
   __shared__ uint32_t wtot[16];
-  constexpr int PER = kOrderBins / 1024;
+  static_assert(kOrderBins == 4 * 1024, "four signatures per thread");
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  uint32_t *start = a.order.start + static_cast<size_t>(blockIdx.x) * kOrderBins + PER * t;
-  uint32_t k[PER], mine = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) mine += k[i] = start[i];
-  const uint32_t incl = wave_incl_scan(mine);
+  uint4 *start = reinterpret_cast<uint4 *>(starts_of(a, blockIdx.x, 0, blocks)) + t;
+  constexpr int STEP = kOrderBins / 4;
+  uint4 k = make_uint4(0, 0, 0, 0);
+#pragma unroll 8
+  for (int b = 0; b < blocks; ++b) {
+    const uint4 x = start[static_cast<size_t>(b) * STEP];
+    k = make_uint4(k.x + x.x, k.y + x.y, k.z + x.z, k.w + x.w);
+  }
+  const uint32_t mine = k.x + k.y + k.z + k.w, incl = wave_incl_scan(mine);
   if (lane == 63) wtot[w] = incl;
   __syncthreads();
   uint32_t at = incl - mine;
   for (int i = 0; i < w; ++i) at += wtot[i];
+  uint4 next = make_uint4(at, at + k.x, at + k.x + k.y, at + k.x + k.y + k.z);
+  // eight loads before their stores, which they may not pass
+  for (int b = 0; b < blocks; b += 8) {
+    uint4 x[8];
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    start[i] = at;
-    at += k[i];
+    for (int i = 0; i < 8; ++i) x[i] = start[static_cast<size_t>(min(b + i, blocks - 1)) * STEP];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (b + i >= blocks) break;
+      start[static_cast<size_t>(b + i) * STEP] = next;
+      next = make_uint4(next.x + x[i].x, next.y + x[i].y, next.z + x[i].z, next.w + x[i].w);
+    }
   }
 }
 
+// A wave ranks 256 consecutive keys, 64 at a time, among those of their signature:
+// after the wave's earlier keys, which its own counters hold, come those of lower
+// lanes, which the signature's bits find in 12 votes.  No two waves share a counter,
+// so nothing depends on who comes first.  5 heads x 32760: 10 us, and 7 with counters
+// that a block's waves shared, in an order that varied.
 __global__ __launch_bounds__(kSortThreads) void order_place_kernel(TrainArgs a) {
-  __shared__ uint32_t next[kOrderBins];
-  const int h = blockIdx.y, t = threadIdx.x;
+  __shared__ __attribute__((aligned(16))) uint16_t count[kSortWaves][kOrderBins];
+  const int h = blockIdx.y, t = threadIdx.x, lane = t & 63, w = t >> 6;
   const size_t first = static_cast<size_t>(h) * a.n;
-  for (int i = t; i < kOrderBins; i += kSortThreads) next[i] = 0;
-  __syncthreads();
-  int bin[kSortKeys];
+  const int from = blockIdx.x * kOrderKeys + w * 64 * kSortKeys + lane;
+  int bin[kSortKeys], rank[kSortKeys];
+#pragma unroll
+  for (int i = 0; i < kSortKeys; ++i) bin[i] = from + 64 * i < a.n ? a.order.bin[first + from + 64 * i] : -1;
+  for (int i = lane; i < kOrderBins / 8; i += 64) reinterpret_cast<uint4 *>(count[w])[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
   for (int i = 0; i < kSortKeys; ++i) {
-    const int key = (blockIdx.x * kSortKeys + i) * kSortThreads + t;
-    bin[i] = key < a.n ? a.order.bin[first + key] : -1;
-    if (bin[i] >= 0) atomicAdd(&next[bin[i]], 1u);
+    unsigned long long same = __ballot(bin[i] >= 0);
+#pragma unroll
+    for (int b = 0; b < kBits; ++b) {
+      const bool bit = bin[i] >> b & 1;
+      const unsigned long long votes = __ballot(bit);
+      same &= bit ? votes : ~votes;
+    }
+    const int below = __popcll(same & ((1ull << lane) - 1ull));
+    // the counters are the wave's own: its LDS accesses keep their order
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int before = bin[i] >= 0 ? count[w][bin[i]] : 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (bin[i] >= 0 && below == 0) count[w][bin[i]] = static_cast<uint16_t>(before + __popcll(same));
+    rank[i] = before + below;
   }
   __syncthreads();
-  for (int i = t; i < kOrderBins; i += kSortThreads)
-    if (next[i]) next[i] = atomicAdd(&a.order.start[static_cast<size_t>(h) * kOrderBins + i], next[i]);
+  // the waves' counts to what the block's earlier waves hold
+  for (int i = t; i < kOrderBins; i += kSortThreads) {
+    int sum = 0;
+#pragma unroll
+    for (int x = 0; x < kSortWaves; ++x) {
+      const int k = count[x][i];
+      count[x][i] = static_cast<uint16_t>(sum);
+      sum += k;
+    }
+  }
   __syncthreads();
+  const uint32_t *start = starts_of(a, h, blockIdx.x, gridDim.x);
 #pragma unroll
   for (int i = 0; i < kSortKeys; ++i) {
     if (bin[i] < 0) continue;
-    const uint32_t at = atomicAdd(&next[bin[i]], 1u);
-    if (at < static_cast<uint32_t>(a.n)) a.order.key[first + at] = (blockIdx.x * kSortKeys + i) * kSortThreads + t;
+    const uint32_t at = start[bin[i]] + count[w][bin[i]] + rank[i];
+    if (at < static_cast<uint32_t>(a.n)) a.order.key[first + at] = from + 64 * i;
   }
 }
 
@@ -157,12 +203,11 @@ __global__ __launch_bounds__(256) void order_masks_kernel(TrainArgs a) {
 // Fewer than 8 clusters were not measured: such sets share most blocks of 32 keys.
 bool train_orders_keys(int n, int c_q) { return n >= 8192 && c_q >= 8; }
 
-// After the bins and costs have been cleared.
+// After the costs have been cleared.
 hipError_t train_order(const TrainArgs &a, int heads, hipStream_t s) {
-  constexpr int kKeys = kSortThreads * kSortKeys;
-  const dim3 grid((a.n + kKeys - 1) / kKeys, heads);
+  const dim3 grid((a.n + kOrderKeys - 1) / kOrderKeys, heads);
   hipLaunchKernelGGL(order_count_kernel, grid, dim3(kSortThreads), 0, s, a);
-  hipLaunchKernelGGL(order_scan_kernel, dim3(heads), dim3(1024), 0, s, a);
+  hipLaunchKernelGGL(order_scan_kernel, dim3(heads), dim3(1024), 0, s, a, static_cast<int>(grid.x));
   hipLaunchKernelGGL(order_place_kernel, grid, dim3(kSortThreads), 0, s, a);
   // the clusters in eighths: its loads are scattered words
   hipLaunchKernelGGL(order_masks_kernel, dim3((a.n + 255) / 256, heads, 8), dim3(256), 0, s, a);

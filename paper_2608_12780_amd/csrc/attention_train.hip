@@ -454,7 +454,7 @@ struct Prepare {
   int4 *items[2];
   int rows[2], per_head[2], stride[2];  // stride 2: work slots of one chunk
   uint32_t *masks;
-  KeyOrder order;  // its bins and costs are cleared
+  KeyOrder order;  // its costs are cleared
   int32_t *status;
   const uint64_t *rng;
   uint32_t *words;
@@ -608,7 +608,6 @@ __global__ __launch_bounds__(256) void train_prepare_kernel(Prepare p) {
     const int i = b / p.heads;
     if (i == 0 && p.order.cost) {
       const int h = b % p.heads;
-      for (int x = threadIdx.x; x < kOrderBins; x += 256) p.order.start[static_cast<size_t>(h) * kOrderBins + x] = 0;
       if (threadIdx.x < 2 * kOrderSlots) p.order.cost[static_cast<size_t>(h) * 2 * kOrderSlots + threadIdx.x] = 0;
     }
     prepare_items(p, b % p.heads, p.rows[i], p.per_head[i], p.stride[i], p.items[i]);
@@ -875,7 +874,7 @@ size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, 
   char *masks = take(mask_bytes);
   const size_t ordered_keys = train_orders_keys(n, c_q) ? 1 : 0;
   char *bin = take(ordered_keys * H * n * sizeof(uint16_t));
-  char *start = take(ordered_keys * H * kOrderBins * sizeof(uint32_t));
+  char *start = take(ordered_keys * H * ((n + kOrderKeys - 1) / kOrderKeys) * kOrderBins * sizeof(uint32_t));
   char *key = take(ordered_keys * H * n * sizeof(int32_t));
   char *by_position = take(ordered_keys * mask_bytes);
   char *cost = take(ordered_keys * H * 2 * kOrderSlots * sizeof(unsigned long long));

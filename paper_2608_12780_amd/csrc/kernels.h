@@ -270,12 +270,12 @@ constexpr int kTrainMaxClusters = 1024;
 // dK and dV (attention_order.hip); null: none.
 struct KeyOrder {
   uint16_t *bin;               // [heads][n]
-  uint32_t *start;             // [heads][kOrderBins]
+  uint32_t *start;             // [heads][ceil(n / kOrderKeys)][kOrderBins]
   int32_t *key;                // [heads][n] the key at a position
   uint32_t *masks;             // the key bits by position, as TrainArgs::masks
   unsigned long long *cost;    // [heads][kOrderSlots][by key, by position]
 };
-constexpr int kOrderBins = 4096, kOrderSlots = 64;
+constexpr int kOrderBins = 4096, kOrderSlots = 64, kOrderKeys = 4096;
 struct TrainArgs {
   int n, c_q, items_per_head;
   const void *q, *k, *v, *d_o;

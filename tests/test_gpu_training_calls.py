@@ -237,3 +237,31 @@ def test_status_of_autograds_calls_is_the_layers():
     dense.attention(*leaves).sum().backward()
     assert int(dense.training_attention().status.item()) == 8
     assert int(dense.autograd_attention().status.item()) == 8
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "bf16"), (64, "f32")])
+def test_non_finite_rows_reach_the_same_keys_on_every_run(d, dtype):
+    """Keys of few signatures, so that most positions in the keys' order are a choice
+    among equals: a NaN and an infinity in Q and dO reach the keys that share a wave
+    with one that their clusters keep, the same ones on every run."""
+    H, n, C = 2, 9000, 24
+    x = R.make(H, n, d, dtype, C, 0.5, 17)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    group = torch.randint(0, 48, (H, n), generator=g, device="cuda")
+    for h in range(H):
+        for c in range(C):
+            keys = (torch.rand(48, generator=g, device="cuda") < 0.3)[group[h]].nonzero()[:, 0]
+            x["sel_counts"][h, c] = len(keys)
+            x["sel_idx"][h, c, :len(keys)] = keys.int()
+    x["q"][0, 100, 3], x["q"][1, 5000, 7] = float("nan"), float("inf")
+    x["d_o"][0, 4000, 1], x["d_o"][1, 1, 2] = float("inf"), float("nan")
+    a = TrainingAttention(H, n, d, C, dtype)
+    qkv = (x["q"], x["k"], x["v"])
+    out = a.forward(*qkv, *R.sets(x))
+    bits = torch.int16 if dtype == "bf16" else torch.int32
+    runs = [[t.view(bits) for t in a.backward(*qkv, *out, x["d_o"], *R.sets(x), into=a.gradients())]
+            for _ in range(6)]
+    assert all(int(t.view(x["q"].dtype).isnan().any(2).sum()) for t in runs[0])
+    for again in runs[1:]:
+        for first, t in zip(runs[0], again):
+            assert torch.equal(first, t)
