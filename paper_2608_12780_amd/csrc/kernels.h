@@ -324,7 +324,8 @@ hipError_t train_forward(int d, bool bf16, const TrainArgs &a, const TrainCall &
 hipError_t train_backward(int d, bool bf16, const TrainArgs &a, const TrainCall &c, hipStream_t s);
 
 // Dropout of `count` elements (dropout.hip): y = x kept / (1 - p) + residual
-// (residual null: none); threshold as TrainArgs::drop.
+// (residual null: none).  threshold: T in [0, 65535], an element is dropped where
+// its 16-bit number is below it (not shifted, unlike TrainArgs::drop).
 hipError_t dropout_run(bool bf16, int64_t count, const void *x, const void *residual,
                        uint32_t threshold, const uint64_t *rng, void *y, hipStream_t s);
 
