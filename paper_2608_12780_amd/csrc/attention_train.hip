@@ -732,28 +732,6 @@ int parts_of(long long blocks, long long tiles, int least, int resident) {
   }
   return best;
 }
-int key_splits(int heads, int n, int d, bool bf16, int c_q) {
-  const int keys = bf16 ? kTrainKeyBlock : kRows, tile = bf16 ? kTrainKeyTile : kTile;
-  return parts_of(static_cast<long long>(heads) * ((n + keys - 1) / keys), train_items_per_head(n, c_q, tile), 2,
-                  512);
-}
-// The lists are on the device: clusters of a block's queries or fewer are taken to
-// fill a block each, larger ones half a block more than their queries do, and every
-// key to be selected.
-int query_splits(int heads, int n, int d, bool bf16, int c_q) {
-  const int rows = bf16 ? kBM : kRows, tile = bf16 ? kBN : kTile;
-  const long long chunks = n / rows + c_q / 2 > c_q ? n / rows + (c_q + 1) / 2 : c_q;
-  const int resident = bf16 && d == 128 ? 256 : 512;
-  // a block order of its own fills the chip better, where there are the blocks
-  if (bf16 && 2 * heads * chunks > resident && attention_ordered(heads, n, d, c_q)) return 1;
-  return parts_of(heads * chunks, n / tile, 4, resident);
-}
-// Whether the work slots of a bf16 call are listed with the rest: chunks alone, in
-// cluster order.  With so few no slots share a block and their order matters little.
-bool lists_slots(int heads, int n, int c_q) {
-  return static_cast<long long>(heads) * attn_items_per_head(n, c_q) <= 256;
-}
-
 // grad: masks and statistics too.
 template <typename T, int D>
 hipError_t prepare(const TrainArgs &a, const TrainCall &c, bool grad, hipStream_t s) {
@@ -772,7 +750,7 @@ hipError_t prepare(const TrainArgs &a, const TrainCall &c, bool grad, hipStream_
     p.per_head[lists++] = train_items_per_head(a.n, a.c_q, rows);
   };
   if (sizeof(T) == 4) list(c.items, kRows, 1);
-  else if (lists_slots(c.heads, a.n, a.c_q)) list(c.slots.items, kBM, 2);
+  else if (train_lists_slots(c.heads, a.n, a.c_q)) list(c.slots.items, kBM, 2);
   if (grad) list(c.tiles, sizeof(T) == 4 ? kTile : kTrainKeyTile, 1);
   p.list_blocks = lists * c.heads;
   p.word_blocks = a.drop ? 2 * c.heads * ((a.n + 255) / 256) : 0;
@@ -798,9 +776,9 @@ hipError_t prepare(const TrainArgs &a, const TrainCall &c, bool grad, hipStream_
 // The kernels by queries, and where they ran in parts the join.
 template <typename T, int D>
 hipError_t queries(TrainArgs a, const TrainCall &c, bool grad, T *out, hipStream_t s) {
-  a.splits = query_splits(c.heads, a.n, D, sizeof(T) == 2, a.c_q);
+  a.splits = train_query_parts(c.heads, a.n, D, sizeof(T) == 2, a.c_q);
   if constexpr (sizeof(T) == 2) {
-    TRAIN_TRY(train_queries(D, grad, a, c.heads, lists_slots(c.heads, a.n, a.c_q), c.slots, out, s));
+    TRAIN_TRY(train_queries(D, grad, a, c.heads, train_lists_slots(c.heads, a.n, a.c_q), c.slots, out, s));
   } else {
     a.items = c.items;
     a.items_per_head = train_items_per_head(a.n, a.c_q, kRows);
@@ -831,7 +809,7 @@ hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
   T *dk = static_cast<T *>(c.dk), *dv = static_cast<T *>(c.dv);
   a.items = c.tiles;
   a.items_per_head = train_items_per_head(a.n, a.c_q, sizeof(T) == 2 ? kTrainKeyTile : kTile);
-  a.splits = key_splits(c.heads, a.n, D, sizeof(T) == 2, a.c_q);
+  a.splits = train_key_parts(c.heads, a.n, sizeof(T) == 2, a.c_q);
   if (a.order.cost) TRAIN_TRY(train_order(a, c.heads, s));
   if constexpr (sizeof(T) == 2) {
     TRAIN_TRY(train_keys(D, a, c.heads, dk, dv, s));
@@ -844,6 +822,28 @@ hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
 }
 
 }  // namespace
+
+int train_key_parts(int heads, int n, bool bf16, int c_q) {
+  const int keys = bf16 ? kTrainKeyBlock : kRows, tile = bf16 ? kTrainKeyTile : kTile;
+  return parts_of(static_cast<long long>(heads) * ((n + keys - 1) / keys), train_items_per_head(n, c_q, tile), 2,
+                  512);
+}
+// The lists are on the device: clusters of a block's queries or fewer are taken to
+// fill a block each, larger ones half a block more than their queries do, and every
+// key to be selected.
+int train_query_parts(int heads, int n, int d, bool bf16, int c_q) {
+  const int rows = bf16 ? kBM : kRows, tile = bf16 ? kBN : kTile;
+  const long long chunks = n / rows + c_q / 2 > c_q ? n / rows + (c_q + 1) / 2 : c_q;
+  const int resident = bf16 && d == 128 ? 256 : 512;
+  // a block order of its own fills the chip better, where there are the blocks
+  if (bf16 && 2 * heads * chunks > resident && attention_ordered(heads, n, d, c_q)) return 1;
+  return parts_of(heads * chunks, n / tile, 4, resident);
+}
+// Whether the work slots of a bf16 call are listed with the rest: chunks alone, in
+// cluster order.  With so few no slots share a block and their order matters little.
+bool train_lists_slots(int heads, int n, int c_q) {
+  return static_cast<long long>(heads) * attn_items_per_head(n, c_q) <= 256;
+}
 
 bool train_launchable(int heads, int n, int d, bool bf16, int c_q) {
   const uint64_t H = heads, chunks = bf16 ? attn_items_per_head(n, c_q) : train_items_per_head(n, c_q, kRows);
@@ -878,7 +878,7 @@ size_t train_workspace(int heads, int n, int d, bool bf16, int c_q, void *base, 
   char *key = take(ordered_keys * H * n * sizeof(int32_t));
   char *by_position = take(ordered_keys * mask_bytes);
   char *cost = take(ordered_keys * H * 2 * kOrderSlots * sizeof(unsigned long long));
-  const size_t sk = key_splits(heads, n, d, bf16, c_q), sq = query_splits(heads, n, d, bf16, c_q);
+  const size_t sk = train_key_parts(heads, n, bf16, c_q), sq = train_query_parts(heads, n, d, bf16, c_q);
   const size_t by_keys = sk > 1 ? 2 * sk * d : 0, by_queries = sq > 1 ? sq * (d + 2) : 0;
   char *parts = take(H * n * (by_keys > by_queries ? by_keys : by_queries) * sizeof(float));
   if (a) {

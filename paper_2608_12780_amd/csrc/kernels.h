@@ -315,6 +315,11 @@ bool train_orders_keys(int n, int c_q);
 hipError_t train_order(const TrainArgs &a, int heads, hipStream_t s);
 hipError_t train_keys(int d, const TrainArgs &a, int heads, uint16_t *dk, uint16_t *dv, hipStream_t s);
 int train_items_per_head(int n, int c_q, int rows);
+// The launches' rules: parts of dK and dV and of the kernels by queries, and whether
+// a bf16 call's work slots are listed with the rest (no block order then).
+int train_key_parts(int heads, int n, bool bf16, int c_q);
+int train_query_parts(int heads, int n, int d, bool bf16, int c_q);
+bool train_lists_slots(int heads, int n, int c_q);
 // Whether every launch stays below 2^32 threads.
 bool train_launchable(int heads, int n, int d, bool bf16, int c_q);
 // Lays the workspace out (base null: only its size).
