@@ -2,7 +2,8 @@
 // and dropout, and dQ (attention_train.hip has the formulas, and the kernels for
 // fp32).
 //
-// Work slots are the inference attention's (attention.hip): a block runs up to 256
+// Work slots and their order, with the costs measured on it, are the inference
+// attention's (attention.hip): a block runs up to 256
 // queries of a cluster, or of two clusters side by side, a wave 32 of them, over
 // the cluster's keys 64 at a time, K and V rows gathered into LDS by the buffer unit
 // while the tile before is computed.  The gradient recomputes p from the row's

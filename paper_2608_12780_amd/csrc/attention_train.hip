@@ -11,8 +11,9 @@
 // dk and dv run over the clusters' queries, a wave per 32 keys (fp32: 16), with a
 // bit for each (cluster, key), so every sum has one owner and a fixed order: no
 // atomics on results, the same bits on every run.  S and dP are computed for either
-// side, seven products where five are needed; one pass for all three would add dq
-// from every block of keys, in an order that varies or through memory of its own.
+// side, seven products where five are needed (eight for bf16, whose dq takes ds in two
+// terms); one pass for all three would add dq from every block of keys, in an order
+// that varies or through memory of its own.
 #include <math.h>
 
 #include "attention_slots.h"
@@ -32,7 +33,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // instruction, so that inputs, weights and ds are not rounded.  They run at a
 // sixteenth of the bf16 rate and need little bandwidth: a wave owns 16 queries
 // (or keys), four waves a block, which makes short work items for an even load and
-// leaves two blocks a CU (d = 64: four) to cover the staging of tiles.  Bound by the
+// leaves two blocks a CU (d = 64: four by queries, three by keys) to cover the staging
+// of tiles.  Bound by the
 // matrix pipe, 73 to 76% busy: 4 heads x 6417 tokens, d = 128, 53% of the keys kept,
 // dq 740 to 766 us (88 TFLOP/s of the products that count), dk and dv 1270 to 1300.
 constexpr int kThreads = 256;
@@ -716,9 +718,9 @@ hipError_t join_parts(size_t count, int splits, float scale_k, float scale_v, co
 // Parts that each block's tiles are cut into, with fp32 sums of their own that a
 // second kernel adds: as many, up to 16 of `least` tiles or more, as make the
 // launch's rounds shortest; a part costs about 4% of a block more (its start, its
-// sums).  `resident`: the blocks that the chip holds at once.  3 heads x 2185 tokens,
-// d = 128: dq in parts 43 us and their join 5, dk and dv 47 and 10; the largest cases,
-// whose blocks fill the chip many times, stay whole or take two parts.
+// sums).  `resident`: the blocks that the chip is taken to hold at once.  3 heads x 2185
+// tokens, d = 128: dq in parts 43 us and their join 5, dk and dv 47 and 10; calls whose
+// blocks fill the chip many times stay whole or take few parts.
 int parts_of(long long blocks, long long tiles, int least, int resident) {
   constexpr int kMost = 16;
   int best = 1;
@@ -823,6 +825,8 @@ hipError_t backward(TrainArgs a, const TrainCall &c, hipStream_t s) {
 
 }  // namespace
 
+// Two blocks a CU.  At d = 64 the chip holds three (bf16 with dropout two), which was
+// not measured here.
 int train_key_parts(int heads, int n, bool bf16, int c_q) {
   const int keys = bf16 ? kTrainKeyBlock : kRows, tile = bf16 ? kTrainKeyTile : kTile;
   return parts_of(static_cast<long long>(heads) * ((n + keys - 1) / keys), train_items_per_head(n, c_q, tile), 2,
@@ -830,7 +834,8 @@ int train_key_parts(int heads, int n, bool bf16, int c_q) {
 }
 // The lists are on the device: clusters of a block's queries or fewer are taken to
 // fill a block each, larger ones half a block more than their queries do, and every
-// key to be selected.
+// key to be selected.  Blocks a CU: bf16 one (d = 64: two, though with dropout the
+// chip holds one), fp32 two (though at d = 64 it holds four).
 int train_query_parts(int heads, int n, int d, bool bf16, int c_q) {
   const int rows = bf16 ? kBM : kRows, tile = bf16 ? kBN : kTile;
   const long long chunks = n / rows + c_q / 2 > c_q ? n / rows + (c_q + 1) / 2 : c_q;

@@ -196,10 +196,11 @@ class _Differentiable:
 
     def attention(self, q, k, v, scale=0.0, dropout=0.0, rng=None):
         """Attention over the clusters and key sets that the layer holds (calls
-        6 and 7), differentiable in q, k and v.  They must not be rewritten (a
-        new clustering or selection) before the backward pass has run.  To
-        capture a graph, call `training_attention`'s forward and backward:
-        they allocate nothing when given their outputs."""
+        6 and 7), on the current stream, differentiable in q, k and v, whose
+        gradients have their shapes.  The sets must not be rewritten (a new
+        clustering or selection) before the backward pass has run.  To capture
+        a graph, call `training_attention`'s forward and backward: they
+        allocate nothing when given their outputs."""
         count = self.heads * self.n * self.d
         for t, name in ((q, "q"), (k, "k"), (v, "v")):
             if torch.is_grad_enabled() and t.requires_grad and t.numel() != count:
