@@ -121,12 +121,12 @@ class _AttentionFunction(torch.autograd.Function):
 
 class _DropoutFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, residual, p, rng):
+    def forward(ctx, x, residual, p, rng, stream):
         rng = rng.clone() if rng is not None else None
         ctx.save_for_backward(*(() if rng is None else (rng,)))
         ctx.p = p
         y = torch.empty_like(x)
-        B.scope_dropout(x, residual, p, rng, y)
+        B.scope_dropout(x, residual, p, rng, y, stream)
         return y
 
     @staticmethod
@@ -138,7 +138,7 @@ class _DropoutFunction(torch.autograd.Function):
             dx = torch.empty_like(d_y)
             B.scope_dropout(d_y, None, ctx.p, ctx.saved_tensors[0] if ctx.saved_tensors else None,
                             dx)
-        return dx, d_y if ctx.needs_input_grad[1] else None, None, None
+        return dx, d_y if ctx.needs_input_grad[1] else None, None, None, None
 
 
 def dropout(x, p, rng, residual=None, out=None, stream=None):
@@ -148,13 +148,14 @@ def dropout(x, p, rng, residual=None, out=None, stream=None):
     offset) on the GPU."""
     if residual is not None and residual.shape != x.shape:
         raise ValueError(f"residual is {tuple(residual.shape)}, x {tuple(x.shape)}")
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad
-                                       for t in (x, residual, out)):
+    if torch.is_grad_enabled() and (
+            x.requires_grad or residual is not None and residual.requires_grad
+            or out is not None and out.requires_grad):
         if out is not None:
             raise ValueError("dropout into `out` is not differentiable: leave `out` away, or call "
                              "it under torch.no_grad()")
-        with _allocating_on(stream):  # the function runs on the current stream
-            return _DropoutFunction.apply(x, residual, p, rng)
+        with _allocating_on(stream):  # the backward pass runs on this stream too
+            return _DropoutFunction.apply(x, residual, p, rng, stream)
     y = out
     if y is None:
         with _allocating_on(stream):
