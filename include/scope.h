@@ -434,6 +434,106 @@ int32_t scope_dropout(int32_t dtype, int64_t count, const void *x,
                       const void *residual, float dropout, const uint64_t *rng,
                       void *y, void *stream);
 
+/* Rows of a tensor [heads][rows][d] wherever they lie: element (h, i, c) is at
+ * h * head + i * row + c, in elements.  A NULL pointer in place of strides is
+ * the dense layout (row = d, head = rows * d).  Inputs may have any strides >= 0
+ * (0: one row for all); rows of an output must not overlap one another.      */
+typedef struct {
+  int64_t row, head;
+} scope_strides;
+
+/* 9. Rotary positions: queries and keys turned by their tokens' positions (the
+ * layer takes them after this), or their gradients turned back.  `axes` channel
+ * ranges I_a = [range_off[a], range_off[a] + range_len[a]), disjoint, of even
+ * length, hold range_len[a] / 2 pairs each: neighbours (2 i, 2 i + 1) of the range
+ * for SCOPE_PAIRS (even offsets), (i, i + len / 2) for SCOPE_HALVES.  With t the
+ * angle of the pair at the token's position p_a,
+ *   y_a = factor (x_a cos t - x_b sin t), y_b = factor (x_a sin t + x_b cos t),
+ * t replaced by -t where `inverse` (the gradient of x from that of y).  Channels
+ * in no range are copied.  positions [axes][rows]; turns: for each pair, axis after
+ * axis, the fraction of a whole turn per position in units of 2^-64, so that
+ * t / (2 pi) = p * turns / 2^64 mod 1 is exact in integers at any position.
+ * Sines and cosines are fp32 within 2^-22, products fp32, y rounded once.
+ * A second tensor x2 -> y2 of heads[1] heads and the same positions (keys with
+ * their queries) is turned by the same launch; heads[1] = 0: none.
+ * y may be x with the same strides; otherwise they must not overlap (nor y, y2).
+ * Requires rows >= 0, 1 <= heads[0], 2 <= d <= 1024 even, 1 <= axes <= 3, a finite
+ * factor; every size below 2^31.  Any alignment of whole elements is taken;
+ * 16-byte alignment of pointers and strides, with d (and for halves ranges'
+ * offsets and half lengths) multiples of 8, is faster.                       */
+typedef enum { SCOPE_PAIRS = 0, SCOPE_HALVES = 1 } scope_rotary_layout;
+typedef struct {
+  int32_t rows, heads[2], d, dtype;
+  int32_t axes, range_off[3], range_len[3];
+  int32_t layout, inverse;
+  float factor;
+} scope_rotation;
+int32_t scope_rotary(const scope_rotation *rotation, const int32_t *positions,
+                     const uint64_t *turns, const void *x, const scope_strides *x_strides,
+                     void *y, const scope_strides *y_strides, const void *x2,
+                     const scope_strides *x2_strides, void *y2,
+                     const scope_strides *y2_strides, void *stream);
+
+/* Exact attention over sequences packed one after the other, with query heads in
+ * groups that share a key head (heads a multiple of kv_heads; query head h reads key
+ * head h / (heads / kv_heads)).  Sequence s has the query rows offsets_q[s] ..
+ * offsets_q[s+1] and the key rows offsets_k[s] .. offsets_k[s+1], or with lengths_k
+ * (call 10) the first lengths_k[s] of those, a cache with room for more.  Lengths may
+ * differ and be 0.  With n queries and m keys of a sequence, query i sees every key,
+ * or where `causal` the keys j <= i + m - n: the last query sees all, queries before
+ * the first key see none.
+ * Supported: d in {64, 128}, 1 <= sequences <= 65536, 0 <= rows <= 2^24, heads * rows
+ * < 2^31 each; 16-byte aligned rows (pointers and strides); the rows of one key head,
+ * or of the query heads that share it, within 2^32 bytes of the first.        */
+typedef struct {
+  int32_t heads, kv_heads;
+  int32_t rows_q, rows_k; /* rows of q, o; of k, v */
+  int32_t sequences;
+  int32_t d, dtype, causal;
+} scope_pack;
+
+/* Workspace bytes that suffice for calls 10 and 11 with these sizes.        */
+int32_t scope_packed_workspace_size(const scope_pack *pack, size_t *bytes);
+
+/* 10. Forward, for prompts, chunks behind a cache and single tokens:
+ *   lse_i = log sum_j exp(scale <q_i, k_j>)   (fp32, natural log; [heads][rows_q])
+ *   O_i   = sum_j exp(scale <q_i, k_j> - lse_i) v_j,  j over the keys that i sees
+ * (scale <= 0 selects 1/sqrt(d)).  A query that sees no key gives O = 0 and
+ * lse = -inf.  Rows in no sequence are left as they were, and key rows in none are
+ * not read.  Types as call 6 (fp32 inputs are not rounded, bf16 weights are); sums
+ * and statistics are fp32.  A non-finite value row may reach queries of its sequence
+ * up to 63 places before the first that sees it, or 31 keys' worth for a few queries;
+ * a non-finite key row reaches only queries that see it.
+ * Results repeat bit for bit.  Long sums may be cut into parts, whose number follows
+ * from the sizes in `pack` alone.
+ * Bad offsets cannot fault: each is taken as the largest so far within [0, rows] and
+ * lengths are cut to their room; either sets bit 4 of dev_status (may be NULL).
+ * lse and O must not overlap the inputs.                                      */
+int32_t scope_packed_attention(const scope_pack *pack, const void *q,
+                               const scope_strides *q_strides, const void *k,
+                               const scope_strides *k_strides, const void *v,
+                               const scope_strides *v_strides, const int32_t *offsets_q,
+                               const int32_t *offsets_k, const int32_t *lengths_k,
+                               float scale, void *o, const scope_strides *o_strides,
+                               float *lse, void *workspace, size_t ws_bytes,
+                               int32_t *dev_status, void *stream);
+
+/* 11. Gradients of call 10 (without lengths_k), formulas and types as call 7
+ * without dropout: dK and dV sum over the query heads that share the key head.  dK
+ * and dV are 0 for keys of a sequence that no query sees, dQ for queries that see no
+ * key; rows in no sequence are left as they were.  A non-finite row of Q or d_o may
+ * reach dK and dV of keys of its sequence that it does not see, a non-finite row of
+ * K or V dQ of queries that do not see it.  No gradient may overlap an input or
+ * another one.  Otherwise as call 10.                                        */
+int32_t scope_packed_attention_backward(
+    const scope_pack *pack, const void *q, const scope_strides *q_strides, const void *k,
+    const scope_strides *k_strides, const void *v, const scope_strides *v_strides,
+    const void *o, const scope_strides *o_strides, const float *lse, const void *d_o,
+    const scope_strides *d_o_strides, const int32_t *offsets_q, const int32_t *offsets_k,
+    float scale, void *dq, const scope_strides *dq_strides, void *dk,
+    const scope_strides *dk_strides, void *dv, const scope_strides *dv_strides,
+    void *workspace, size_t ws_bytes, int32_t *dev_status, void *stream);
+
 /* Diagnostics: the measured peaks that roofline fractions are also quoted
  * against.  scope_debug_copy copies `bytes` (a multiple of 16; src and dst
  * 16-byte aligned, not overlapping) with a plain vector copy kernel, so its

@@ -31,9 +31,12 @@ ENTRY_POINTS = (
     "scope_debug_attention_items",
     "scope_training_workspace_size", "scope_sparse_attention_train",
     "scope_sparse_attention_backward", "scope_dropout",
+    "scope_rotary", "scope_packed_workspace_size", "scope_packed_attention",
+    "scope_packed_attention_backward",
 )
 MAX_SUBSPACES, MAX_D = 8, 128
 POLICIES = {"online": 0, "fixed": 1, "topp": 2}
+LAYOUTS = {"pairs": 0, "halves": 1}
 
 
 class ScopeError(RuntimeError):
@@ -79,6 +82,42 @@ def make_partition(sets, c_m) -> Partition:
     for t, ch in enumerate(chan):
         p.channels[t] = ch
     return p
+
+
+class Strides(ctypes.Structure):
+    """Where the rows of a tensor [heads][rows][d] lie, in elements."""
+    _fields_ = [("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("heads", ctypes.c_int32 * 2),
+                ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("range_off", ctypes.c_int32 * 3), ("range_len", ctypes.c_int32 * 3),
+                ("layout", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("factor", ctypes.c_float)]
+
+
+def make_rotation(rows, heads, d, dtype, ranges, layout="pairs", inverse=False,
+                  factor=1.0) -> Rotation:
+    """ranges: the axes' (offsets, lengths); heads: of the first and second tensor."""
+    off, ln = ranges
+    if len(off) != len(ln) or not 1 <= len(off) <= 3:
+        raise ValueError("need 1..3 channel ranges")
+    pad = [0] * (3 - len(off))
+    return Rotation(int(rows), (ctypes.c_int32 * 2)(*map(int, heads)), int(d), int(dtype),
+                    len(off), (ctypes.c_int32 * 3)(*map(int, [*off, *pad])),
+                    (ctypes.c_int32 * 3)(*map(int, [*ln, *pad])), LAYOUTS[layout],
+                    int(bool(inverse)), float(factor))
+
+
+class Pack(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("heads", "kv_heads", "rows_q", "rows_k",
+                                              "sequences", "d", "dtype", "causal")]
+
+
+def make_pack(heads, kv_heads, rows_q, rows_k, sequences, d, dtype, causal) -> Pack:
+    return Pack(int(heads), int(kv_heads), int(rows_q), int(rows_k), int(sequences), int(d),
+                int(dtype), int(bool(causal)))
 
 
 _lib = None
@@ -130,6 +169,13 @@ def lib() -> ctypes.CDLL:
         L.scope_sparse_attention_backward.argtypes = [SP, P, P, P, P, P, P, I, P, P, P, P, F, F,
                                                       P, P, P, P, P, Z, P, P]
         L.scope_dropout.argtypes = [I, ctypes.c_int64, P, P, F, P, P, P]
+        ST, KP = ctypes.POINTER(Strides), ctypes.POINTER(Pack)
+        L.scope_rotary.argtypes = [ctypes.POINTER(Rotation), P, P, P, ST, P, ST, P, ST, P, ST, P]
+        L.scope_packed_workspace_size.argtypes = [KP, ctypes.POINTER(Z)]
+        L.scope_packed_attention.argtypes = [KP, P, ST, P, ST, P, ST, P, P, P, F, P, ST, P,
+                                             P, Z, P, P]
+        L.scope_packed_attention_backward.argtypes = [KP, P, ST, P, ST, P, ST, P, ST, P, P, ST,
+                                                      P, P, F, P, ST, P, ST, P, ST, P, Z, P, P]
         for name in ENTRY_POINTS[2:]:
             getattr(L, name).restype = I
         _lib = L
@@ -418,6 +464,100 @@ def scope_dropout(x, residual, dropout, rng, y, stream=None):
             _rng(rng, dropout), _ptr(y, x.dtype, None, "y"))
     _check("scope_dropout", _on_device(lambda s: lib().scope_dropout(*args, s), stream,
                                        x, residual, rng, y))
+
+
+def _rows(t, dtype, heads, rows, d, name):
+    """(pointer, strides) of a tensor [heads][rows][d] whose channels are contiguous."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != (heads, rows, d):
+        raise ValueError(f"{name} must be {(heads, rows, d)}, got {tuple(t.shape)}")
+    if t.numel() and d > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name} needs contiguous channels")
+    # of a dimension of one row the stride says nothing
+    row = t.stride(1) if rows > 1 and heads else d
+    head = t.stride(0) if heads > 1 and rows else rows * d
+    return ctypes.c_void_p(t.data_ptr()), ctypes.byref(Strides(row, head))
+
+
+def scope_rotary(x, y, positions, turns, ranges, layout="pairs", inverse=False, factor=1.0,
+                 x2=None, y2=None, stream=None):
+    """y = x, [heads][rows][d], turned by positions [axes][rows] (y2 = x2 too)."""
+    if x.dim() != 3 or (x2 is not None and x2.dim() != 3):
+        raise ValueError("need tensors of three dimensions: heads, rows, channels")
+    if x.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"x must be bfloat16 or float32, got {x.dtype}")
+    if (x2 is None) != (y2 is None):
+        raise ValueError("x2 and y2 go together")
+    heads, rows, d = x.shape
+    heads2 = x2.shape[0] if x2 is not None else 0
+    r = make_rotation(rows, (heads, heads2), d, BF16 if x.dtype == torch.bfloat16 else F32, ranges,
+                      layout, inverse, factor)
+    pairs = sum(int(n) for n in ranges[1]) // 2
+    args = [ctypes.byref(r), _ptr(positions, torch.int32, r.axes * rows, "positions"),
+            _ptr(turns, torch.int64, pairs, "turns"),
+            *_rows(x, x.dtype, heads, rows, d, "x"), *_rows(y, x.dtype, heads, rows, d, "y")]
+    args += ([*_rows(x2, x.dtype, heads2, rows, d, "x2"), *_rows(y2, x.dtype, heads2, rows, d, "y2")]
+             if x2 is not None else [None] * 4)
+    _check("scope_rotary", _on_device(lambda s: lib().scope_rotary(*args, s), stream, x, y,
+                                      positions, turns, x2, y2))
+
+
+def scope_packed_workspace_size(pack: Pack) -> int:
+    out = ctypes.c_size_t(0)
+    _check("scope_packed_workspace_size", lib().scope_packed_workspace_size(
+        ctypes.byref(pack), ctypes.byref(out)))
+    return int(out.value)
+
+
+def alloc_packed_workspace(pack: Pack, device="cuda"):
+    """A uint8 workspace tensor for the packed calls."""
+    return torch.empty(max(scope_packed_workspace_size(pack), 1), dtype=torch.uint8, device=device)
+
+
+def _packed(pack, tensors):
+    """Pointers and strides of (name, tensor, of queries) entries."""
+    dt, out = _data_dtype(pack), {}
+    for name, t, queries in tensors:
+        out[name] = _rows(t, dt, pack.heads if queries else pack.kv_heads,
+                          pack.rows_q if queries else pack.rows_k, pack.d, name)
+    return out
+
+
+def scope_packed_attention(pack, q, k, v, offsets_q, offsets_k, lengths_k, scale, o, lse,
+                           workspace, dev_status=None, stream=None):
+    r = _packed(pack, (("q", q, True), ("k", k, False), ("v", v, False), ("o", o, True)))
+    S = pack.sequences
+    args = (ctypes.byref(pack), *r["q"], *r["k"], *r["v"],
+            _ptr(offsets_q, torch.int32, S + 1, "offsets_q"),
+            _ptr(offsets_k, torch.int32, S + 1, "offsets_k"),
+            _ptr(lengths_k, torch.int32, S, "lengths_k", optional=True), float(scale), *r["o"],
+            _ptr(lse, torch.float32, pack.heads * pack.rows_q, "lse"),
+            _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel(),
+            _ptr(dev_status, torch.int32, 1, "dev_status", optional=True))
+    _check("scope_packed_attention", _on_device(
+        lambda s: lib().scope_packed_attention(*args, s), stream, q, k, v, offsets_q, offsets_k,
+        lengths_k, o, lse, workspace, dev_status))
+
+
+def scope_packed_attention_backward(pack, q, k, v, o, lse, d_o, offsets_q, offsets_k, scale, dq,
+                                    dk, dv, workspace, dev_status=None, stream=None):
+    r = _packed(pack, (("q", q, True), ("k", k, False), ("v", v, False), ("o", o, True),
+                       ("d_o", d_o, True), ("dq", dq, True), ("dk", dk, False), ("dv", dv, False)))
+    S = pack.sequences
+    args = (ctypes.byref(pack), *r["q"], *r["k"], *r["v"], *r["o"],
+            _ptr(lse, torch.float32, pack.heads * pack.rows_q, "lse"), *r["d_o"],
+            _ptr(offsets_q, torch.int32, S + 1, "offsets_q"),
+            _ptr(offsets_k, torch.int32, S + 1, "offsets_k"), float(scale), *r["dq"], *r["dk"],
+            *r["dv"], _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel(),
+            _ptr(dev_status, torch.int32, 1, "dev_status", optional=True))
+    _check("scope_packed_attention_backward", _on_device(
+        lambda s: lib().scope_packed_attention_backward(*args, s), stream, q, k, v, o, lse, d_o,
+        offsets_q, offsets_k, dq, dk, dv, workspace, dev_status))
 
 
 def scope_debug_copy(src, dst, stream=None):

@@ -13,7 +13,8 @@ LIB = os.path.join(PKG, "libscope.so")
 SOURCES = ["api.cpp", "kmeans.hip", "kmeans_mfma.hip", "kmeans_update.hip",
            "kmeans_codebook.hip", "kmeans_lloyd.hip", "score.hip",
            "select.hip",
-           "attention.hip", "attention_train.hip", "attention_queries.hip", "attention_keys.hip", "attention_order.hip", "dropout.hip", "peaks.hip"]
+           "attention.hip", "attention_train.hip", "attention_queries.hip", "attention_keys.hip", "attention_order.hip", "dropout.hip", "peaks.hip",
+           "api_packed.cpp", "rotary.hip", "packed_plan.hip", "packed_queries.hip", "packed_keys.hip", "packed_f32.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = [

@@ -334,4 +334,78 @@ hipError_t train_backward(int d, bool bf16, const TrainArgs &a, const TrainCall 
 hipError_t dropout_run(bool bf16, int64_t count, const void *x, const void *residual,
                        uint32_t threshold, const uint64_t *rng, void *y, hipStream_t s);
 
+// Rotary positions (rotary.hip).
+struct RotaryArgs {
+  int rows, heads[2], units, per;   // units of a row's channels, heads of a thread
+  int axes, off[3], len[3], by_off[3];  // by_off: the axes by ascending offset
+  int inverse;
+  float factor;
+  const int32_t *positions;
+  const uint64_t *turns;
+  const void *x[2];
+  void *y[2];
+  scope_strides xs[2], ys[2];
+};
+// vectors: 16-byte accesses are aligned, and whole
+hipError_t rotary_run(const RotaryArgs &a, bool bf16, bool pairs, bool vectors, int d, hipStream_t s);
+
+// Attention over packed sequences (packed_*.hip).  A tensor's rows, strides in bytes.
+struct PackRows {
+  char *base;
+  int64_t row, head;
+};
+// One list of work items, by falling cost: item i is a sequence's (first query row,
+// queries, first key row, keys) and (first row or key of the item, ..).  An item by
+// queries holds kRows rows (query, head of the group) of one key head.
+struct PackList {
+  int4 *items;
+  int rows;       // rows or keys of an item
+  int capacity;   // items at most
+};
+struct PackArgs {
+  int kv_heads, group, rows_q, rows_k, sequences, causal;
+  PackRows q, k, v, d_o;
+  const int32_t *offsets_q, *offsets_k, *lengths_k;
+  float scale, scale_log2;
+  float *lse;             // [heads][rows_q]
+  PackList list;          // of this launch
+  const int32_t *count;   // items in it
+  const int32_t *ends;    // first and last query row, first and last key row of all sequences
+  // Parts that an item's tiles are cut into, and with more than one their sums: O or
+  // dQ [part][kv_heads][rows_q * group][d], then of the forward (maximum, normaliser);
+  // dK, dV [part][2][kv_heads][rows_k][d].
+  int splits;
+  float *parts;
+  // [2][kv_heads][rows_q * group]: -lse in the exp2 domain (-inf where no key is seen)
+  // and <do, o>, by query and head of the group
+  const float *stats;
+};
+struct PackCall {
+  int d;
+  bool bf16;
+  PackRows o, dq, dk, dv;
+  PackList by_rows, by_keys;
+  int splits_rows, splits_keys;
+  bool tokens;            // few queries a sequence: packed_tokens.hip
+  int slots;              // its work slots of a key head
+  int32_t *header, *status;
+  const float *lse;
+};
+// Lays the workspace out (base null: only its size) and chooses the launches.
+size_t packed_workspace(const scope_pack *p, void *base, PackArgs *a, PackCall *c);
+bool packed_launchable(const scope_pack *p);
+hipError_t packed_forward(const PackArgs &a, const PackCall &c, hipStream_t s);
+hipError_t packed_backward(const PackArgs &a, const PackCall &c, hipStream_t s);
+// The kernels: O (grad false) or dQ, by rows; dK and dV, by keys; few queries.
+hipError_t packed_queries(const PackArgs &a, int d, bool grad, const PackRows &out, hipStream_t s);
+hipError_t packed_keys(const PackArgs &a, int d, const PackRows &dk, const PackRows &dv, hipStream_t s);
+hipError_t packed_queries_f32(const PackArgs &a, int d, bool grad, const PackRows &out, hipStream_t s);
+hipError_t packed_keys_f32(const PackArgs &a, int d, const PackRows &dk, const PackRows &dv, hipStream_t s);
+hipError_t packed_tokens(const PackArgs &a, int d, const PackRows &out, int slots, int32_t *status, hipStream_t s);
+constexpr int kPackRows = 256;       // rows of a bf16 item by queries
+constexpr int kPackKeys = 128;       // keys of a bf16 item by keys
+constexpr int kPackRowsF32 = 64;     // rows, or keys, of an fp32 item
+constexpr int kPackTokenRows = 32;   // rows of an item of few queries
+constexpr int kPackTokenKeys = 512;  // and its keys
+
 }  // namespace scope

@@ -1,0 +1,433 @@
+// Attention over packed sequences (calls 10 and 11): the work lists, the rows'
+// statistics for the gradients, the joins of parts, and the order of launches.
+//
+// With n queries and m keys of a sequence, key head h and the query heads of its
+// group side by side as rows (query, head):
+//   s_ij = <q_i, k_j>, p_ij = exp(scale s_ij - lse_i), j <= i + m - n where causal
+//   o_i = sum_j p_ij v_j,  ds_ij = p_ij (<do_i, v_j> - <do_i, o_i>)
+//   dq_i = scale sum_j ds_ij k_j, dk_j = scale sum_i ds_ij q_i, dv_j = sum_i p_ij do_i
+// A group's rows share their keys' tiles, and dk and dv sum over them in one place.
+// As in the sparse layer's training attention every sum has one owner and a fixed
+// order (dq by rows, dk and dv by keys).
+//
+// Sequence lengths are on the device, so the host launches as many blocks as any
+// lengths could need, and one block makes the list of those that there are, longest
+// first.
+#include <math.h>
+
+#include "common.h"
+#include "kernels.h"
+#include "mfma.h"
+#include "packed.h"
+
+namespace scope {
+
+namespace {
+
+constexpr int kThreads = 1024;
+constexpr int kBins = 1024;
+constexpr int kStatusBadOffsets = 16;
+constexpr int kCostKeys = 64, kCostRows = 32;  // a unit of an item's cost
+
+struct PackPrepare {
+  PackArgs a;
+  PackList lists[2];
+  int n_lists;
+  int32_t *header;   // counts, ends
+  int32_t *status;
+  int d;
+  PackRows o;        // gradients: the statistics' inputs
+  const float *lse;
+  float *stats;
+};
+
+// Inclusive scan over the block's threads; `total` receives the last.
+template <bool MAX>
+__device__ int block_scan(int v, int *wave, int *total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int t = __shfl_up(v, o);
+    if (lane >= o) v = MAX ? max(v, t) : v + t;
+  }
+  __syncthreads();
+  if (lane == 63) wave[w] = v;
+  __syncthreads();
+  int all = wave[0];
+  for (int i = 1; i < kThreads / 64; ++i) {
+    if (i == w) v = MAX ? max(v, all) : v + all;
+    all = MAX ? max(all, wave[i]) : all + wave[i];
+  }
+  *total = all;
+  return v;
+}
+
+__device__ void make_list(const PackPrepare &p, int which) {
+  const PackArgs &a = p.a;
+  const PackList list = p.lists[which];
+  __shared__ int wave[kThreads / 64], first[kThreads + 1], hist[kBins];
+  __shared__ int4 seq[kThreads];
+  const int t = threadIdx.x, S = a.sequences;
+  const bool by_keys = which == 1;
+  hist[t] = 0;
+  // a cost's bin: the longest first; items without work last
+  const int most = by_keys ? (a.rows_q * a.group + kCostRows - 1) / kCostRows : (a.rows_k + kCostKeys - 1) / kCostKeys;
+  const float per_cost = static_cast<float>(kBins - 2) / max(most, kBins - 2);
+  auto bin_of = [&](const int4 &s, int at) {
+    int cost;
+    if (by_keys) {
+      const int from = a.causal ? max(at - (s.w - s.y), 0) : 0;
+      cost = (max(s.y - from, 0) * a.group + kCostRows - 1) / kCostRows;
+    } else {
+      const int last = min(at + list.rows, s.y * a.group) - 1;
+      cost = (keys_seen(last, a.group, s.y, s.w, a.causal) + kCostKeys - 1) / kCostKeys;
+    }
+    return kBins - 1 - min(static_cast<int>(cost * per_cost) + (cost > 0 ? 1 : 0), kBins - 1);
+  };
+  for (int pass = 0; pass < 2; ++pass) {
+    int run_q = 0, run_k = 0;
+    bool bad = false;
+    for (int base = 0; base < S; base += kThreads) {
+      const int s = base + t;
+      const int q = s < S ? a.offsets_q[s] : 0, q_next = s < S ? a.offsets_q[s + 1] : 0;
+      const int k = s < S ? a.offsets_k[s] : 0, k_next = s < S ? a.offsets_k[s + 1] : 0;
+      bad = bad || (s < S && (q < 0 || q_next < q || q_next > a.rows_q || k < 0 || k_next < k || k_next > a.rows_k));
+      auto clamped = [](int x, int rows) { return min(max(x, 0), rows); };
+      int top_q, top_k;
+      const int q1 = max(block_scan<true>(max(clamped(q, a.rows_q), clamped(q_next, a.rows_q)), wave, &top_q), run_q);
+      const int k1 = max(block_scan<true>(max(clamped(k, a.rows_k), clamped(k_next, a.rows_k)), wave, &top_k), run_k);
+      // a sequence's end is the next one's start
+      __syncthreads();
+      seq[t] = make_int4(q1, 0, k1, 0);
+      __syncthreads();
+      int q0, k0;
+      if (t > 0) {
+        q0 = seq[t - 1].x;
+        k0 = seq[t - 1].z;
+      } else {
+        q0 = base ? run_q : clamped(q, a.rows_q);
+        k0 = base ? run_k : clamped(k, a.rows_k);
+      }
+      __syncthreads();
+      int lk = k1 - k0;
+      if (a.lengths_k && s < S) {
+        const int n = a.lengths_k[s];
+        bad = bad || n < 0 || n > lk;
+        lk = min(max(n, 0), lk);
+      }
+      seq[t] = make_int4(q0, q1 - q0, k0, lk);
+      if (pass == 0 && which == 0 && base == 0 && t == 0) {
+        p.header[2] = q0;
+        p.header[4] = k0;
+      }
+      const int tiles = s < S ? ((by_keys ? lk : (q1 - q0) * a.group) + list.rows - 1) / list.rows : 0;
+      int total;
+      const int incl = block_scan<false>(tiles, wave, &total);
+      first[t] = incl - tiles;
+      if (t == 0) first[kThreads] = total;
+      __syncthreads();
+      for (int slot = t; slot < total; slot += kThreads) {
+        int lo = 0, hi = kThreads;  // first[lo] <= slot < first[hi]
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) / 2;
+          if (first[mid] <= slot) lo = mid; else hi = mid;
+        }
+        const int4 sq = seq[lo];
+        const int at = (slot - first[lo]) * list.rows;
+        const int place = atomicAdd(&hist[bin_of(sq, at)], 1);
+        if (pass == 1 && place < list.capacity) {
+          list.items[2 * place] = sq;
+          list.items[2 * place + 1] = make_int4(at, base + lo, 0, 0);
+        }
+      }
+      run_q = max(run_q, top_q);
+      run_k = max(run_k, top_k);
+      __syncthreads();
+    }
+    if (pass == 0) {
+      // counts to first places
+      __syncthreads();
+      const int n = hist[t];
+      int total;
+      const int incl = block_scan<false>(n, wave, &total);
+      hist[t] = incl - n;
+      if (t == 0) {
+        p.header[which] = min(total, list.capacity);
+        if (which == 0) {
+          p.header[3] = run_q;
+          p.header[5] = run_k;
+        }
+      }
+      if (bad && which == 0 && p.status) atomicOr(p.status, kStatusBadOffsets);
+      __syncthreads();
+    }
+  }
+}
+
+template <typename T, int D>
+__device__ void make_stats(const PackPrepare &p, size_t block) {
+  // a group of D / 8 lanes per row, in the rows' order by key head
+  constexpr int LANES = D / 8;
+  const size_t rows = static_cast<size_t>(p.a.kv_heads) * p.a.rows_q * p.a.group;
+  const size_t i = block * (kThreads / LANES) + threadIdx.x / LANES;
+  const int x = threadIdx.x % LANES;
+  if (i >= rows) return;
+  const size_t per = static_cast<size_t>(p.a.rows_q) * p.a.group;
+  const int kv = static_cast<int>(i / per), r = static_cast<int>(i % per);
+  const int query = r / p.a.group, head = kv * p.a.group + r % p.a.group;
+  const T *o = reinterpret_cast<const T *>(rows_base(p.o, query, head)) + 8 * x;
+  const T *g = reinterpret_cast<const T *>(rows_base(p.a.d_o, query, head)) + 8 * x;
+  float sum = 0.0f;
+  if constexpr (sizeof(T) == 2) {
+    const uint4 u = *reinterpret_cast<const uint4 *>(o), v = *reinterpret_cast<const uint4 *>(g);
+    const uint32_t us[4] = {u.x, u.y, u.z, u.w}, vs[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      sum = fmaf(__uint_as_float(us[j] << 16), __uint_as_float(vs[j] << 16), sum);
+      sum = fmaf(__uint_as_float(us[j] & 0xFFFF0000u), __uint_as_float(vs[j] & 0xFFFF0000u), sum);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; j += 4) {
+      const float4 u = *reinterpret_cast<const float4 *>(o + j), v = *reinterpret_cast<const float4 *>(g + j);
+      sum = fmaf(u.x, v.x, sum);
+      sum = fmaf(u.y, v.y, sum);
+      sum = fmaf(u.z, v.z, sum);
+      sum = fmaf(u.w, v.w, sum);
+    }
+  }
+#pragma unroll
+  for (int m = 1; m < LANES; m <<= 1) sum += __shfl_xor(sum, m);
+  if (x == 0) {
+    const float lse = p.lse[static_cast<size_t>(head) * p.a.rows_q + query];
+    p.stats[i] = lse == -INFINITY ? -INFINITY : lse * -1.4426950408889634f;  // no key: no weight
+    p.stats[rows + i] = sum;
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void pack_prepare_kernel(PackPrepare p) {
+  const int b = static_cast<int>(blockIdx.x);
+  if (b < p.n_lists)
+    make_list(p, b);
+  else
+    make_stats<T, D>(p, b - p.n_lists);
+}
+
+// O and lse, or dQ, from the parts' sums.  A group of D / 4 lanes per row.
+template <typename T, int D, bool GRAD>
+__global__ __launch_bounds__(256) void pack_join_rows_kernel(PackArgs a, PackRows out) {
+  constexpr int LANES = D / 4;
+  const size_t per = static_cast<size_t>(a.rows_q) * a.group, rows = per * a.kv_heads;
+  const size_t row = static_cast<size_t>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
+  const int x = threadIdx.x % LANES;
+  if (row >= rows) return;
+  const int kv = static_cast<int>(row / per), r = static_cast<int>(row % per);
+  const int query = r / a.group, head = kv * a.group + r % a.group;
+  if (query < a.ends[0] || query >= a.ends[1]) return;
+  const float2 *ml = reinterpret_cast<const float2 *>(a.parts + a.splits * rows * D);
+  float top = 0.0f, l = 0.0f, f = a.scale;
+  if constexpr (!GRAD) {
+    top = -INFINITY;
+    for (int p = 0; p < a.splits; ++p) top = fmaxf(top, ml[p * rows + row].x);
+    if (top == -INFINITY) top = 0.0f;
+    for (int p = 0; p < a.splits; ++p) {
+      const float2 s = ml[p * rows + row];
+      l = fmaf(s.y, __builtin_amdgcn_exp2f(s.x - top), l);
+    }
+    f = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+    if (x == 0) a.lse[static_cast<size_t>(head) * a.rows_q + query] = l > 0.0f ? (top + __log2f(l)) * kPackLn2 : l == 0.0f ? -INFINITY : l;
+  }
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int p = 0; p < a.splits; ++p) {
+    const float4 v = *reinterpret_cast<const float4 *>(a.parts + (p * rows + row) * D + 4 * x);
+    const float w = GRAD ? 1.0f : __builtin_amdgcn_exp2f(ml[p * rows + row].x - top);
+    s.x = fmaf(v.x, w, s.x);
+    s.y = fmaf(v.y, w, s.y);
+    s.z = fmaf(v.z, w, s.z);
+    s.w = fmaf(v.w, w, s.w);
+  }
+  T *to = reinterpret_cast<T *>(rows_base(out, query, head)) + 4 * x;
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(s.x * f, s.y * f), pack_bf16(s.z * f, s.w * f));
+  else
+    *reinterpret_cast<float4 *>(to) = make_float4(s.x * f, s.y * f, s.z * f, s.w * f);
+}
+
+// dK (blockIdx.y 0) and dV from the parts' sums.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void pack_join_keys_kernel(PackArgs a, PackRows dk, PackRows dv) {
+  constexpr int LANES = D / 4;
+  const size_t rows = static_cast<size_t>(a.kv_heads) * a.rows_k;
+  const size_t row = static_cast<size_t>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
+  const int x = threadIdx.x % LANES;
+  if (row >= rows) return;
+  const int head = static_cast<int>(row / a.rows_k), key = static_cast<int>(row % a.rows_k);
+  if (key < a.ends[2] || key >= a.ends[3]) return;
+  const int v = blockIdx.y;
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int p = 0; p < a.splits; ++p) {
+    const float4 y = *reinterpret_cast<const float4 *>(a.parts + ((2 * static_cast<size_t>(p) + v) * rows + row) * D + 4 * x);
+    s.x += y.x;
+    s.y += y.y;
+    s.z += y.z;
+    s.w += y.w;
+  }
+  const float f = v ? 1.0f : a.scale;
+  T *to = reinterpret_cast<T *>(rows_base(v ? dv : dk, key, head)) + 4 * x;
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(s.x * f, s.y * f), pack_bf16(s.z * f, s.w * f));
+  else
+    *reinterpret_cast<float4 *>(to) = make_float4(s.x * f, s.y * f, s.z * f, s.w * f);
+}
+
+#define PACK_TRY(x)                  \
+  do {                               \
+    const hipError_t e_ = (x);       \
+    if (e_ != hipSuccess) return e_; \
+  } while (0)
+
+// Parts that an item's tiles are cut into: as many, up to 16 of `least` tiles or more,
+// as make the launch's rounds shortest, a part costing about 4% of an item more (its
+// start, its sums).  `resident`: the blocks that the chip holds at once.
+int parts_of(long long blocks, long long tiles, int least, int resident) {
+  constexpr int kMost = 16;
+  int best = 1;
+  double shortest = 0.0;
+  for (int s = 1; s <= kMost && (s == 1 || static_cast<long long>(s) * least <= tiles); ++s) {
+    const double rounds = static_cast<double>((blocks * s + resident - 1) / resident) * (1.0 / s + 0.04);
+    if (s == 1 || rounds < shortest) {
+      shortest = rounds;
+      best = s;
+    }
+  }
+  return best;
+}
+
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+template <typename T, int D>
+hipError_t prepare(const PackArgs &a, const PackCall &c, bool grad, hipStream_t s) {
+  PackPrepare p{};
+  p.a = a;
+  p.lists[0] = c.by_rows;
+  p.lists[1] = c.by_keys;
+  p.n_lists = grad ? 2 : 1;
+  p.header = c.header;
+  p.status = c.status;
+  p.d = D;
+  size_t blocks = p.n_lists;
+  if (grad) {
+    p.o = c.o;
+    p.lse = c.lse;
+    p.stats = const_cast<float *>(a.stats);
+    const size_t rows = static_cast<size_t>(a.kv_heads) * a.rows_q * a.group, per = kThreads / (D / 8);
+    blocks += (rows + per - 1) / per;
+  }
+  hipLaunchKernelGGL((pack_prepare_kernel<T, D>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, s, p);
+  return hipGetLastError();
+}
+
+template <typename T, int D, bool GRAD>
+hipError_t join_rows(const PackArgs &a, const PackRows &out, hipStream_t s) {
+  const size_t rows = static_cast<size_t>(a.kv_heads) * a.rows_q * a.group, per = 256 / (D / 4);
+  hipLaunchKernelGGL((pack_join_rows_kernel<T, D, GRAD>), dim3(static_cast<unsigned>((rows + per - 1) / per)), dim3(256), 0, s, a, out);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t forward(PackArgs a, const PackCall &c, hipStream_t s) {
+  PACK_TRY((prepare<T, D>(a, c, false, s)));
+  a.list = c.by_rows;
+  a.count = c.header;
+  a.splits = c.splits_rows;
+  PACK_TRY(sizeof(T) == 2 ? packed_queries(a, D, false, c.o, s) : packed_queries_f32(a, D, false, c.o, s));
+  return a.splits > 1 ? join_rows<T, D, false>(a, c.o, s) : hipSuccess;
+}
+
+template <typename T, int D>
+hipError_t backward(PackArgs a, const PackCall &c, hipStream_t s) {
+  PACK_TRY((prepare<T, D>(a, c, true, s)));
+  a.list = c.by_rows;
+  a.count = c.header;
+  a.splits = c.splits_rows;
+  PACK_TRY(sizeof(T) == 2 ? packed_queries(a, D, true, c.dq, s) : packed_queries_f32(a, D, true, c.dq, s));
+  if (a.splits > 1) PACK_TRY((join_rows<T, D, true>(a, c.dq, s)));
+  a.list = c.by_keys;
+  a.count = c.header + 1;
+  a.splits = c.splits_keys;
+  PACK_TRY(sizeof(T) == 2 ? packed_keys(a, D, c.dk, c.dv, s) : packed_keys_f32(a, D, c.dk, c.dv, s));
+  if (a.splits > 1) {
+    const size_t rows = static_cast<size_t>(a.kv_heads) * a.rows_k, per = 256 / (D / 4);
+    hipLaunchKernelGGL((pack_join_keys_kernel<T, D>), dim3(static_cast<unsigned>((rows + per - 1) / per), 2), dim3(256), 0, s, a, c.dk, c.dv);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+size_t packed_workspace(const scope_pack *p, void *base, PackArgs *a, PackCall *c) {
+  const bool bf16 = p->dtype == SCOPE_BF16;
+  const int group = p->heads / p->kv_heads;
+  const long long rows = static_cast<long long>(p->rows_q) * group, keys = p->rows_k;
+  char *at = static_cast<char *>(base);
+  size_t used = 0;
+  auto take = [&](size_t bytes) {
+    char *q = at ? at + used : nullptr;
+    used = (used + bytes + 255) / 256 * 256;
+    return q;
+  };
+  PackList by_rows{nullptr, bf16 ? kPackRows : kPackRowsF32, 0}, by_keys{nullptr, bf16 ? kPackKeys : kPackRowsF32, 0};
+  by_rows.capacity = static_cast<int>(rows / by_rows.rows + p->sequences);
+  by_keys.capacity = static_cast<int>(keys / by_keys.rows + p->sequences);
+  int32_t *header = reinterpret_cast<int32_t *>(take(64));
+  by_rows.items = reinterpret_cast<int4 *>(take(32 * static_cast<size_t>(by_rows.capacity)));
+  by_keys.items = reinterpret_cast<int4 *>(take(32 * static_cast<size_t>(by_keys.capacity)));
+  float *stats = reinterpret_cast<float *>(take(8 * static_cast<size_t>(p->kv_heads) * rows));
+  // items that sequences of one length would give
+  const long long items_q = p->kv_heads * ceil_div(ceil_div(rows, p->sequences), by_rows.rows) * p->sequences;
+  const long long items_k = p->kv_heads * ceil_div(ceil_div(keys, p->sequences), by_keys.rows) * p->sequences;
+  const int tile = bf16 ? 64 : 32;
+  const int splits_rows = parts_of(items_q, ceil_div(ceil_div(keys, p->sequences), tile), 4, bf16 ? 256 : 512);
+  const int splits_keys = parts_of(items_k, ceil_div(ceil_div(rows, p->sequences), 32), 8, 512);
+  const size_t row_parts = splits_rows > 1 ? static_cast<size_t>(splits_rows) * p->kv_heads * rows * (4 * p->d + 8) : 0;
+  const size_t key_parts = splits_keys > 1 ? static_cast<size_t>(splits_keys) * 2 * p->kv_heads * keys * 4 * p->d : 0;
+  float *parts = reinterpret_cast<float *>(take(row_parts > key_parts ? row_parts : key_parts));
+  if (a) {
+    a->stats = stats;
+    a->parts = parts;
+    a->ends = header + 2;
+    c->by_rows = by_rows;
+    c->by_keys = by_keys;
+    c->header = header;
+    c->splits_rows = splits_rows;
+    c->splits_keys = splits_keys;
+  }
+  return used;
+}
+
+bool packed_launchable(const scope_pack *p) {
+  PackArgs a{};
+  PackCall c{};
+  packed_workspace(p, nullptr, &a, &c);
+  auto fits = [](long long capacity, long long heads, int splits, int threads) {
+    return (capacity + kXcds - 1) / kXcds * kXcds * heads * splits * threads < (1LL << 32);
+  };
+  return fits(c.by_rows.capacity, p->kv_heads, c.splits_rows, 512) && fits(c.by_keys.capacity, p->kv_heads, c.splits_keys, 256) &&
+         static_cast<long long>(p->heads) * p->rows_q * (p->d / 4) < (1LL << 32) - 1024 &&
+         static_cast<long long>(p->kv_heads) * p->rows_k * (p->d / 4) < (1LL << 32) - 1024;
+}
+
+hipError_t packed_forward(const PackArgs &a, const PackCall &c, hipStream_t s) {
+  if (c.bf16) return c.d == 128 ? forward<uint16_t, 128>(a, c, s) : forward<uint16_t, 64>(a, c, s);
+  return c.d == 128 ? forward<float, 128>(a, c, s) : forward<float, 64>(a, c, s);
+}
+hipError_t packed_backward(const PackArgs &a, const PackCall &c, hipStream_t s) {
+  if (c.bf16) return c.d == 128 ? backward<uint16_t, 128>(a, c, s) : backward<uint16_t, 64>(a, c, s);
+  return c.d == 128 ? backward<float, 128>(a, c, s) : backward<float, 64>(a, c, s);
+}
+
+}  // namespace scope

@@ -1,0 +1,342 @@
+// Attention over packed sequences by rows, bf16 inputs: the forward with row
+// statistics, and dQ (packed_plan.hip has the formulas).
+//
+// A block runs an item's up to 256 rows (query, head of the group) of a key head, a
+// wave 32 of them, over the keys that its last row sees, 64 at a time: K and V tiles
+// are brought into LDS by the buffer unit while the tile before is computed.  A
+// wave's tile is
+//   S^T = K_tile . Q^T                   keys x rows, a row per lane column
+//   online softmax in fp32, exp2 domain; weights rounded to bf16 for
+//   O^T += V_tile^T . P^T                (transposing LDS reads of V)
+// and for the gradient, p recomputed from the row's log-sum-exp,
+//   dP^T = V_tile . dO^T, ds = p (dP - D), dQ^T += K_tile^T . ds^T
+// with ds as two bf16 terms, the second what rounding the first left: a row's ds sum
+// to zero, so dQ is a difference of larger sums and keeps more of their rounding.
+#include "attention_tile.h"
+#include "packed.h"
+
+namespace scope {
+
+namespace {
+
+constexpr float kLag = 8.0f;  // the running maximum may lag by 2^8
+static_assert(kPackRows == kBM, "rows of a block");
+
+template <int D, bool GRAD>
+__global__ __launch_bounds__(kNW * 64)
+__attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel(PackArgs a, PackRows out) {
+  constexpr int CH = D / 8;        // 16-byte chunks per row
+  constexpr int RPL = 64 / CH;     // rows per load
+  constexpr int NG = kBN / kNW / RPL;  // loads per wave, tile and matrix
+  __shared__ __attribute__((aligned(16))) uint16_t K0[kBN * D], K1[kBN * D], V0[kBN * D], V1[kBN * D];
+  int h, rank;
+  if (!pack_place(static_cast<int>(blockIdx.x), a.kv_heads, a.count[0], &h, &rank)) return;
+  const int part = static_cast<int>(blockIdx.y);
+  const int4 sq = a.list.items[2 * rank];
+  const int row0 = a.list.items[2 * rank + 1].x;
+  const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
+  const int t = threadIdx.x, lane = t & 63, l32 = lane & 31, hf = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(t >> 6);
+  TileReader<D> at(lane);
+  const int own = row0 + 32 * w + l32, row = min(own, rows - 1);
+  const bool valid = own < rows, active = row0 + 32 * w < rows;
+  const int query = row / a.group, member = row - query * a.group;
+  const size_t stat = (static_cast<size_t>(h) * a.rows_q + q0) * a.group + row;  // of (key head, row)
+  // keys that this row sees, and the wave's fewest and most
+  const int seen = keys_seen(row, a.group, lq, lk, a.causal);
+  const int fewest = __builtin_amdgcn_readlane(seen, 0), most = __builtin_amdgcn_readlane(seen, 31);
+  const int block_most = keys_seen(min(row0 + kBM, rows) - 1, a.group, lq, lk, a.causal);
+
+  bf16x8 qf[D / 16], gf[GRAD ? D / 16 : 1];
+  {
+    const uint16_t *q = reinterpret_cast<const uint16_t *>(rows_base(a.q, q0, h * a.group) + query * a.q.row + member * a.q.head);
+    const uint16_t *g = reinterpret_cast<const uint16_t *>(rows_base(a.d_o, q0, h * a.group) + query * a.d_o.row + member * a.d_o.head);
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) {
+      qf[x] = as_bf16x8(valid ? load8<true>(q, 16 * x + 8 * hf) : make_uint4(0, 0, 0, 0));
+      if constexpr (GRAD) gf[x] = as_bf16x8(valid ? load8<true>(g, 16 * x + 8 * hf) : make_uint4(0, 0, 0, 0));
+    }
+  }
+  float neg_lse = -INFINITY, delta = 0.0f;
+  if (GRAD && valid) {
+    neg_lse = a.stats[stat];
+    delta = a.stats[static_cast<size_t>(a.kv_heads) * a.rows_q * a.group + stat];
+  }
+
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[db][e] = 0.0f;
+  float m_run = -INFINITY, l_run = 0.0f;
+
+  // the part's tiles
+  const int all = (block_most + kBN - 1) / kBN, per = (all + a.splits - 1) / a.splits;
+  const int first = min(part * per, all), last = min(first + per, all);
+  const int last_own = active ? min(last, (most + kBN - 1) / kBN) : 0;
+
+  const uint32_t k_row = static_cast<uint32_t>(a.k.row), v_row = static_cast<uint32_t>(a.v.row);
+  const __amdgpu_buffer_rsrc_t rk = pack_resource(rows_base(a.k, k0, h), lk ? span(a.k, lk, 1, 2 * D) : 0);
+  const __amdgpu_buffer_rsrc_t rv = pack_resource(rows_base(a.v, k0, h), lk ? span(a.v, lk, 1, 2 * D) : 0);
+  // wave w brings rows 8 w .. 8 w + 7 of a tile, RPL rows (1 KB) per load; rows past
+  // the last key repeat it, with no weight
+  auto bring = [&](const __amdgpu_buffer_rsrc_t &from, uint32_t stride, uint16_t *tile, int index) {
+    const bool whole = (index + 1) * kBN <= lk;
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const int r0 = kBN / kNW * w + RPL * i, r = r0 + lane / CH;
+      const int col = 16 * ((lane % CH) ^ tile_swizzle<D>(r));
+      if (whole)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16, r * stride + col, index * kBN * stride, 0, 0);
+      else
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16, min(index * kBN + r, lk - 1) * stride + col, 0, 0, 0);
+    }
+  };
+  auto scores = [&](const uint16_t *kt, int kb) {
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x)
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.row(kt + 32 * kb * D, x), qf[x], s, 0, 0, 0);
+    return s;
+  };
+  // -inf for the keys from `from` on that the row does not see
+  auto cut = [&](f32x16 &s, int from) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (from + 8 * (e >> 2) + 4 * hf + (e & 3) >= seen) s[e] = -INFINITY;
+  };
+  auto add = [&](const uint16_t *tile, const bf16x8 (&p)[2]) {
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.columns(tile + 16 * s2 * D, db), p[s2], acc[db], 0, 0, 0);
+  };
+  // of two terms
+  auto add2 = [&](const uint16_t *tile, const bf16x8 (&p)[2], const bf16x8 (&rest)[2]) {
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        const bf16x8 k = at.columns(tile + 16 * s2 * D, db);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, p[s2], acc[db], 0, 0, 0);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, rest[s2], acc[db], 0, 0, 0);
+      }
+  };
+
+  auto forward_tile = [&](int index, const uint16_t *kt, const uint16_t *vt) {
+    f32x16 s[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[kb][e] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.row(kt + 32 * kb * D, x), qf[x], s[kb], 0, 0, 0);
+    interleave<D / 8, 1, 0>();
+    if ((index + 1) * kBN > fewest) {
+      cut(s[0], index * kBN);
+      cut(s[1], index * kBN + 32);
+    }
+    float mx0 = fmaxf(s[0][0], s[0][1]), mx1 = fmaxf(s[1][0], s[1][1]);
+#pragma unroll
+    for (int e = 2; e < 16; e += 2) {
+      mx0 = fmaxf(fmaxf(mx0, s[0][e]), s[0][e + 1]);
+      mx1 = fmaxf(fmaxf(mx1, s[1][e]), s[1][e + 1]);
+    }
+    float mx = fmaxf(mx0, mx1);
+    {
+      // the other half-wave holds the row's other keys
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    }
+    // a row rescales on its own, where its maximum falls too far behind
+    const float mt = mx * a.scale_log2;
+    const bool behind = mt > m_run + kLag;
+    if (__ballot(behind)) {
+      const float m_new = behind ? fmaxf(m_run, mt) : m_run;
+      const float alpha = behind ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.0f;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[db][e] *= alpha;
+      m_run = m_new;
+    }
+    // no logit above -inf so far: weights of 0, where inf - inf would be NaN
+    const float neg_m = m_run == -INFINITY ? 0.0f : -m_run;
+    bf16x8 pk[2][2];
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto weights = [&](int kb) {
+      float p[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(fmaf(s[kb][e], a.scale_log2, neg_m));
+        sum[e & 3] += p[e];
+      }
+      pk[kb][0] = pack8(p);
+      pk[kb][1] = pack8(p + 8);
+    };
+    weights(0);
+    asm volatile("" : "+v"(pk[0][0]), "+v"(pk[0][1]), "+v"(at.col_at));
+    // the second block's weights beside the first's product
+    add(vt, pk[0]);
+    weights(1);
+    interleave<D / 16, 2, D == 128 ? 7 : 14>();
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(acc[db]));
+    asm volatile("" : "+v"(pk[1][0]), "+v"(pk[1][1]), "+v"(at.col_at));
+    add(vt + 32 * D, pk[1]);
+    interleave<D / 16, 2, 0>();
+    l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  };
+
+  // In phases, each with matrix products next to the vector work of another block of
+  // keys; the empty asm statements end a phase as in attention_keys.hip.
+  auto grad_tile = [&](int index, const uint16_t *kt, const uint16_t *vt) {
+    f32x16 s[2], dp[2];
+    float p[2][16];
+    bf16x8 dsk[2][2], rest[2][2];
+    const bool edge = (index + 1) * kBN > fewest;
+    auto weights = [&](int kb) {  // p beside dP^T
+      f32x16 x;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.row(vt + 32 * kb * D, i), gf[i], x, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) p[kb][e] = __builtin_amdgcn_exp2f(fmaf(s[kb][e], a.scale_log2, neg_lse));
+      dp[kb] = x;
+      interleave<D / 16, 1, D == 128 ? 4 : 8>();
+      asm volatile("" : "+v"(dp[kb]), "+v"(at.row_at), "+v"(at.col_at));
+    };
+    auto gradient = [&](int kb) {  // ds
+      float ds[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) ds[e] = p[kb][e] * (dp[kb][e] - delta);
+      dsk[kb][0] = pack8(ds);
+      dsk[kb][1] = pack8(ds + 8);
+      // what the rounding left
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint4 u = __builtin_bit_cast(uint4, dsk[kb][i]);
+        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          ds[8 * i + 2 * j] -= __uint_as_float(x[j] << 16);
+          ds[8 * i + 2 * j + 1] -= __uint_as_float(x[j] & 0xFFFF0000u);
+        }
+      }
+      rest[kb][0] = pack8(ds);
+      rest[kb][1] = pack8(ds + 8);
+    };
+    s[0] = scores(kt, 0);
+    interleave<D / 16, 1, 0>();
+    asm volatile("" : "+v"(s[0]), "+v"(at.row_at));
+    if (edge) cut(s[0], index * kBN);
+    weights(0);
+    gradient(0);
+    s[1] = scores(kt, 1);
+    interleave<D / 16, 1, D == 128 ? 5 : 10>();
+    asm volatile("" : "+v"(s[1]), "+v"(dsk[0][0]), "+v"(dsk[0][1]), "+v"(rest[0][0]), "+v"(rest[0][1]), "+v"(at.row_at));
+    // d = 64 has registers for one block of keys' ds
+    if constexpr (D == 64) {
+      add2(kt, dsk[0], rest[0]);
+      interleave<D / 8, 1, 0>();
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(acc[db]));
+    }
+    if (edge) cut(s[1], index * kBN + 32);
+    weights(1);
+    gradient(1);
+    if constexpr (D == 128) {
+      add2(kt, dsk[0], rest[0]);
+      interleave<D / 8, 1, 4>();
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(acc[db]));
+    }
+    asm volatile("" : "+v"(dsk[1][0]), "+v"(dsk[1][1]), "+v"(rest[1][0]), "+v"(rest[1][1]), "+v"(at.col_at));
+    add2(kt + 32 * D, dsk[1], rest[1]);
+    interleave<D / 8, 1, 0>();
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(acc[db]));
+    asm volatile("" : "+v"(at.row_at), "+v"(at.col_at));
+  };
+
+  // one step: tile T computed while tile T + 1 is brought into the free buffers; every
+  // wave's loads land before the barrier
+  auto step = [&](int index, const uint16_t *kc, const uint16_t *vc, uint16_t *kn, uint16_t *vn) {
+    if (index + 1 < last) {
+      bring(rk, k_row, kn, index + 1);
+      bring(rv, v_row, vn, index + 1);
+    }
+    if (index < last_own) {
+      if constexpr (GRAD)
+        grad_tile(index, kc, vc);
+      else
+        forward_tile(index, kc, vc);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+    __syncthreads();
+  };
+  if (first < last) {
+    bring(rk, k_row, K0, first);
+    bring(rv, v_row, V0, first);
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);
+  __syncthreads();
+  for (int index = first; index < last; index += 2) {
+    step(index, K0, V0, K1, V1);
+    if (index + 1 < last) step(index + 1, K1, V1, K0, V0);
+  }
+
+  const float l = l_run + __shfl_xor(l_run, 32);  // the halves of a row's sum
+  if (!valid) return;
+  if (a.splits > 1) {  // the part's sums, and the forward's maximum and normaliser
+    const size_t total = static_cast<size_t>(a.kv_heads) * a.rows_q * a.group, i = part * total + stat;
+    float *to = a.parts + i * D + 4 * hf;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *reinterpret_cast<float4 *>(to + 32 * db + 8 * x) =
+            make_float4(acc[db][4 * x], acc[db][4 * x + 1], acc[db][4 * x + 2], acc[db][4 * x + 3]);
+    if (!GRAD && hf == 0) reinterpret_cast<float2 *>(a.parts + a.splits * total * D)[i] = make_float2(m_run, l);
+    return;
+  }
+  float f = a.scale;
+  if constexpr (!GRAD) {
+    f = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+    if (hf == 0)
+      a.lse[static_cast<size_t>(h * a.group + member) * a.rows_q + q0 + query] =
+          l > 0.0f ? (m_run + __log2f(l)) * kPackLn2 : l == 0.0f ? -INFINITY : l;
+  }
+  uint16_t *to = reinterpret_cast<uint16_t *>(rows_base(out, q0, h * a.group) + query * out.row + member * out.head) + 4 * hf;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *reinterpret_cast<uint2 *>(to + 32 * db + 8 * x) = make_uint2(pack_bf16(acc[db][4 * x] * f, acc[db][4 * x + 1] * f),
+                                                                     pack_bf16(acc[db][4 * x + 2] * f, acc[db][4 * x + 3] * f));
+}
+
+template <int D, bool GRAD>
+hipError_t run(const PackArgs &a, const PackRows &out, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(kXcds) * a.kv_heads * ((a.list.capacity + kXcds - 1) / kXcds), a.splits);
+  hipLaunchKernelGGL((packed_queries_kernel<D, GRAD>), grid, dim3(kNW * 64), 0, s, a, out);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t packed_queries(const PackArgs &a, int d, bool grad, const PackRows &out, hipStream_t s) {
+  if (d == 128) return grad ? run<128, true>(a, out, s) : run<128, false>(a, out, s);
+  return grad ? run<64, true>(a, out, s) : run<64, false>(a, out, s);
+}
+
+}  // namespace scope
