@@ -67,6 +67,7 @@ int32_t check_pack(const scope_pack *p) {
   if (p->heads > 65535 || p->rows_q > kMaxRows || p->rows_k > kMaxRows || p->sequences > 65536) return SCOPE_ERR_UNSUPPORTED;
   if (static_cast<int64_t>(p->heads) * p->rows_q >= (1LL << 31) || static_cast<int64_t>(p->kv_heads) * p->rows_k >= (1LL << 31))
     return SCOPE_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(p->heads / p->kv_heads) * p->rows_q > (1LL << 30)) return SCOPE_ERR_UNSUPPORTED;  // costs of 32 bits
   if (!scope::packed_launchable(p)) return SCOPE_ERR_UNSUPPORTED;
   return SCOPE_OK;
 }
@@ -114,7 +115,7 @@ void set_pack(const scope_pack *p, const int32_t *offsets_q, const int32_t *offs
   a->scale_log2 = a->scale * 1.4426950408889634f;
   c->d = p->d;
   c->bf16 = p->dtype == SCOPE_BF16;
-  c->status = status;
+  a->status = status;
   scope::packed_workspace(p, workspace, a, c);
 }
 
@@ -251,7 +252,7 @@ int32_t scope_packed_attention_backward(const scope_pack *pack, const void *q, c
   const Tensor t[] = {{q, q_strides, H, nq, false},   {o, o_strides, H, nq, false},   {d_o, d_o_strides, H, nq, false},
                       {dq, dq_strides, H, nq, true},  {k, k_strides, G, nk, false},   {v, v_strides, G, nk, false},
                       {dk, dk_strides, G, nk, true},  {dv, dv_strides, G, nk, true}};
-  scope::PackRows *const rows[] = {&a.q, &c.o, &a.d_o, &c.dq, &a.k, &a.v, &c.dk, &c.dv};
+  scope::PackRows *const rows[] = {&a.q, &a.o, &a.d_o, &c.dq, &a.k, &a.v, &c.dk, &c.dv};
   for (int i = 0; i < 8; ++i)
     if ((st = check_rows(t[i], pack->d, el, i < 4 ? group : 1, rows[i]))) return st;
   if ((st = check_apart(t, 8, pack->d, el))) return st;
@@ -260,7 +261,7 @@ int32_t scope_packed_attention_backward(const scope_pack *pack, const void *q, c
   if (!(scale == scale) || isinf(scale)) return SCOPE_ERR_INVALID_ARGUMENT;
   if ((st = check_workspace(pack, workspace, ws_bytes))) return st;
   set_pack(pack, offsets_q, offsets_k, nullptr, scale, workspace, dev_status, &a, &c);
-  c.lse = lse;
+  a.lse = const_cast<float *>(lse);
   return scope::packed_backward(a, c, static_cast<hipStream_t>(stream)) == hipSuccess ? SCOPE_OK : SCOPE_ERR_HIP;
 }
 

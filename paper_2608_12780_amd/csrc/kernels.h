@@ -364,21 +364,24 @@ struct PackList {
 };
 struct PackArgs {
   int kv_heads, group, rows_q, rows_k, sequences, causal;
-  PackRows q, k, v, d_o;
+  PackRows q, k, v, o, d_o;  // o: gradients
   const int32_t *offsets_q, *offsets_k, *lengths_k;
   float scale, scale_log2;
-  float *lse;             // [heads][rows_q]
-  PackList list;          // of this launch
-  const int32_t *count;   // items in it
-  const int32_t *ends;    // first and last query row, first and last key row of all sequences
+  float *lse;             // [heads][rows_q]; gradients: read
+  int32_t *status;
+  // more than 64 sequences: the items of this launch and their number, and first and
+  // last query row, first and last key row of all sequences
+  PackList list;
+  const int32_t *count;
+  const int32_t *ends;
   // Parts that an item's tiles are cut into, and with more than one their sums: O or
   // dQ [part][kv_heads][rows_q * group][d], then of the forward (maximum, normaliser);
   // dK, dV [part][2][kv_heads][rows_k][d].
   int splits;
   float *parts;
   // [2][kv_heads][rows_q * group]: -lse in the exp2 domain (-inf where no key is seen)
-  // and <do, o>, by query and head of the group
-  const float *stats;
+  // and <do, o>, by query and head of the group: dQ's kernel writes them for dK and dV
+  float *stats;
 };
 struct PackCall {
   int d;
@@ -386,26 +389,20 @@ struct PackCall {
   PackRows o, dq, dk, dv;
   PackList by_rows, by_keys;
   int splits_rows, splits_keys;
-  bool tokens;            // few queries a sequence: packed_tokens.hip
-  int slots;              // its work slots of a key head
-  int32_t *header, *status;
-  const float *lse;
+  int32_t *header;
 };
 // Lays the workspace out (base null: only its size) and chooses the launches.
 size_t packed_workspace(const scope_pack *p, void *base, PackArgs *a, PackCall *c);
 bool packed_launchable(const scope_pack *p);
 hipError_t packed_forward(const PackArgs &a, const PackCall &c, hipStream_t s);
 hipError_t packed_backward(const PackArgs &a, const PackCall &c, hipStream_t s);
-// The kernels: O (grad false) or dQ, by rows; dK and dV, by keys; few queries.
+// The kernels: O (grad false) or dQ, by rows; dK and dV, by keys.
 hipError_t packed_queries(const PackArgs &a, int d, bool grad, const PackRows &out, hipStream_t s);
 hipError_t packed_keys(const PackArgs &a, int d, const PackRows &dk, const PackRows &dv, hipStream_t s);
 hipError_t packed_queries_f32(const PackArgs &a, int d, bool grad, const PackRows &out, hipStream_t s);
 hipError_t packed_keys_f32(const PackArgs &a, int d, const PackRows &dk, const PackRows &dv, hipStream_t s);
-hipError_t packed_tokens(const PackArgs &a, int d, const PackRows &out, int slots, int32_t *status, hipStream_t s);
-constexpr int kPackRows = 256;       // rows of a bf16 item by queries
+constexpr int kPackRows = 128;       // rows of a bf16 item by queries
 constexpr int kPackKeys = 128;       // keys of a bf16 item by keys
 constexpr int kPackRowsF32 = 64;     // rows, or keys, of an fp32 item
-constexpr int kPackTokenRows = 32;   // rows of an item of few queries
-constexpr int kPackTokenKeys = 512;  // and its keys
 
 }  // namespace scope

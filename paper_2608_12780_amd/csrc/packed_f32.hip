@@ -17,11 +17,10 @@ __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_f32_kernel(PackArgs a, PackRows out) {
   typedef TileF32<D> T;
   __shared__ __attribute__((aligned(16))) float K0[T::kFloats], K1[T::kFloats], V0[T::kFloats], V1[T::kFloats];
-  int h, rank;
-  if (!pack_place(static_cast<int>(blockIdx.x), a.kv_heads, a.count[0], &h, &rank)) return;
+  int h, row0;
+  int4 sq;
+  if (!pack_item<false, kPackRowsF32>(a, &h, &sq, &row0)) return;
   const int part = static_cast<int>(blockIdx.y);
-  const int4 sq = a.list.items[2 * rank];
-  const int row0 = a.list.items[2 * rank + 1].x;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -38,9 +37,24 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_f32_ke
   float neg_lse = -INFINITY, delta = 0.0f;
   if constexpr (GRAD) {
     load_row<D>(gf, reinterpret_cast<const float *>(rows_base(a.d_o, q0, h * a.group) + query * a.d_o.row + member * a.d_o.head), valid, g);
+    float4 of[D / 16];
+    load_row<D>(of, reinterpret_cast<const float *>(rows_base(a.o, q0, h * a.group) + query * a.o.row + member * a.o.head), valid, g);
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      delta = fmaf(of[s].x, gf[s].x, delta);
+      delta = fmaf(of[s].y, gf[s].y, delta);
+      delta = fmaf(of[s].z, gf[s].z, delta);
+      delta = fmaf(of[s].w, gf[s].w, delta);
+    }
+    delta += __shfl_xor(delta, 16);
+    delta += __shfl_xor(delta, 32);
     if (valid) {
-      neg_lse = a.stats[stat];
-      delta = a.stats[static_cast<size_t>(a.kv_heads) * a.rows_q * a.group + stat];
+      const float lse = a.lse[static_cast<size_t>(h * a.group + member) * a.rows_q + q0 + query];
+      neg_lse = lse == -INFINITY ? -INFINITY : lse * -1.4426950408889634f;  // no key: no weight
+      if (g == 0 && part == 0) {
+        a.stats[stat] = neg_lse;
+        a.stats[static_cast<size_t>(a.kv_heads) * a.rows_q * a.group + stat] = delta;
+      }
     }
   }
   f32x4 acc[D / 16];
@@ -50,8 +64,8 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_f32_ke
 
   // the part's tiles
   const int all = (block_most + kTile - 1) / kTile, per = (all + a.splits - 1) / a.splits;
-  const int first = min(part * per, all), last = min(first + per, all);
-  const int last_own = active ? min(last, (most + kTile - 1) / kTile) : 0;
+  const int first = scalar(min(part * per, all)), last = scalar(min(first + per, all));
+  const int last_own = scalar(active ? min(last, (most + kTile - 1) / kTile) : 0);
   const uint32_t k_row = static_cast<uint32_t>(a.k.row), v_row = static_cast<uint32_t>(a.v.row);
   const __amdgpu_buffer_rsrc_t rk = pack_resource(rows_base(a.k, k0, h), lk ? span(a.k, lk, 1, 4 * D) : 0);
   const __amdgpu_buffer_rsrc_t rv = pack_resource(rows_base(a.v, k0, h), lk ? span(a.v, lk, 1, 4 * D) : 0);
@@ -147,11 +161,10 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_f32_kerne
   // attention_keys.hip)
   constexpr int kQ = T::kFloats + 2 * 64;
   __shared__ __attribute__((aligned(16))) float Q0[kQ], Q1[kQ], G0[T::kFloats], G1[T::kFloats];
-  int h, rank;
-  if (!pack_place(static_cast<int>(blockIdx.x), a.kv_heads, a.count[0], &h, &rank)) return;
+  int h, key0;
+  int4 sq;
+  if (!pack_item<true, kPackRowsF32>(a, &h, &sq, &key0)) return;
   const int part = static_cast<int>(blockIdx.y);
-  const int4 sq = a.list.items[2 * rank];
-  const int key0 = a.list.items[2 * rank + 1].x;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -171,8 +184,8 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_f32_kerne
   const int tiles_all = (rows + kTile - 1) / kTile;
   const int from_tile = min((a.causal ? max(key0 - (lk - lq), 0) * a.group : 0) / kTile, tiles_all);
   const int per = (tiles_all - from_tile + a.splits - 1) / a.splits;
-  const int first = min(from_tile + part * per, tiles_all), last = min(first + per, tiles_all);
-  const int first_own = active ? sees_least / kTile : last;
+  const int first = scalar(min(from_tile + part * per, tiles_all)), last = scalar(min(first + per, tiles_all));
+  const int first_own = scalar(active ? sees_least / kTile : last);
   const __amdgpu_buffer_rsrc_t rq = pack_resource(rows_base(a.q, q0, h * a.group), lq ? span(a.q, lq, a.group, 4 * D) : 0);
   const __amdgpu_buffer_rsrc_t rg = pack_resource(rows_base(a.d_o, q0, h * a.group), lq ? span(a.d_o, lq, a.group, 4 * D) : 0);
   const __amdgpu_buffer_rsrc_t rs = pack_resource(

@@ -35,11 +35,10 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_kernel(Pa
   __shared__ __attribute__((aligned(256))) uint16_t Q0[kStats + 4 * kPlane], Q1[kStats + 4 * kPlane], G0[kRowTile * D], G1[kRowTile * D];
   constexpr bool VLDS = D == 128;
   __shared__ __attribute__((aligned(16))) uint16_t Vs[VLDS ? kPackKeys * D : 8];
-  int h, rank;
-  if (!pack_place(static_cast<int>(blockIdx.x), a.kv_heads, a.count[0], &h, &rank)) return;
+  int h, key0;
+  int4 sq;
+  if (!pack_item<true, kPackKeys>(a, &h, &sq, &key0)) return;
   const int part = static_cast<int>(blockIdx.y);
-  const int4 sq = a.list.items[2 * rank];
-  const int key0 = a.list.items[2 * rank + 1].x;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -75,9 +74,9 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_kernel(Pa
   const int tiles_all = (rows + kRowTile - 1) / kRowTile;
   const int from_tile = min((a.causal ? max(key0 - (lk - lq), 0) * a.group : 0) / kRowTile, tiles_all);
   const int per = (tiles_all - from_tile + a.splits - 1) / a.splits;
-  const int first = min(from_tile + part * per, tiles_all), last = min(first + per, tiles_all);
+  const int first = scalar(min(from_tile + part * per, tiles_all)), last = scalar(min(first + per, tiles_all));
   // this wave's first tile
-  const int first_own = active ? sees_least / kRowTile : last;
+  const int first_own = scalar(active ? sees_least / kRowTile : last);
 
   const __amdgpu_buffer_rsrc_t rq = pack_resource(rows_base(a.q, q0, h * a.group), lq ? span(a.q, lq, a.group, 2 * D) : 0);
   const __amdgpu_buffer_rsrc_t rg = pack_resource(rows_base(a.d_o, q0, h * a.group), lq ? span(a.d_o, lq, a.group, 2 * D) : 0);

@@ -1,5 +1,5 @@
-// Attention over packed sequences (calls 10 and 11): the work lists, the rows'
-// statistics for the gradients, the joins of parts, and the order of launches.
+// Attention over packed sequences (calls 10 and 11): the work lists of many sequences,
+// the joins of parts, and the order of launches.
 //
 // With n queries and m keys of a sequence, key head h and the query heads of its
 // group side by side as rows (query, head):
@@ -11,8 +11,8 @@
 // order (dq by rows, dk and dv by keys).
 //
 // Sequence lengths are on the device, so the host launches as many blocks as any
-// lengths could need, and one block makes the list of those that there are, longest
-// first.
+// lengths could need; they find their items, longest first, from the offsets (packed.h),
+// or from a list where there are more than 64 sequences.
 #include <math.h>
 
 #include "common.h"
@@ -26,19 +26,11 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kBins = 1024;
-constexpr int kStatusBadOffsets = 16;
-constexpr int kCostKeys = 64, kCostRows = 32;  // a unit of an item's cost
 
-struct PackPrepare {
+struct PackLists {
   PackArgs a;
   PackList lists[2];
-  int n_lists;
   int32_t *header;   // counts, ends
-  int32_t *status;
-  int d;
-  PackRows o;        // gradients: the statistics' inputs
-  const float *lse;
-  float *stats;
 };
 
 // Inclusive scan over the block's threads; `total` receives the last.
@@ -62,7 +54,10 @@ __device__ int block_scan(int v, int *wave, int *total) {
   return v;
 }
 
-__device__ void make_list(const PackPrepare &p, int which) {
+// Lists of work items for more sequences than a wave has lanes: block 0's by rows, block
+// 1's by keys.
+__global__ __launch_bounds__(kThreads) void pack_lists_kernel(PackLists p) {
+  const int which = static_cast<int>(blockIdx.x);
   const PackArgs &a = p.a;
   const PackList list = p.lists[which];
   __shared__ int wave[kThreads / 64], first[kThreads + 1], hist[kBins];
@@ -158,60 +153,10 @@ __device__ void make_list(const PackPrepare &p, int which) {
           p.header[5] = run_k;
         }
       }
-      if (bad && which == 0 && p.status) atomicOr(p.status, kStatusBadOffsets);
+      if (bad && which == 0 && a.status) atomicOr(a.status, kStatusBadOffsets);
       __syncthreads();
     }
   }
-}
-
-template <typename T, int D>
-__device__ void make_stats(const PackPrepare &p, size_t block) {
-  // a group of D / 8 lanes per row, in the rows' order by key head
-  constexpr int LANES = D / 8;
-  const size_t rows = static_cast<size_t>(p.a.kv_heads) * p.a.rows_q * p.a.group;
-  const size_t i = block * (kThreads / LANES) + threadIdx.x / LANES;
-  const int x = threadIdx.x % LANES;
-  if (i >= rows) return;
-  const size_t per = static_cast<size_t>(p.a.rows_q) * p.a.group;
-  const int kv = static_cast<int>(i / per), r = static_cast<int>(i % per);
-  const int query = r / p.a.group, head = kv * p.a.group + r % p.a.group;
-  const T *o = reinterpret_cast<const T *>(rows_base(p.o, query, head)) + 8 * x;
-  const T *g = reinterpret_cast<const T *>(rows_base(p.a.d_o, query, head)) + 8 * x;
-  float sum = 0.0f;
-  if constexpr (sizeof(T) == 2) {
-    const uint4 u = *reinterpret_cast<const uint4 *>(o), v = *reinterpret_cast<const uint4 *>(g);
-    const uint32_t us[4] = {u.x, u.y, u.z, u.w}, vs[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      sum = fmaf(__uint_as_float(us[j] << 16), __uint_as_float(vs[j] << 16), sum);
-      sum = fmaf(__uint_as_float(us[j] & 0xFFFF0000u), __uint_as_float(vs[j] & 0xFFFF0000u), sum);
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; j += 4) {
-      const float4 u = *reinterpret_cast<const float4 *>(o + j), v = *reinterpret_cast<const float4 *>(g + j);
-      sum = fmaf(u.x, v.x, sum);
-      sum = fmaf(u.y, v.y, sum);
-      sum = fmaf(u.z, v.z, sum);
-      sum = fmaf(u.w, v.w, sum);
-    }
-  }
-#pragma unroll
-  for (int m = 1; m < LANES; m <<= 1) sum += __shfl_xor(sum, m);
-  if (x == 0) {
-    const float lse = p.lse[static_cast<size_t>(head) * p.a.rows_q + query];
-    p.stats[i] = lse == -INFINITY ? -INFINITY : lse * -1.4426950408889634f;  // no key: no weight
-    p.stats[rows + i] = sum;
-  }
-}
-
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void pack_prepare_kernel(PackPrepare p) {
-  const int b = static_cast<int>(blockIdx.x);
-  if (b < p.n_lists)
-    make_list(p, b);
-  else
-    make_stats<T, D>(p, b - p.n_lists);
 }
 
 // O and lse, or dQ, from the parts' sums.  A group of D / 4 lanes per row.
@@ -221,10 +166,11 @@ __global__ __launch_bounds__(256) void pack_join_rows_kernel(PackArgs a, PackRow
   const size_t per = static_cast<size_t>(a.rows_q) * a.group, rows = per * a.kv_heads;
   const size_t row = static_cast<size_t>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
   const int x = threadIdx.x % LANES;
+  const int2 ends = pack_ends(a, false);
   if (row >= rows) return;
   const int kv = static_cast<int>(row / per), r = static_cast<int>(row % per);
   const int query = r / a.group, head = kv * a.group + r % a.group;
-  if (query < a.ends[0] || query >= a.ends[1]) return;
+  if (query < ends.x || query >= ends.y) return;
   const float2 *ml = reinterpret_cast<const float2 *>(a.parts + a.splits * rows * D);
   float top = 0.0f, l = 0.0f, f = a.scale;
   if constexpr (!GRAD) {
@@ -262,9 +208,10 @@ __global__ __launch_bounds__(256) void pack_join_keys_kernel(PackArgs a, PackRow
   const size_t rows = static_cast<size_t>(a.kv_heads) * a.rows_k;
   const size_t row = static_cast<size_t>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
   const int x = threadIdx.x % LANES;
+  const int2 ends = pack_ends(a, true);
   if (row >= rows) return;
   const int head = static_cast<int>(row / a.rows_k), key = static_cast<int>(row % a.rows_k);
-  if (key < a.ends[2] || key >= a.ends[3]) return;
+  if (key < ends.x || key >= ends.y) return;
   const int v = blockIdx.y;
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
@@ -289,44 +236,25 @@ __global__ __launch_bounds__(256) void pack_join_keys_kernel(PackArgs a, PackRow
     if (e_ != hipSuccess) return e_; \
   } while (0)
 
-// Parts that an item's tiles are cut into: as many, up to 16 of `least` tiles or more,
-// as make the launch's rounds shortest, a part costing about 4% of an item more (its
-// start, its sums).  `resident`: the blocks that the chip holds at once.
+// Parts that an item's tiles are cut into where the items are fewer than the blocks
+// that the chip holds at once (`resident`): as many as fill it, up to 16 of `least`
+// tiles or more.
 int parts_of(long long blocks, long long tiles, int least, int resident) {
-  constexpr int kMost = 16;
-  int best = 1;
-  double shortest = 0.0;
-  for (int s = 1; s <= kMost && (s == 1 || static_cast<long long>(s) * least <= tiles); ++s) {
-    const double rounds = static_cast<double>((blocks * s + resident - 1) / resident) * (1.0 / s + 0.04);
-    if (s == 1 || rounds < shortest) {
-      shortest = rounds;
-      best = s;
-    }
-  }
-  return best;
+  long long s = blocks > 0 ? resident / blocks : 1;
+  if (s > tiles / least) s = tiles / least;
+  return static_cast<int>(s < 1 ? 1 : s > 16 ? 16 : s);
 }
 
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
-template <typename T, int D>
-hipError_t prepare(const PackArgs &a, const PackCall &c, bool grad, hipStream_t s) {
-  PackPrepare p{};
+hipError_t prepare(const PackArgs &a, const PackCall &c, int lists, hipStream_t s) {
+  if (a.sequences <= 64) return hipSuccess;
+  PackLists p{};
   p.a = a;
   p.lists[0] = c.by_rows;
   p.lists[1] = c.by_keys;
-  p.n_lists = grad ? 2 : 1;
   p.header = c.header;
-  p.status = c.status;
-  p.d = D;
-  size_t blocks = p.n_lists;
-  if (grad) {
-    p.o = c.o;
-    p.lse = c.lse;
-    p.stats = const_cast<float *>(a.stats);
-    const size_t rows = static_cast<size_t>(a.kv_heads) * a.rows_q * a.group, per = kThreads / (D / 8);
-    blocks += (rows + per - 1) / per;
-  }
-  hipLaunchKernelGGL((pack_prepare_kernel<T, D>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL(pack_lists_kernel, dim3(lists), dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }
 
@@ -339,7 +267,7 @@ hipError_t join_rows(const PackArgs &a, const PackRows &out, hipStream_t s) {
 
 template <typename T, int D>
 hipError_t forward(PackArgs a, const PackCall &c, hipStream_t s) {
-  PACK_TRY((prepare<T, D>(a, c, false, s)));
+  PACK_TRY(prepare(a, c, 1, s));
   a.list = c.by_rows;
   a.count = c.header;
   a.splits = c.splits_rows;
@@ -349,7 +277,7 @@ hipError_t forward(PackArgs a, const PackCall &c, hipStream_t s) {
 
 template <typename T, int D>
 hipError_t backward(PackArgs a, const PackCall &c, hipStream_t s) {
-  PACK_TRY((prepare<T, D>(a, c, true, s)));
+  PACK_TRY(prepare(a, c, 2, s));
   a.list = c.by_rows;
   a.count = c.header;
   a.splits = c.splits_rows;
@@ -391,7 +319,7 @@ size_t packed_workspace(const scope_pack *p, void *base, PackArgs *a, PackCall *
   const long long items_q = p->kv_heads * ceil_div(ceil_div(rows, p->sequences), by_rows.rows) * p->sequences;
   const long long items_k = p->kv_heads * ceil_div(ceil_div(keys, p->sequences), by_keys.rows) * p->sequences;
   const int tile = bf16 ? 64 : 32;
-  const int splits_rows = parts_of(items_q, ceil_div(ceil_div(keys, p->sequences), tile), 4, bf16 ? 256 : 512);
+  const int splits_rows = parts_of(items_q, ceil_div(ceil_div(keys, p->sequences), tile), 4, 512);
   const int splits_keys = parts_of(items_k, ceil_div(ceil_div(rows, p->sequences), 32), 8, 512);
   const size_t row_parts = splits_rows > 1 ? static_cast<size_t>(splits_rows) * p->kv_heads * rows * (4 * p->d + 8) : 0;
   const size_t key_parts = splits_keys > 1 ? static_cast<size_t>(splits_keys) * 2 * p->kv_heads * keys * 4 * p->d : 0;

@@ -20,20 +20,41 @@ namespace scope {
 namespace {
 
 constexpr float kLag = 8.0f;  // the running maximum may lag by 2^8
-static_assert(kPackRows == kBM, "rows of a block");
+constexpr int kWaves = kPackRows / 32;  // a wave owns 32 rows
+
+// Wave w's share of a tile of keys' rows, 1 KB per load; rows past the last key repeat
+// it, with no weight.
+template <int D>
+struct KeyTile {
+  static __device__ __forceinline__ void bring(const __amdgpu_buffer_rsrc_t &from, uint32_t stride, uint16_t *tile, int index, int lk, int w,
+                                               int lane) {
+    constexpr int CH = D / 8, RPL = 64 / CH;  // 16-byte chunks per row, rows per load
+    if ((index + 1) * kBN <= lk) {
+#pragma unroll
+      for (int i = 0; i < kBN / kWaves / RPL; ++i) {
+        const int r0 = kBN / kWaves * w + RPL * i, r = r0 + lane / CH;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16, r * stride + 16 * ((lane % CH) ^ tile_swizzle<D>(r)),
+                                                 index * kBN * stride, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kBN / kWaves / RPL; ++i) {
+        const int r0 = kBN / kWaves * w + RPL * i, r = r0 + lane / CH;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16,
+                                                 min(index * kBN + r, lk - 1) * stride + 16 * ((lane % CH) ^ tile_swizzle<D>(r)), 0, 0, 0);
+      }
+    }
+  }
+};
 
 template <int D, bool GRAD>
-__global__ __launch_bounds__(kNW * 64)
+__global__ __launch_bounds__(kWaves * 64)
 __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel(PackArgs a, PackRows out) {
-  constexpr int CH = D / 8;        // 16-byte chunks per row
-  constexpr int RPL = 64 / CH;     // rows per load
-  constexpr int NG = kBN / kNW / RPL;  // loads per wave, tile and matrix
   __shared__ __attribute__((aligned(16))) uint16_t K0[kBN * D], K1[kBN * D], V0[kBN * D], V1[kBN * D];
-  int h, rank;
-  if (!pack_place(static_cast<int>(blockIdx.x), a.kv_heads, a.count[0], &h, &rank)) return;
+  int h, row0;
+  int4 sq;
+  if (!pack_item<false, kPackRows>(a, &h, &sq, &row0)) return;
   const int part = static_cast<int>(blockIdx.y);
-  const int4 sq = a.list.items[2 * rank];
-  const int row0 = a.list.items[2 * rank + 1].x;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -45,7 +66,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
   // keys that this row sees, and the wave's fewest and most
   const int seen = keys_seen(row, a.group, lq, lk, a.causal);
   const int fewest = __builtin_amdgcn_readlane(seen, 0), most = __builtin_amdgcn_readlane(seen, 31);
-  const int block_most = keys_seen(min(row0 + kBM, rows) - 1, a.group, lq, lk, a.causal);
+  const int block_most = keys_seen(min(row0 + kPackRows, rows) - 1, a.group, lq, lk, a.causal);
 
   bf16x8 qf[D / 16], gf[GRAD ? D / 16 : 1];
   {
@@ -58,9 +79,23 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
     }
   }
   float neg_lse = -INFINITY, delta = 0.0f;
-  if (GRAD && valid) {
-    neg_lse = a.stats[stat];
-    delta = a.stats[static_cast<size_t>(a.kv_heads) * a.rows_q * a.group + stat];
+  if constexpr (GRAD) {
+    if (valid) {
+      const uint16_t *o = reinterpret_cast<const uint16_t *>(rows_base(a.o, q0, h * a.group) + query * a.o.row + member * a.o.head);
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x) {
+        const bf16x8 of = as_bf16x8(load8<true>(o, 16 * x + 8 * hf));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) delta = fmaf(static_cast<float>(of[j]), static_cast<float>(gf[x][j]), delta);
+      }
+      const float lse = a.lse[static_cast<size_t>(h * a.group + member) * a.rows_q + q0 + query];
+      neg_lse = lse == -INFINITY ? -INFINITY : lse * -1.4426950408889634f;  // no key: no weight
+    }
+    delta += __shfl_xor(delta, 32);
+    if (valid && hf == 0 && part == 0) {
+      a.stats[stat] = neg_lse;
+      a.stats[static_cast<size_t>(a.kv_heads) * a.rows_q * a.group + stat] = delta;
+    }
   }
 
   f32x16 acc[D / 32];
@@ -72,26 +107,14 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
 
   // the part's tiles
   const int all = (block_most + kBN - 1) / kBN, per = (all + a.splits - 1) / a.splits;
-  const int first = min(part * per, all), last = min(first + per, all);
-  const int last_own = active ? min(last, (most + kBN - 1) / kBN) : 0;
+  const int first = scalar(min(part * per, all)), last = scalar(min(first + per, all));
+  const int last_own = scalar(active ? min(last, (most + kBN - 1) / kBN) : 0);
 
   const uint32_t k_row = static_cast<uint32_t>(a.k.row), v_row = static_cast<uint32_t>(a.v.row);
   const __amdgpu_buffer_rsrc_t rk = pack_resource(rows_base(a.k, k0, h), lk ? span(a.k, lk, 1, 2 * D) : 0);
   const __amdgpu_buffer_rsrc_t rv = pack_resource(rows_base(a.v, k0, h), lk ? span(a.v, lk, 1, 2 * D) : 0);
-  // wave w brings rows 8 w .. 8 w + 7 of a tile, RPL rows (1 KB) per load; rows past
-  // the last key repeat it, with no weight
-  auto bring = [&](const __amdgpu_buffer_rsrc_t &from, uint32_t stride, uint16_t *tile, int index) {
-    const bool whole = (index + 1) * kBN <= lk;
-#pragma unroll
-    for (int i = 0; i < NG; ++i) {
-      const int r0 = kBN / kNW * w + RPL * i, r = r0 + lane / CH;
-      const int col = 16 * ((lane % CH) ^ tile_swizzle<D>(r));
-      if (whole)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16, r * stride + col, index * kBN * stride, 0, 0);
-      else
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16, min(index * kBN + r, lk - 1) * stride + col, 0, 0, 0);
-    }
-  };
+  auto bring_k = [&](uint16_t *tile, int index) { KeyTile<D>::bring(rk, k_row, tile, index, lk, w, lane); };
+  auto bring_v = [&](uint16_t *tile, int index) { KeyTile<D>::bring(rv, v_row, tile, index, lk, w, lane); };
   auto scores = [&](const uint16_t *kt, int kb) {
     f32x16 s;
 #pragma unroll
@@ -272,8 +295,8 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
   // wave's loads land before the barrier
   auto step = [&](int index, const uint16_t *kc, const uint16_t *vc, uint16_t *kn, uint16_t *vn) {
     if (index + 1 < last) {
-      bring(rk, k_row, kn, index + 1);
-      bring(rv, v_row, vn, index + 1);
+      bring_k(kn, index + 1);
+      bring_v(vn, index + 1);
     }
     if (index < last_own) {
       if constexpr (GRAD)
@@ -285,8 +308,8 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
     __syncthreads();
   };
   if (first < last) {
-    bring(rk, k_row, K0, first);
-    bring(rv, v_row, V0, first);
+    bring_k(K0, first);
+    bring_v(V0, first);
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);
   __syncthreads();
@@ -328,7 +351,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
 template <int D, bool GRAD>
 hipError_t run(const PackArgs &a, const PackRows &out, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(kXcds) * a.kv_heads * ((a.list.capacity + kXcds - 1) / kXcds), a.splits);
-  hipLaunchKernelGGL((packed_queries_kernel<D, GRAD>), grid, dim3(kNW * 64), 0, s, a, out);
+  hipLaunchKernelGGL((packed_queries_kernel<D, GRAD>), grid, dim3(kWaves * 64), 0, s, a, out);
   return hipGetLastError();
 }
 
