@@ -10,6 +10,7 @@ module computes nothing.  It fails loudly if the library is not built.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -393,15 +394,17 @@ def alloc_training_workspace(shape: Shape, c_q: int, device="cuda"):
 def _on_device(call, stream, *tensors):
     """Runs call(stream pointer) with the tensors' device current: the current
     stream is that device's, and all tensors have to be on it."""
-    tensors = [t for t in tensors if t is not None]
     dev = tensors[0].device
     for t in tensors:
-        if t.device != dev:
+        if t is not None and t.device != dev:
             raise ValueError(f"tensors on {dev} and {t.device}")
     if stream is not None and stream.device != dev:
         raise ValueError(f"tensors on {dev}, the stream on {stream.device}")
-    if dev.index == torch.cuda.current_device():
-        return call(_stream(stream))
+    index = dev.index
+    # as torch.cuda.current_device and current_stream, without 4 us of objects a call
+    if index == torch._C._cuda_getDevice():
+        return call(torch._C._cuda_getCurrentRawStream(index) if stream is None
+                    else stream.cuda_stream)
     with torch.cuda.device(dev):
         return call(_stream(stream))
 
@@ -466,6 +469,11 @@ def scope_dropout(x, residual, dropout, rng, y, stream=None):
                                        x, residual, rng, y))
 
 
+@functools.lru_cache(maxsize=256)
+def _strides(row, head):
+    return ctypes.byref(Strides(row, head))
+
+
 def _rows(t, dtype, heads, rows, d, name):
     """(pointer, strides) of a tensor [heads][rows][d] whose channels are contiguous."""
     if t is None:
@@ -474,34 +482,43 @@ def _rows(t, dtype, heads, rows, d, name):
         raise ValueError(f"{name} must be a GPU tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != (heads, rows, d):
+    if t.shape != (heads, rows, d):
         raise ValueError(f"{name} must be {(heads, rows, d)}, got {tuple(t.shape)}")
-    if t.numel() and d > 1 and t.stride(2) != 1:
+    head, row, channel = t.stride()
+    if channel != 1 and d > 1 and heads and rows:
         raise ValueError(f"{name} needs contiguous channels")
     # of a dimension of one row the stride says nothing
-    row = t.stride(1) if rows > 1 and heads else d
-    head = t.stride(0) if heads > 1 and rows else rows * d
-    return ctypes.c_void_p(t.data_ptr()), ctypes.byref(Strides(row, head))
+    if rows <= 1 or not heads:
+        row = d
+    if heads <= 1 or not rows:
+        head = rows * d
+    return t.data_ptr(), _strides(row, head)
+
+
+@functools.lru_cache(maxsize=256)
+def _rotation(*args):
+    return ctypes.byref(make_rotation(*args))
 
 
 def scope_rotary(x, y, positions, turns, ranges, layout="pairs", inverse=False, factor=1.0,
                  x2=None, y2=None, stream=None):
-    """y = x, [heads][rows][d], turned by positions [axes][rows] (y2 = x2 too)."""
+    """y = x, [heads][rows][d], turned by positions [axes][rows] (y2 = x2 too);
+    ranges: the axes' (offsets, lengths), as tuples."""
     if x.dim() != 3 or (x2 is not None and x2.dim() != 3):
         raise ValueError("need tensors of three dimensions: heads, rows, channels")
-    if x.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"x must be bfloat16 or float32, got {x.dtype}")
+    dt = x.dtype
+    if dt not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"x must be bfloat16 or float32, got {dt}")
     if (x2 is None) != (y2 is None):
         raise ValueError("x2 and y2 go together")
     heads, rows, d = x.shape
     heads2 = x2.shape[0] if x2 is not None else 0
-    r = make_rotation(rows, (heads, heads2), d, BF16 if x.dtype == torch.bfloat16 else F32, ranges,
-                      layout, inverse, factor)
-    pairs = sum(int(n) for n in ranges[1]) // 2
-    args = [ctypes.byref(r), _ptr(positions, torch.int32, r.axes * rows, "positions"),
-            _ptr(turns, torch.int64, pairs, "turns"),
-            *_rows(x, x.dtype, heads, rows, d, "x"), *_rows(y, x.dtype, heads, rows, d, "y")]
-    args += ([*_rows(x2, x.dtype, heads2, rows, d, "x2"), *_rows(y2, x.dtype, heads2, rows, d, "y2")]
+    r = _rotation(rows, (heads, heads2), d, BF16 if dt == torch.bfloat16 else F32, ranges, layout,
+                  bool(inverse), float(factor))
+    args = [r, _ptr(positions, torch.int32, len(ranges[0]) * rows, "positions"),
+            _ptr(turns, torch.int64, sum(ranges[1]) // 2, "turns"),
+            *_rows(x, dt, heads, rows, d, "x"), *_rows(y, dt, heads, rows, d, "y")]
+    args += ([*_rows(x2, dt, heads2, rows, d, "x2"), *_rows(y2, dt, heads2, rows, d, "y2")]
              if x2 is not None else [None] * 4)
     _check("scope_rotary", _on_device(lambda s: lib().scope_rotary(*args, s), stream, x, y,
                                       positions, turns, x2, y2))
@@ -521,11 +538,10 @@ def alloc_packed_workspace(pack: Pack, device="cuda"):
 
 def _packed(pack, tensors):
     """Pointers and strides of (name, tensor, of queries) entries."""
-    dt, out = _data_dtype(pack), {}
-    for name, t, queries in tensors:
-        out[name] = _rows(t, dt, pack.heads if queries else pack.kv_heads,
-                          pack.rows_q if queries else pack.rows_k, pack.d, name)
-    return out
+    dt, d = _data_dtype(pack), pack.d
+    queries, keys = (dt, pack.heads, pack.rows_q, d), (dt, pack.kv_heads, pack.rows_k, d)
+    return {name: _rows(t, *(queries if of_queries else keys), name)
+            for name, t, of_queries in tensors}
 
 
 def scope_packed_attention(pack, q, k, v, offsets_q, offsets_k, lengths_k, scale, o, lse,

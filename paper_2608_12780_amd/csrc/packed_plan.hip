@@ -237,10 +237,13 @@ __global__ __launch_bounds__(256) void pack_join_keys_kernel(PackArgs a, PackRow
   } while (0)
 
 // Parts that an item's tiles are cut into where the items are fewer than the blocks
-// that the chip holds at once (`resident`): as many as fill it, up to 16 of `least`
-// tiles or more.
-int parts_of(long long blocks, long long tiles, int least, int resident) {
-  long long s = blocks > 0 ? resident / blocks : 1;
+// that the chip holds at once (512): as many as fill it, up to 16 of `least` tiles or
+// more.  Twice as many where items are full, since sequences differ in length and
+// causal rows in keys: 4 sequences of 512 queries behind 5000 to 16000 keys, 16 heads in
+// groups of 4, 219 and 17 us to join them for 264 and 12; but single tokens, whose
+// parts are short, 34 and 9 us for 31 and 6.
+int parts_of(long long blocks, long long tiles, int least, bool full) {
+  long long s = blocks > 0 ? (full ? 1024 : 512) / blocks : 1;
   if (s > tiles / least) s = tiles / least;
   return static_cast<int>(s < 1 ? 1 : s > 16 ? 16 : s);
 }
@@ -319,8 +322,9 @@ size_t packed_workspace(const scope_pack *p, void *base, PackArgs *a, PackCall *
   const long long items_q = p->kv_heads * ceil_div(ceil_div(rows, p->sequences), by_rows.rows) * p->sequences;
   const long long items_k = p->kv_heads * ceil_div(ceil_div(keys, p->sequences), by_keys.rows) * p->sequences;
   const int tile = bf16 ? 64 : 32;
-  const int splits_rows = parts_of(items_q, ceil_div(ceil_div(keys, p->sequences), tile), 4, 512);
-  const int splits_keys = parts_of(items_k, ceil_div(ceil_div(rows, p->sequences), 32), 8, 512);
+  const bool full = rows >= static_cast<long long>(by_rows.rows) * p->sequences;
+  const int splits_rows = parts_of(items_q, ceil_div(ceil_div(keys, p->sequences), tile), 4, full);
+  const int splits_keys = parts_of(items_k, ceil_div(ceil_div(rows, p->sequences), 32), 8, true);
   const size_t row_parts = splits_rows > 1 ? static_cast<size_t>(splits_rows) * p->kv_heads * rows * (4 * p->d + 8) : 0;
   const size_t key_parts = splits_keys > 1 ? static_cast<size_t>(splits_keys) * 2 * p->kv_heads * keys * 4 * p->d : 0;
   float *parts = reinterpret_cast<float *>(take(row_parts > key_parts ? row_parts : key_parts));

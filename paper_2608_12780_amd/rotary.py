@@ -85,7 +85,7 @@ class Rotary:
         lengths = [self.d] if lengths is None else [int(x) for x in lengths]
         if offsets is None:
             offsets = [sum(lengths[:i]) for i in range(len(lengths))]
-        self.ranges = ([int(x) for x in offsets], lengths)
+        self.ranges = (tuple(int(x) for x in offsets), tuple(lengths))
         if layout not in B.LAYOUTS:
             raise ValueError(f"layout {layout!r}: pairs or halves")
         if not 1 <= len(lengths) <= 3 or len(self.ranges[0]) != len(lengths):
@@ -105,7 +105,7 @@ class Rotary:
             with _allocating_on(stream):
                 out = [torch.empty(t.shape, dtype=t.dtype, device=t.device)
                        for t in (x, x2) if t is not None]
-        y, y2 = (*out, None)[:2]
+        y, y2 = out if x2 is not None else (out[0], None)
         B.scope_rotary(x, y, positions, self.turns, self.ranges, self.layout, inverse, self.factor,
                        x2, y2, stream)
         return (y, y2) if x2 is not None else y
@@ -121,14 +121,15 @@ class Rotary:
             raise ValueError(f"x must be [heads][n][{self.d}], is {tuple(x.shape)}")
         if x2 is not None and (x2.dim() != 3 or x2.shape[1:] != x.shape[1:] or x2.dtype != x.dtype):
             raise ValueError(f"x2 is {tuple(x2.shape)} {x2.dtype}, x {tuple(x.shape)} {x.dtype}")
-        axes = len(self.ranges[0])
-        if tuple(positions.shape) not in ((axes, x.shape[1]), *(((x.shape[1],),) if axes == 1 else ())):
-            raise ValueError(f"positions must be [{axes}][{x.shape[1]}], is {tuple(positions.shape)}")
-        given = [t for t in (out if isinstance(out, (tuple, list)) else (out,)) if t is not None]
-        if out is not None and len(given) != (1 if x2 is None else 2):
+        n, axes = x.shape[1], len(self.ranges[0])
+        if positions.shape != (axes, n) and (axes > 1 or positions.shape != (n,)):
+            raise ValueError(f"positions must be [{axes}][{n}], is {tuple(positions.shape)}")
+        given = () if out is None else tuple(out) if isinstance(out, (tuple, list)) else (out,)
+        if out is not None and (len(given) != (1 if x2 is None else 2)
+                                or any([t is None for t in given])):
             raise ValueError("out needs a tensor for each input")
-        if torch.is_grad_enabled() and any(t is not None and t.requires_grad
-                                           for t in (x, x2, *given)):
+        if torch.is_grad_enabled() and any([t is not None and t.requires_grad
+                                            for t in (x, x2, *given)]):
             if given:
                 raise ValueError("rotate into `out` is not differentiable: leave `out` away, or "
                                  "call it under torch.no_grad()")
