@@ -161,7 +161,7 @@ int32_t scope_rotary(const scope_rotation *r, const int32_t *positions, const ui
     a.len[i] = n;
     if (!pairs) vectors = vectors && o % 8 == 0 && n % 16 == 0;
   }
-  if (!positions || !turns || reinterpret_cast<uintptr_t>(positions) % 4 || reinterpret_cast<uintptr_t>(turns) % 8)
+  if ((r->rows && !positions) || !turns || reinterpret_cast<uintptr_t>(positions) % 4 || reinterpret_cast<uintptr_t>(turns) % 8)
     return SCOPE_ERR_INVALID_ARGUMENT;
   const void *xs[2] = {x, x2};
   void *ys[2] = {y, y2};

@@ -18,15 +18,29 @@ namespace scope {
 
 namespace {
 
-constexpr int kRowTile = 32;
 constexpr int kWaves = kPackKeys / 32;  // a wave owns 32 keys
+
+// A tile's rows, 32 of them: 64 at d = 64 took as long, and at d = 128 would leave a CU
+// one block.
+template <int D>
+struct RowTile {
+  static constexpr int kRows = 32;
+  static constexpr int CH = D / 8;              // 16-byte chunks per row
+  static constexpr int RPL = 64 / CH;           // rows per load
+  static constexpr int NG = kRows / kWaves / RPL; // loads per wave
+  // row and 16-byte column (in bytes) that load x of a wave brings for a lane
+  static __device__ __forceinline__ int row(int x, int w, int lane) { return kRows / kWaves * w + RPL * x + lane / CH; }
+  static __device__ __forceinline__ int column(int r, int lane) { return 16 * ((lane % CH) ^ tile_swizzle<D>(r)); }
+  static __device__ __forceinline__ void bring(const __amdgpu_buffer_rsrc_t &from, uint16_t *tile, int x, int w, uint32_t at, uint32_t first) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + (kRows / kWaves * w + RPL * x) * D, 16, at, first, 0, 0);
+  }
+};
 
 template <int D>
 __global__ __launch_bounds__(64 * kWaves)
 __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_kernel(PackArgs a, PackRows dk, PackRows dv) {
-  constexpr int CH = D / 8;              // 16-byte chunks per row
-  constexpr int RPL = 64 / CH;           // rows per load
-  constexpr int NG = kRowTile / kWaves / RPL; // loads per wave, tile and matrix
+  typedef RowTile<D> T;
+  constexpr int kRowTile = T::kRows;
   constexpr int kPlane = 64;             // a row value's plane: a lane each
   // a tile of Q, followed by two values per row: -lse (exp2 domain) and D (in the
   // tile's array: the compiler does not see the buffer unit write to an array of their
@@ -84,22 +98,42 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_kernel(Pa
   const __amdgpu_buffer_rsrc_t rs = pack_resource(
       a.stats + ((static_cast<size_t>(w & 1) * a.kv_heads + h) * a.rows_q + q0) * a.group, 4u * rows);
 
+  // Where a whole tile starts with a query's first row, its rows lie at lane offsets from
+  // a scalar one (a quotient for each row and tile: 796 us for 756, 16 heads in groups of
+  // 4, 30011 tokens of 24 prompts, d = 64).
+  const bool even = kRowTile % a.group == 0;
+  const int queries = kRowTile / a.group;
+  uint32_t at_q[T::NG], at_g[T::NG];
+#pragma unroll
+  for (int x = 0; x < T::NG; ++x) {
+    const int r = T::row(x, w, lane);
+    at_q[x] = row_offset(r, a.group, a.q) + T::column(r, lane);
+    at_g[x] = row_offset(r, a.group, a.d_o) + T::column(r, lane);
+  }
   // Rows past the last repeat it, with no weight.
   auto bring = [&](uint16_t *q, uint16_t *g, int index) {
+    if (even && (index + 1) * kRowTile <= rows) {
+      const uint32_t first_q = static_cast<uint32_t>(index * queries) * static_cast<uint32_t>(a.q.row);
+      const uint32_t first_g = static_cast<uint32_t>(index * queries) * static_cast<uint32_t>(a.d_o.row);
 #pragma unroll
-    for (int x = 0; x < NG; ++x) {
-      const int r0 = kRowTile / kWaves * w + RPL * x, r = r0 + lane / CH;
-      const int row = min(index * kRowTile + r, rows - 1);
-      const int col = 16 * ((lane % CH) ^ tile_swizzle<D>(r));
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, q + r0 * D, 16, row_offset(row, a.group, a.q) + col, 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rg, g + r0 * D, 16, row_offset(row, a.group, a.d_o) + col, 0, 0, 0);
+      for (int x = 0; x < T::NG; ++x) {
+        T::bring(rq, q, x, w, at_q[x], first_q);
+        T::bring(rg, g, x, w, at_g[x], first_g);
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < T::NG; ++x) {
+        const int r = T::row(x, w, lane), row = min(index * kRowTile + r, rows - 1);
+        T::bring(rq, q, x, w, row_offset(row, a.group, a.q) + T::column(r, lane), 0);
+        T::bring(rg, g, x, w, row_offset(row, a.group, a.d_o) + T::column(r, lane), 0);
+      }
     }
     if (w < 2)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, q + kStats + 2 * kPlane * w, 4, 4 * min(index * kRowTile + lane, rows - 1), 0, 0, 0);
   };
 
-  auto compute = [&](const uint16_t *qt, const uint16_t *gt, int row0) {
-    const float *st = reinterpret_cast<const float *>(qt + kStats);
+  // 32 rows of a tile
+  auto compute = [&](const uint16_t *qt, const uint16_t *gt, const float *st, int row0) {
     // The empty asm statements end a phase: its products stay before them, and the
     // places are formed anew after them (as in attention_keys.hip).
     f32x16 s, dp;
@@ -111,7 +145,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_kernel(Pa
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.row(qt, x), kf[x], s, 0, 0, 0);
     interleave<D / 16, 1, 0>();
     asm volatile("" : "+v"(s), "+v"(at.row_at));
-    if (row0 < sees_most || row0 + kRowTile > rows) {  // rows that do not see this lane's key
+    if (row0 < sees_most || row0 + 32 > rows) {  // rows that do not see this lane's key
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int row = row0 + 8 * (e >> 2) + 4 * hf + (e & 3);
@@ -173,7 +207,11 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_kernel(Pa
   // barrier
   auto step = [&](int index, const uint16_t *qc, const uint16_t *gc, uint16_t *qn, uint16_t *gn) {
     if (index + 1 < last) bring(qn, gn, index + 1);
-    if (index >= first_own) compute(qc, gc, index * kRowTile);
+    if (index >= first_own) {
+      const float *st = reinterpret_cast<const float *>(qc + kStats);
+#pragma unroll
+      for (int b = 0; b < kRowTile / 32; ++b) compute(qc + 32 * b * D, gc + 32 * b * D, st + 32 * b, index * kRowTile + 32 * b);
+    }
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
     __syncthreads();
   };
