@@ -401,6 +401,10 @@ hipError_t packed_queries(const PackArgs &a, int d, bool grad, const PackRows &o
 hipError_t packed_keys(const PackArgs &a, int d, const PackRows &dk, const PackRows &dv, hipStream_t s);
 hipError_t packed_queries_f32(const PackArgs &a, int d, bool grad, const PackRows &out, hipStream_t s);
 hipError_t packed_keys_f32(const PackArgs &a, int d, const PackRows &dk, const PackRows &dv, hipStream_t s);
+// Blocks of a launch over a list of at most `capacity` items.
+inline unsigned pack_blocks(long long capacity, int kv_heads, int splits) {
+  return static_cast<unsigned>((capacity * splits + 7) / 8 * 8 * kv_heads);
+}
 constexpr int kPackRows = 128;       // rows of a bf16 item by queries
 constexpr int kPackKeys = 128;       // keys of a bf16 item by keys
 constexpr int kPackRowsF32 = 64;     // rows, or keys, of an fp32 item

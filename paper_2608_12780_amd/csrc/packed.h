@@ -13,9 +13,10 @@ constexpr float kPackLn2 = 0.6931471805599453f;
 // so each is given an equal share by construction: a key head's list, which falls in
 // cost, is dealt out in eight classes (rank mod 8), and an XCD runs kv_heads
 // neighbouring (head, class) pairs, heads one after the other: its L2 then holds the
-// rows of one or two key heads.  False: nothing for this block.
-__device__ __forceinline__ bool pack_place(int block, int kv_heads, int count, int *head, int *rank) {
-  const int x = block % kXcds, per = (count + kXcds - 1) / kXcds;
+// rows of one or two key heads.  The parts of an item are neighbours in the list, so
+// that it falls in cost with them too.  False: nothing for this block.
+__device__ __forceinline__ bool pack_place(int block, int kv_heads, int items, int parts, int *head, int *rank, int *part) {
+  const int count = items * parts, x = block % kXcds, per = (count + kXcds - 1) / kXcds;
   int j = block / kXcds;
   if (per == 0 || j >= kv_heads * per) return false;
   const int u0 = x * kv_heads, u1 = u0 + kv_heads;
@@ -34,8 +35,10 @@ __device__ __forceinline__ bool pack_place(int block, int kv_heads, int count, i
     i = j / n;
     c = j % n;
   }
-  *rank = kXcds * i + c;
-  return *rank < count;
+  const int at = kXcds * i + c;
+  *rank = at / parts;
+  *part = at - *rank * parts;
+  return at < count;
 }
 
 // Keys that row `row` of a sequence's (query, head of the group) rows sees.
@@ -117,16 +120,16 @@ __device__ __forceinline__ int4 lane_sequence(const PackArgs &a, int lane, bool 
   return make_int4(q0, q1 - q0, k0, lk);
 }
 
-// The item of this block: its key head, its sequence and its first row (KEYS: key)
-// there.  Items run by falling cost, the keys that a block of ROWS rows sees (KEYS: the
+// The item of this block: its key head, its part, its sequence and its first row (KEYS:
+// key) there.  Items run by falling cost, the keys that a block of ROWS rows sees (KEYS: the
 // rows that see a block of ROWS keys).  Up to 64 sequences, a wave holds one per lane
 // and finds the item of a rank from how many cost more, for which there is a formula:
 // no list, and no launch to make one (that took 10 us); more sequences have a list.
 template <bool KEYS, int ROWS>
-__device__ __forceinline__ bool find_item(const PackArgs &a, int *head, int4 *seq, int *at) {
+__device__ __forceinline__ bool find_item(const PackArgs &a, int *head, int *part, int4 *seq, int *at) {
   int rank;
   if (a.sequences > 64) {
-    if (!pack_place(static_cast<int>(blockIdx.x), a.kv_heads, a.count[0], head, &rank)) return false;
+    if (!pack_place(static_cast<int>(blockIdx.x), a.kv_heads, a.count[0], a.splits, head, &rank, part)) return false;
     *seq = a.list.items[2 * rank];
     *at = a.list.items[2 * rank + 1].x;
     return true;
@@ -134,11 +137,11 @@ __device__ __forceinline__ bool find_item(const PackArgs &a, int *head, int4 *se
   const int lane = static_cast<int>(threadIdx.x) & 63;
   bool bad;
   const int4 s = lane_sequence(a, lane, &bad);
-  if (bad && a.status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(a.status, kStatusBadOffsets);
+  if (bad && a.status && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.status, kStatusBadOffsets);
   const int rows = s.y * a.group, ahead = s.w - s.y;
   const int tiles = ((KEYS ? s.w : rows) + ROWS - 1) / ROWS;
   const int total = lane_sum(tiles);
-  if (!pack_place(static_cast<int>(blockIdx.x), a.kv_heads, total, head, &rank)) return false;
+  if (!pack_place(static_cast<int>(blockIdx.x), a.kv_heads, total, a.splits, head, &rank, part)) return false;
   // this lane's items of cost c or more
   auto costing = [&](int c) {
     if (c == 0) return tiles;
@@ -185,9 +188,10 @@ __device__ __forceinline__ bool find_item(const PackArgs &a, int *head, int4 *se
 }
 
 template <bool KEYS, int ROWS>
-__device__ __forceinline__ bool pack_item(const PackArgs &a, int *head, int4 *seq, int *at) {
-  if (!find_item<KEYS, ROWS>(a, head, seq, at)) return false;
+__device__ __forceinline__ bool pack_item(const PackArgs &a, int *head, int *part, int4 *seq, int *at) {
+  if (!find_item<KEYS, ROWS>(a, head, part, seq, at)) return false;
   *head = scalar(*head);
+  *part = scalar(*part);
   *at = scalar(*at);
   *seq = make_int4(scalar(seq->x), scalar(seq->y), scalar(seq->z), scalar(seq->w));
   return true;

@@ -17,10 +17,9 @@ __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_f32_kernel(PackArgs a, PackRows out) {
   typedef TileF32<D> T;
   __shared__ __attribute__((aligned(16))) float K0[T::kFloats], K1[T::kFloats], V0[T::kFloats], V1[T::kFloats];
-  int h, row0;
+  int h, part, row0;
   int4 sq;
-  if (!pack_item<false, kPackRowsF32>(a, &h, &sq, &row0)) return;
-  const int part = static_cast<int>(blockIdx.y);
+  if (!pack_item<false, kPackRowsF32>(a, &h, &part, &sq, &row0)) return;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -161,10 +160,9 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_f32_kerne
   // attention_keys.hip)
   constexpr int kQ = T::kFloats + 2 * 64;
   __shared__ __attribute__((aligned(16))) float Q0[kQ], Q1[kQ], G0[T::kFloats], G1[T::kFloats];
-  int h, key0;
+  int h, part, key0;
   int4 sq;
-  if (!pack_item<true, kPackRowsF32>(a, &h, &sq, &key0)) return;
-  const int part = static_cast<int>(blockIdx.y);
+  if (!pack_item<true, kPackRowsF32>(a, &h, &part, &sq, &key0)) return;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -249,7 +247,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_f32_kerne
 }
 
 dim3 grid_of(const PackArgs &a) {
-  return dim3(static_cast<unsigned>(kXcds) * a.kv_heads * ((a.list.capacity + kXcds - 1) / kXcds), a.splits);
+  return dim3(pack_blocks(a.list.capacity, a.kv_heads, a.splits));
 }
 
 template <int D, bool GRAD>

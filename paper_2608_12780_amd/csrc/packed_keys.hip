@@ -49,10 +49,9 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_kernel(Pa
   __shared__ __attribute__((aligned(256))) uint16_t Q0[kStats + 4 * kPlane], Q1[kStats + 4 * kPlane], G0[kRowTile * D], G1[kRowTile * D];
   constexpr bool VLDS = D == 128;
   __shared__ __attribute__((aligned(16))) uint16_t Vs[VLDS ? kPackKeys * D : 8];
-  int h, key0;
+  int h, part, key0;
   int4 sq;
-  if (!pack_item<true, kPackKeys>(a, &h, &sq, &key0)) return;
-  const int part = static_cast<int>(blockIdx.y);
+  if (!pack_item<true, kPackKeys>(a, &h, &part, &sq, &key0)) return;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -252,7 +251,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_kernel(Pa
 
 template <int D>
 hipError_t run(const PackArgs &a, const PackRows &dk, const PackRows &dv, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(kXcds) * a.kv_heads * ((a.list.capacity + kXcds - 1) / kXcds), a.splits);
+  const dim3 grid(pack_blocks(a.list.capacity, a.kv_heads, a.splits));
   hipLaunchKernelGGL((packed_keys_kernel<D>), grid, dim3(64 * kWaves), 0, s, a, dk, dv);
   return hipGetLastError();
 }

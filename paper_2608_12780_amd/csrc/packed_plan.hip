@@ -236,14 +236,16 @@ __global__ __launch_bounds__(256) void pack_join_keys_kernel(PackArgs a, PackRow
     if (e_ != hipSuccess) return e_; \
   } while (0)
 
-// Parts that an item's tiles are cut into where the items are fewer than the blocks
-// that the chip holds at once (512): as many as fill it, up to 16 of `least` tiles or
-// more.  Twice as many where items are full, since sequences differ in length and
-// causal rows in keys: 4 sequences of 512 queries behind 5000 to 16000 keys, 16 heads in
-// groups of 4, 219 and 17 us to join them for 264 and 12; but single tokens, whose
-// parts are short, 34 and 9 us for 31 and 6.
-int parts_of(long long blocks, long long tiles, int least, bool full) {
-  long long s = blocks > 0 ? (full ? 1024 : 512) / blocks : 1;
+// Parts that an item's tiles are cut into: as many as make `blocks` of the items, up to
+// 16 of `least` tiles or more.  The chip holds 512 blocks at once; items differ in length
+// as sequences do, and causal rows in keys, so that twice as many (dK and dV of bf16
+// inputs, whose longest items take longest: four times) end more evenly.  4 sequences of
+// 512 queries behind 5000 to 16000 keys, 16 heads in groups of 4: 276 us with 512, 212
+// with 1024; 24 prompts of 22 to 6600 tokens, d = 64, dK and dV: 797 us whole, 571 in two
+// parts, joining them included.  Single tokens' parts are short: 16 behind up to 8000
+// keys, 37 us with 512 and 43 with 1024.
+int parts_of(long long items, long long tiles, int least, int blocks) {
+  long long s = items > 0 ? blocks / items : 1;
   if (s > tiles / least) s = tiles / least;
   return static_cast<int>(s < 1 ? 1 : s > 16 ? 16 : s);
 }
@@ -323,8 +325,8 @@ size_t packed_workspace(const scope_pack *p, void *base, PackArgs *a, PackCall *
   const long long items_k = p->kv_heads * ceil_div(ceil_div(keys, p->sequences), by_keys.rows) * p->sequences;
   const int tile = bf16 ? 64 : 32;
   const bool full = rows >= static_cast<long long>(by_rows.rows) * p->sequences;
-  const int splits_rows = parts_of(items_q, ceil_div(ceil_div(keys, p->sequences), tile), 4, full);
-  const int splits_keys = parts_of(items_k, ceil_div(ceil_div(rows, p->sequences), 32), 8, true);
+  const int splits_rows = parts_of(items_q, ceil_div(ceil_div(keys, p->sequences), tile), 4, full ? 1024 : 512);
+  const int splits_keys = parts_of(items_k, ceil_div(ceil_div(rows, p->sequences), 32), 8, bf16 ? 2048 : 1024);
   const size_t row_parts = splits_rows > 1 ? static_cast<size_t>(splits_rows) * p->kv_heads * rows * (4 * p->d + 8) : 0;
   const size_t key_parts = splits_keys > 1 ? static_cast<size_t>(splits_keys) * 2 * p->kv_heads * keys * 4 * p->d : 0;
   float *parts = reinterpret_cast<float *>(take(row_parts > key_parts ? row_parts : key_parts));
@@ -346,7 +348,7 @@ bool packed_launchable(const scope_pack *p) {
   PackCall c{};
   packed_workspace(p, nullptr, &a, &c);
   auto fits = [](long long capacity, long long heads, int splits, int threads) {
-    return (capacity + kXcds - 1) / kXcds * kXcds * heads * splits * threads < (1LL << 32);
+    return (capacity * splits + 7) / 8 * 8 * heads * threads < (1LL << 32);
   };
   return fits(c.by_rows.capacity, p->kv_heads, c.splits_rows, 512) && fits(c.by_keys.capacity, p->kv_heads, c.splits_keys, 256) &&
          static_cast<long long>(p->heads) * p->rows_q * (p->d / 4) < (1LL << 32) - 1024 &&

@@ -51,10 +51,9 @@ template <int D, bool GRAD>
 __global__ __launch_bounds__(kWaves * 64)
 __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel(PackArgs a, PackRows out) {
   __shared__ __attribute__((aligned(16))) uint16_t K0[kBN * D], K1[kBN * D], V0[kBN * D], V1[kBN * D];
-  int h, row0;
+  int h, part, row0;
   int4 sq;
-  if (!pack_item<false, kPackRows>(a, &h, &sq, &row0)) return;
-  const int part = static_cast<int>(blockIdx.y);
+  if (!pack_item<false, kPackRows>(a, &h, &part, &sq, &row0)) return;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -350,7 +349,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
 
 template <int D, bool GRAD>
 hipError_t run(const PackArgs &a, const PackRows &out, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(kXcds) * a.kv_heads * ((a.list.capacity + kXcds - 1) / kXcds), a.splits);
+  const dim3 grid(pack_blocks(a.list.capacity, a.kv_heads, a.splits));
   hipLaunchKernelGGL((packed_queries_kernel<D, GRAD>), grid, dim3(kWaves * 64), 0, s, a, out);
   return hipGetLastError();
 }
