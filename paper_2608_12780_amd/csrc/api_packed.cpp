@@ -146,7 +146,8 @@ int32_t scope_rotary(const scope_rotation *r, const int32_t *positions, const ui
   a.turns = turns;
   const bool pairs = r->layout == SCOPE_PAIRS;
   const int el = r->dtype == SCOPE_BF16 ? 2 : 4;
-  bool vectors = r->d % 8 == 0;
+  const int w = 16 / el;  // elements of a vector
+  bool vectors = r->d % w == 0;
   for (int i = 0; i < r->axes; ++i) {
     const int o = r->range_off[i], n = r->range_len[i];
     if (o < 0 || n < 2 || n % 2 || n > r->d || o > r->d - n || (pairs && o % 2)) return SCOPE_ERR_INVALID_ARGUMENT;
@@ -159,7 +160,7 @@ int32_t scope_rotary(const scope_rotation *r, const int32_t *positions, const ui
     a.by_off[at] = i;
     a.off[i] = o;
     a.len[i] = n;
-    if (!pairs) vectors = vectors && o % 8 == 0 && n % 16 == 0;
+    if (!pairs) vectors = vectors && o % w == 0 && n % (2 * w) == 0;
   }
   if ((r->rows && !positions) || !turns || reinterpret_cast<uintptr_t>(positions) % 4 || reinterpret_cast<uintptr_t>(turns) % 8)
     return SCOPE_ERR_INVALID_ARGUMENT;

@@ -7,7 +7,11 @@
 // turn in integers: position times frequency modulo 2^64 wraps as the angle does, so
 // position 2^24 is as exact as position 1.
 //
-// Bound by memory.
+// Bound by memory.  A 720p layer's queries and keys (24 + 24 heads x 118800 x 128 bf16)
+// take 560 us, 5.2 TB/s read and written, where a copy by torch reaches 4.8; gradients of
+// 5 + 5 heads x 32760, which leave the caches, 37 us (4.6 TB/s).  With at most 8 heads a
+// thread and no loads ahead the gradients took 48, with at most 4 the layer 698: the
+// angles cost a thread about as much as 4 heads' rows.
 #include "common.h"
 #include "kernels.h"
 #include "mfma.h"
@@ -17,7 +21,8 @@ namespace scope {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kAhead = 4;  // heads loaded together
+constexpr int kAhead = 4;   // heads loaded together
+constexpr int kBlocks = 4;  // blocks of a CU that fill it
 
 // sin and cos of u / 2^32 turns.  The nearest quarter turn is taken off in integers;
 // what is left, |x| <= pi / 4, goes through the Taylor series (the first terms left
@@ -68,29 +73,30 @@ __device__ __forceinline__ Unit half_unit(const RotaryArgs &a, int u) {
   return {c, -1, -1, 0};
 }
 
+// A vector as it lies in memory, and its values.
 template <typename T, int N>
-__device__ __forceinline__ void load_values(const T *p, float (&x)[N]) {
-  if constexpr (N == 1) {
-    x[0] = load_elem(p, 0);
-  } else if constexpr (sizeof(T) == 2) {
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
+struct Raw {
+  uint4 u;
+  __device__ __forceinline__ void load(const T *p) { u = *reinterpret_cast<const uint4 *>(p); }
+  __device__ __forceinline__ void values(float (&x)[N]) const {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const float4 v = *reinterpret_cast<const float4 *>(p + i);
-      x[i] = v.x;
-      x[i + 1] = v.y;
-      x[i + 2] = v.z;
-      x[i + 3] = v.w;
+      if constexpr (sizeof(T) == 2) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      } else {
+        x[i] = __uint_as_float(w[i]);
+      }
     }
   }
-}
+};
+template <typename T>
+struct Raw<T, 1> {
+  T v;
+  __device__ __forceinline__ void load(const T *p) { v = *p; }
+  __device__ __forceinline__ void values(float (&x)[1]) const { x[0] = load_elem(&v, 0); }
+};
 template <typename T, int N>
 __device__ __forceinline__ void store_values(T *p, const float (&x)[N]) {
   if constexpr (N == 1) {
@@ -106,8 +112,9 @@ __device__ __forceinline__ void store_values(T *p, const float (&x)[N]) {
   }
 }
 
-// PAIRS, vectors: a unit is 8 channels, whose 4 pairs may lie in different ranges.
-// Otherwise a unit is W values of either half (W = 8 or 1), or W copied ones; pairs
+// PAIRS, vectors: a unit is the W channels of 16 bytes, whose pairs may lie in different
+// ranges.  Otherwise a unit is W values of either half, or W copied ones (W = 1: alignment
+// allows no more); pairs
 // of single elements are halves one channel apart.
 template <typename T, bool PAIRS, int W>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
@@ -115,9 +122,44 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
   const long long row = at / a.units;
   if (row >= a.rows) return;
   const int u = static_cast<int>(at - row * a.units);
-  constexpr int P = PAIRS && W == 8 ? 4 : W;  // pairs of a unit
+  constexpr int P = PAIRS && W > 1 ? W / 2 : W;  // pairs of a unit
+  constexpr bool TWO = !(PAIRS && W > 1);        // a pair's values lie in two places
+  Unit unit{W * u, -1, -1, 0};
+  if constexpr (PAIRS && W == 1) {
+    unit = half_unit<1>(a, u);
+    if (unit.axis >= 0) {
+      unit.first = 2 * unit.first - a.off[unit.axis];
+      unit.second = unit.first + 1;
+    }
+  } else if constexpr (!PAIRS) {
+    unit = half_unit<W>(a, u);
+  }
+  const bool two = TWO && unit.axis >= 0;
+
+  const int heads = a.heads[0] + a.heads[1];
+  const int h0 = static_cast<int>(blockIdx.y) * a.per, h1 = min(h0 + a.per, heads);
+  auto place = [&](int h, int &i) {  // the row of a head past the last is the last's
+    const int hc = min(h, h1 - 1);
+    i = hc >= a.heads[0] ? 1 : 0;
+    return hc - (i ? a.heads[0] : 0);
+  };
+  // The next kAhead heads' loads go out before these are stored (which the compiler
+  // cannot know to be elsewhere, or the same thread's), the first before the angles.
+  Raw<T, W> raw[2][kAhead], raw2[2][TWO ? kAhead : 1];
+  auto load = [&](int set, int hb) {
+#pragma unroll
+    for (int b = 0; b < kAhead; ++b) {
+      int i;
+      const int hh = place(hb + b, i);
+      const T *x = static_cast<const T *>(a.x[i]) + hh * a.xs[i].head + row * a.xs[i].row;
+      raw[set][b].load(x + unit.first);
+      if constexpr (TWO)
+        if (two) raw2[set][b].load(x + unit.second);
+    }
+  };
+  load(0, h0);
+
   float cs[P], sn[P];
-  Unit unit{8 * u, -1, -1, 0};
   bool turned[P];
   auto angle = [&](int axis, int pair, float &s, float &c) {
     const long long p = a.positions[static_cast<size_t>(axis) * a.rows + row];
@@ -126,91 +168,73 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
     s *= a.inverse ? -a.factor : a.factor;
     c *= a.factor;
   };
-  if constexpr (PAIRS && W == 8) {
 #pragma unroll
-    for (int j = 0; j < P; ++j) {
-      const int ch = 8 * u + 2 * j;
-      int base = 0;
-      turned[j] = false;
-      for (int i = 0; i < a.axes; ++i) {
-        if (ch >= a.off[i] && ch < a.off[i] + a.len[i]) {
-          angle(i, base + (ch - a.off[i]) / 2, sn[j], cs[j]);
-          turned[j] = true;
+  for (int j = 0; j < P; ++j) {
+    if constexpr (!TWO) {
+      const int ch = W * u + 2 * j;
+      int axis = -1, pair = 0, base = 0;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        if (i < a.axes && ch >= a.off[i] && ch < a.off[i] + a.len[i]) {
+          axis = i;
+          pair = base + (ch - a.off[i]) / 2;
         }
         base += a.len[i] / 2;
       }
-    }
-  } else {
-    if constexpr (PAIRS) {
-      unit = half_unit<1>(a, u);
-      if (unit.axis >= 0) {
-        unit.first = 2 * unit.first - a.off[unit.axis];
-        unit.second = unit.first + 1;
-      }
-    } else {
-      unit = half_unit<W>(a, u);
-    }
-    if (unit.axis >= 0) {
-#pragma unroll
-      for (int j = 0; j < P; ++j) angle(unit.axis, unit.pair + j, sn[j], cs[j]);
+      turned[j] = axis >= 0;
+      if (turned[j]) angle(axis, pair, sn[j], cs[j]);
+    } else if (two) {
+      angle(unit.axis, unit.pair + j, sn[j], cs[j]);
     }
   }
 
-  const int heads = a.heads[0] + a.heads[1];
-  const int h0 = static_cast<int>(blockIdx.y) * a.per, h1 = min(h0 + a.per, heads);
-  auto place = [&](int h, int &i) {  // the row of a head past the last is the last's
-    const int hc = min(h, heads - 1);
-    i = hc >= a.heads[0] ? 1 : 0;
-    return hc - (i ? a.heads[0] : 0);
-  };
-  // kAhead heads' loads go out before the first store (which the compiler cannot know
-  // to be elsewhere, or the same thread's)
-  for (int hb = h0; hb < h1; hb += kAhead) {
-    float v[kAhead][W], z[kAhead][PAIRS && W == 8 ? 1 : W];
+  auto turn = [&](int set, int hb) {
 #pragma unroll
     for (int b = 0; b < kAhead; ++b) {
-      int i;
-      const int hh = place(hb + b, i);
-      const T *x = static_cast<const T *>(a.x[i]) + hh * a.xs[i].head + row * a.xs[i].row;
-      load_values<T, W>(x + unit.first, v[b]);
-      if constexpr (!(PAIRS && W == 8))
-        if (unit.axis >= 0) load_values<T, W>(x + unit.second, z[b]);
-    }
-#pragma unroll
-    for (int b = 0; b < kAhead; ++b) {
-      if (hb + b >= h1) break;
+      if (hb + b >= h1) return;
       int i;
       const int hh = place(hb + b, i);
       T *y = static_cast<T *>(a.y[i]) + hh * a.ys[i].head + row * a.ys[i].row;
-      if constexpr (PAIRS && W == 8) {
+      float v[W];
+      raw[set][b].values(v);
+      if constexpr (!TWO) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float p = v[b][2 * j], q = v[b][2 * j + 1];
-          v[b][2 * j] = turned[j] ? fmaf(p, cs[j], -(q * sn[j])) : p;
-          v[b][2 * j + 1] = turned[j] ? fmaf(p, sn[j], q * cs[j]) : q;
+        for (int j = 0; j < P; ++j) {
+          const float p = v[2 * j], q = v[2 * j + 1];
+          v[2 * j] = turned[j] ? fmaf(p, cs[j], -(q * sn[j])) : p;
+          v[2 * j + 1] = turned[j] ? fmaf(p, sn[j], q * cs[j]) : q;
         }
-      } else if (unit.axis >= 0) {
+      } else if (two) {
+        float z[W];
+        raw2[set][b].values(z);
 #pragma unroll
         for (int j = 0; j < W; ++j) {
-          const float p = v[b][j], q = z[b][j];
-          v[b][j] = fmaf(p, cs[j], -(q * sn[j]));
-          z[b][j] = fmaf(p, sn[j], q * cs[j]);
+          const float p = v[j], q = z[j];
+          v[j] = fmaf(p, cs[j], -(q * sn[j]));
+          z[j] = fmaf(p, sn[j], q * cs[j]);
         }
-        store_values<T, W>(y + unit.second, z[b]);
+        store_values<T, W>(y + unit.second, z);
       }
-      store_values<T, W>(y + unit.first, v[b]);
+      store_values<T, W>(y + unit.first, v);
     }
+  };
+  for (int hb = h0; hb < h1; hb += 2 * kAhead) {
+    if (hb + kAhead < h1) load(1, hb + kAhead);
+    turn(0, hb);
+    if (hb + 2 * kAhead < h1) load(0, hb + 2 * kAhead);
+    turn(1, hb + kAhead);
   }
 }
 
 template <typename T>
 hipError_t run(const RotaryArgs &a, bool pairs, bool vectors, dim3 grid, hipStream_t s) {
+  constexpr int W = 16 / sizeof(T);
   if (pairs && vectors)
-    hipLaunchKernelGGL((rotary_kernel<T, true, 8>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((rotary_kernel<T, true, W>), grid, dim3(kThreads), 0, s, a);
   else if (pairs)
     hipLaunchKernelGGL((rotary_kernel<T, true, 1>), grid, dim3(kThreads), 0, s, a);
   else if (vectors)
-    hipLaunchKernelGGL((rotary_kernel<T, false, 8>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((rotary_kernel<T, false, W>), grid, dim3(kThreads), 0, s, a);
   else
     hipLaunchKernelGGL((rotary_kernel<T, false, 1>), grid, dim3(kThreads), 0, s, a);
   return hipGetLastError();
@@ -222,13 +246,14 @@ hipError_t rotary_run(const RotaryArgs &args, bool bf16, bool pairs, bool vector
   RotaryArgs a = args;
   int turned = 0;
   for (int i = 0; i < a.axes; ++i) turned += a.len[i];
-  const int w = vectors ? 8 : 1;
-  a.units = pairs && vectors ? d / 8 : turned / 2 / w + (d - turned) / w;
-  // Heads of a thread: enough threads first, then up to 8 heads for one set of angles.
+  const int w = !vectors ? 1 : bf16 ? 8 : 4;
+  a.units = pairs && vectors ? d / w : turned / 2 / w + (d - turned) / w;
+  // Heads of a thread: all of them where the rows alone fill the chip.
   const long long threads = static_cast<long long>(a.rows) * a.units;
   const int heads = a.heads[0] + a.heads[1];
-  a.per = 1;
-  while (a.per < 8 && threads * ((heads + 2 * a.per - 1) / (2 * a.per)) >= 256LL * 2048) a.per *= 2;
+  const long long groups = (256LL * kBlocks * kThreads + threads - 1) / threads;
+  a.per = groups < heads ? static_cast<int>((heads + groups - 1) / groups) : 1;
+  if (a.per > kAhead) a.per = (a.per + kAhead - 1) / kAhead * kAhead;
   const dim3 grid(static_cast<unsigned>((threads + kThreads - 1) / kThreads), static_cast<unsigned>((heads + a.per - 1) / a.per));
   return bf16 ? run<uint16_t>(a, pairs, vectors, grid, s) : run<float>(a, pairs, vectors, grid, s);
 }
