@@ -1,7 +1,7 @@
 // Attention over packed sequences by rows, bf16 inputs: the forward with row
 // statistics, and dQ (packed_plan.hip has the formulas).
 //
-// A block runs an item's up to 256 rows (query, head of the group) of a key head, a
+// A block runs an item's up to 128 rows (query, head of the group) of a key head, a
 // wave 32 of them, over the keys that its last row sees, 64 at a time: K and V tiles
 // are brought into LDS by the buffer unit while the tile before is computed.  A
 // wave's tile is
@@ -12,6 +12,14 @@
 //   dP^T = V_tile . dO^T, ds = p (dP - D), dQ^T += K_tile^T . ds^T
 // with ds as two bf16 terms, the second what rounding the first left: a row's ds sum
 // to zero, so dQ is a difference of larger sums and keeps more of their rounding.
+//
+// Two blocks share a CU, whose waves drift apart, so that one's matrix products run
+// beside the other's vector work; blocks of 256 rows, one a CU, took as long in the
+// forward and 8% longer in dQ, and 46 us for 31 on single tokens.  Both kernels fill
+// the matrix pipe until the card lowers its clock.  5 heads x 32760, d = 128: forward 2.6
+// ms, 1.05 PFLOP/s, matrix pipe 52% busy at 1.9 GHz; dQ 4.6 ms, 1.19 PFLOP/s of its four
+// products, 67% at 1.75.  d = 64, 10 heads: 0.94 PFLOP/s, and dQ 5.2 ms, bound by vector
+// instructions, 80% busy.
 #include "attention_tile.h"
 #include "packed.h"
 
