@@ -26,11 +26,13 @@
  *    enqueues its kernels on `stream` (a hipStream_t; NULL = the default
  *    stream) and returns.  No call synchronises or copies to the host.
  *  - Layout: Q, K, V, O are [heads][n][d], d contiguous, in the dtype of the
- *    shape (fp32 or bf16).  All other arrays are dense, row-major, with the
- *    shapes given per argument, heads outermost.
+ *    shape (fp32 or bf16); calls 9 to 11 take strides of heads and rows.  All
+ *    other arrays are dense, row-major, with the shapes given per argument,
+ *    heads outermost.
  *  - Workspace: calls that need scratch take `workspace` (256-byte aligned)
  *    of at least scope_workspace_size() bytes, calls 6 and 7 of at least
- *    scope_training_workspace_size().  One workspace serves every call, but
+ *    scope_training_workspace_size(), calls 10 and 11 of at least
+ *    scope_packed_workspace_size().  One workspace serves every call, but
  *    two calls that may run concurrently (replays of captured graphs among
  *    them) need two workspaces.  Nothing in it outlives its call.
  *  - Errors: argument checks run before any GPU work and return
@@ -43,11 +45,12 @@
  *    fixed-point sums of the k-means means are exact (2^22 for n <= 2^17,
  *    2^15 at n = 2^24), also set for non-finite input; bit 2: an initial
  *    row index out of range, replaced by the default row; bit 3: a key set
- *    that is not strictly ascending in [0, n), call 7).  The inputs are
- *    checked in the first update pass of calls 1 and 2.  Nothing aborts or
- *    prints.
+ *    that is not strictly ascending in [0, n), call 7; bit 4: offsets or
+ *    lengths of sequences that fall or leave their array, calls 10 and 11).
+ *    The inputs are checked in the first update pass of calls 1 and 2.
+ *    Nothing aborts or prints.
  *  - Determinism: every output is bitwise reproducible run to run and
- *    independent of launch geometry (calls 6 and 7: see there); calls 1-4 are
+ *    independent of launch geometry (calls 6, 7, 10, 11: see there); calls 1-4 are
  *    bit-exact with respect to the canonical arithmetic defined under each call.
  */
 #ifndef SCOPE_H
@@ -483,8 +486,9 @@ int32_t scope_rotary(const scope_rotation *rotation, const int32_t *positions,
  * or where `causal` the keys j <= i + m - n: the last query sees all, queries before
  * the first key see none.
  * Supported: d in {64, 128}, 1 <= sequences <= 65536, 0 <= rows <= 2^24, heads * rows
- * < 2^31 each; 16-byte aligned rows (pointers and strides); the rows of one key head,
- * or of the query heads that share it, within 2^32 bytes of the first.        */
+ * < 2^31 each, at most 2^30 queries of one key head, so few items that a launch needs
+ * less than 2^32 threads; 16-byte aligned rows (pointers and strides); 66 rows in a row,
+ * of one key head or of all query heads that share it, within 2^32 bytes.     */
 typedef struct {
   int32_t heads, kv_heads;
   int32_t rows_q, rows_k; /* rows of q, o; of k, v */

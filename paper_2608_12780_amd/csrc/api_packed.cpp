@@ -43,8 +43,8 @@ struct Tensor {
   bool out;
 };
 
-// A tensor of the packed calls: its strides in bytes.  The rows of one key head, or of
-// the heads that share it, are addressed with 32-bit byte offsets.
+// A tensor of the packed calls: its strides in bytes.  The rows of a tile, up to 66 of one
+// key head or of the heads that share it, are addressed with 32-bit byte offsets.
 int32_t check_rows(const Tensor &t, int d, int el, int shared, scope::PackRows *rows) {
   const scope_strides s = dense_or(t.strides, t.rows, d);
   const int64_t all = extent(&s, t.heads, t.rows, d, t.out);
@@ -52,7 +52,8 @@ int32_t check_rows(const Tensor &t, int d, int el, int shared, scope::PackRows *
   if (!t.p && t.rows) return SCOPE_ERR_INVALID_ARGUMENT;
   // rows are read and written as 16-byte vectors
   if (reinterpret_cast<uintptr_t>(t.p) % 16 || s.row * el % 16 || s.head * el % 16) return SCOPE_ERR_INVALID_ARGUMENT;
-  if (t.rows && ((t.rows - 1) * s.row + (shared - 1) * s.head + d) * el >= (1LL << 32)) return SCOPE_ERR_UNSUPPORTED;
+  const int64_t near = t.rows < 66 ? t.rows : 66;
+  if (t.rows && ((near - 1) * s.row + (shared - 1) * s.head + d) * el >= (1LL << 32)) return SCOPE_ERR_UNSUPPORTED;
   rows->base = static_cast<char *>(const_cast<void *>(t.p));
   rows->row = s.row * el;
   rows->head = s.head * el;

@@ -46,8 +46,8 @@ __device__ __forceinline__ int keys_seen(int row, int group, int lq, int lk, int
   return causal ? min(max(row / group + lk - lq + 1, 0), lk) : lk;
 }
 
-// Where row `row` of a key head lies, in bytes from the sequence's first query of the
-// group's first head.
+// Where row `row` of a key head lies, in bytes from row 0 of the group's first head: rows
+// of one tile, so that 32 bits hold it.
 __device__ __forceinline__ uint32_t row_offset(int row, int group, const PackRows &r) {
   const int query = row / group;
   return static_cast<uint32_t>(query) * static_cast<uint32_t>(r.row) +

@@ -67,17 +67,19 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_f32_ke
   const int all = (block_most + kTile - 1) / kTile, per = (all + a.splits - 1) / a.splits;
   const int first = scalar(min(part * per, all)), last = scalar(min(first + per, all));
   const int last_own = scalar(active ? min(last, (most + kTile - 1) / kTile) : 0);
-  const uint32_t k_row = static_cast<uint32_t>(a.k.row), v_row = static_cast<uint32_t>(a.v.row);
-  const __amdgpu_buffer_rsrc_t rk = pack_resource(rows_base(a.k, k0, h), lk ? span(a.k, lk, 1, 4 * D) : 0);
-  const __amdgpu_buffer_rsrc_t rv = pack_resource(rows_base(a.v, k0, h), lk ? span(a.v, lk, 1, 4 * D) : 0);
-  // rows past the last key repeat it, with no weight
+  // rows past the last key repeat it, with no weight; addressed from the tile (a sequence
+  // may be longer than 32-bit offsets reach)
+  char *const k_base = rows_base(a.k, k0, h), *const v_base = rows_base(a.v, k0, h);
   auto bring = [&](float *kt, float *vt, int index) {
+    const int held = min(lk - index * kTile, kTile);
+    const __amdgpu_buffer_rsrc_t rk = pack_resource(k_base + static_cast<int64_t>(index) * kTile * a.k.row, span(a.k, held, 1, 4 * D));
+    const __amdgpu_buffer_rsrc_t rv = pack_resource(v_base + static_cast<int64_t>(index) * kTile * a.v.row, span(a.v, held, 1, 4 * D));
 #pragma unroll
     for (int i = 0; i < T::NG; ++i) {
       const int r0 = (T::RPL * T::NG) * w + T::RPL * i, r = r0 + lane / T::CH;
-      const int key = min(index * kTile + r, lk - 1), col = 16 * ((lane % T::CH) ^ (r & 15));
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, kt + r0 * D, 16, key * k_row + col, 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, vt + r0 * D, 16, key * v_row + col, 0, 0, 0);
+      const int key = min(r, held - 1), col = 16 * ((lane % T::CH) ^ (r & 15));
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, kt + r0 * D, 16, key * static_cast<uint32_t>(a.k.row) + col, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, vt + r0 * D, 16, key * static_cast<uint32_t>(a.v.row) + col, 0, 0, 0);
     }
   };
   auto compute = [&](int index, const float *kt, const float *vt) {
@@ -186,16 +188,20 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_f32_kerne
   const int per = (tiles_all - from_tile + a.splits - 1) / a.splits;
   const int first = scalar(min(from_tile + part * per, tiles_all)), last = scalar(min(first + per, tiles_all));
   const int first_own = scalar(active ? sees_least / kTile : last);
-  const __amdgpu_buffer_rsrc_t rq = pack_resource(rows_base(a.q, q0, h * a.group), lq ? span(a.q, lq, a.group, 4 * D) : 0);
-  const __amdgpu_buffer_rsrc_t rg = pack_resource(rows_base(a.d_o, q0, h * a.group), lq ? span(a.d_o, lq, a.group, 4 * D) : 0);
+  char *const q_base = rows_base(a.q, q0, h * a.group), *const g_base = rows_base(a.d_o, q0, h * a.group);
   const __amdgpu_buffer_rsrc_t rs = pack_resource(
       a.stats + ((static_cast<size_t>(w & 1) * a.kv_heads + h) * a.rows_q + q0) * a.group, 4u * rows);
-  // rows past the last repeat it, with no weight
+  // rows past the last repeat it, with no weight; addressed from the first query that the
+  // tile holds a row of
   auto bring = [&](float *q, float *d_o, int index) {
+    const int first_query = scalar(index * kTile / a.group), before = index * kTile - first_query * a.group;
+    const int held = min(lq - first_query, kTile / a.group + 2);
+    const __amdgpu_buffer_rsrc_t rq = pack_resource(q_base + first_query * a.q.row, span(a.q, held, a.group, 4 * D));
+    const __amdgpu_buffer_rsrc_t rg = pack_resource(g_base + first_query * a.d_o.row, span(a.d_o, held, a.group, 4 * D));
 #pragma unroll
     for (int i = 0; i < T::NG; ++i) {
       const int r0 = (T::RPL * T::NG) * w + T::RPL * i, r = r0 + lane / T::CH;
-      const int row = min(index * kTile + r, rows - 1);
+      const int row = min(before + r, rows - 1 - first_query * a.group);
       const int col = 16 * ((lane % T::CH) ^ (r & 15));
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, q + r0 * D, 16, row_offset(row, a.group, a.q) + col, 0, 0, 0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rg, d_o + r0 * D, 16, row_offset(row, a.group, a.d_o) + col, 0, 0, 0);

@@ -34,8 +34,8 @@ struct RowTile {
   // row and 16-byte column (in bytes) that load x of a wave brings for a lane
   static __device__ __forceinline__ int row(int x, int w, int lane) { return kRows / kWaves * w + RPL * x + lane / CH; }
   static __device__ __forceinline__ int column(int r, int lane) { return 16 * ((lane % CH) ^ tile_swizzle<D>(r)); }
-  static __device__ __forceinline__ void bring(const __amdgpu_buffer_rsrc_t &from, uint16_t *tile, int x, int w, uint32_t at, uint32_t first) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + (kRows / kWaves * w + RPL * x) * D, 16, at, first, 0, 0);
+  static __device__ __forceinline__ void bring(const __amdgpu_buffer_rsrc_t &from, uint16_t *tile, int x, int w, uint32_t at) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + (kRows / kWaves * w + RPL * x) * D, 16, at, 0, 0, 0);
   }
 };
 
@@ -94,17 +94,17 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_kernel(Pa
   // this wave's first tile
   const int first_own = scalar(active ? sees_least / kRowTile : last);
 
-  const __amdgpu_buffer_rsrc_t rq = pack_resource(rows_base(a.q, q0, h * a.group), lq ? span(a.q, lq, a.group, 2 * D) : 0);
-  const __amdgpu_buffer_rsrc_t rg = pack_resource(rows_base(a.d_o, q0, h * a.group), lq ? span(a.d_o, lq, a.group, 2 * D) : 0);
   // plane w < 2 of the rows' values
   const __amdgpu_buffer_rsrc_t rs = pack_resource(
       a.stats + ((static_cast<size_t>(w & 1) * a.kv_heads + h) * a.rows_q + q0) * a.group, 4u * rows);
 
-  // Where a whole tile starts with a query's first row, its rows lie at lane offsets from
-  // a scalar one (a quotient for each row and tile: 796 us for 756, 16 heads in groups of
-  // 4, 30011 tokens of 24 prompts, d = 64).
+  // A tile's rows are addressed from the first query that it holds a row of (a sequence
+  // may be longer than 32-bit offsets reach).  Where every tile starts with a query's first
+  // row, at the same offsets in all whole tiles (a quotient for each row and tile: 796 us
+  // for 756, 16 heads in groups of 4, 30011 tokens of 24 prompts, d = 64).
   const bool even = kRowTile % a.group == 0;
   const int queries = kRowTile / a.group;
+  char *const q_base = rows_base(a.q, q0, h * a.group), *const g_base = rows_base(a.d_o, q0, h * a.group);
   uint32_t at_q[T::NG], at_g[T::NG];
 #pragma unroll
   for (int x = 0; x < T::NG; ++x) {
@@ -114,20 +114,23 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_kernel(Pa
   }
   // Rows past the last repeat it, with no weight.
   auto bring = [&](uint16_t *q, uint16_t *g, int index) {
+    const int first_query = even ? index * queries : scalar(index * kRowTile / a.group);
+    const int before = index * kRowTile - first_query * a.group;  // rows of that query before the tile
+    const int held = min(lq - first_query, kRowTile / a.group + 2);
+    const __amdgpu_buffer_rsrc_t rq = pack_resource(q_base + first_query * a.q.row, span(a.q, held, a.group, 2 * D));
+    const __amdgpu_buffer_rsrc_t rg = pack_resource(g_base + first_query * a.d_o.row, span(a.d_o, held, a.group, 2 * D));
     if (even && (index + 1) * kRowTile <= rows) {
-      const uint32_t first_q = static_cast<uint32_t>(index * queries) * static_cast<uint32_t>(a.q.row);
-      const uint32_t first_g = static_cast<uint32_t>(index * queries) * static_cast<uint32_t>(a.d_o.row);
 #pragma unroll
       for (int x = 0; x < T::NG; ++x) {
-        T::bring(rq, q, x, w, at_q[x], first_q);
-        T::bring(rg, g, x, w, at_g[x], first_g);
+        T::bring(rq, q, x, w, at_q[x]);
+        T::bring(rg, g, x, w, at_g[x]);
       }
     } else {
 #pragma unroll
       for (int x = 0; x < T::NG; ++x) {
-        const int r = T::row(x, w, lane), row = min(index * kRowTile + r, rows - 1);
-        T::bring(rq, q, x, w, row_offset(row, a.group, a.q) + T::column(r, lane), 0);
-        T::bring(rg, g, x, w, row_offset(row, a.group, a.d_o) + T::column(r, lane), 0);
+        const int r = T::row(x, w, lane), row = min(before + r, rows - 1 - first_query * a.group);
+        T::bring(rq, q, x, w, row_offset(row, a.group, a.q) + T::column(r, lane));
+        T::bring(rg, g, x, w, row_offset(row, a.group, a.d_o) + T::column(r, lane));
       }
     }
     if (w < 2)

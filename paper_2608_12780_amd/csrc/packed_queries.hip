@@ -30,26 +30,30 @@ namespace {
 constexpr float kLag = 8.0f;  // the running maximum may lag by 2^8
 constexpr int kWaves = kPackRows / 32;  // a wave owns 32 rows
 
-// Wave w's share of a tile of keys' rows, 1 KB per load; rows past the last key repeat
-// it, with no weight.
+// Wave w's share of a tile of keys' rows, 1 KB per load, through a resource that starts
+// at the tile (a sequence may be longer than 32-bit offsets reach); rows past the last
+// key repeat it, with no weight.
 template <int D>
 struct KeyTile {
-  static __device__ __forceinline__ void bring(const __amdgpu_buffer_rsrc_t &from, uint32_t stride, uint16_t *tile, int index, int lk, int w,
-                                               int lane) {
+  static __device__ __forceinline__ void bring(char *base, int64_t stride, uint16_t *tile, int index, int lk, int w, int lane) {
     constexpr int CH = D / 8, RPL = 64 / CH;  // 16-byte chunks per row, rows per load
-    if ((index + 1) * kBN <= lk) {
+    const int rows = min(lk - index * kBN, kBN);
+    const __amdgpu_buffer_rsrc_t from = pack_resource(base + static_cast<int64_t>(index) * kBN * stride,
+                                                      static_cast<uint32_t>(rows - 1) * static_cast<uint32_t>(stride) + 2 * D);
+    if (rows == kBN) {
 #pragma unroll
       for (int i = 0; i < kBN / kWaves / RPL; ++i) {
         const int r0 = kBN / kWaves * w + RPL * i, r = r0 + lane / CH;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16, r * stride + 16 * ((lane % CH) ^ tile_swizzle<D>(r)),
-                                                 index * kBN * stride, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16,
+                                                 r * static_cast<uint32_t>(stride) + 16 * ((lane % CH) ^ tile_swizzle<D>(r)), 0, 0, 0);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < kBN / kWaves / RPL; ++i) {
         const int r0 = kBN / kWaves * w + RPL * i, r = r0 + lane / CH;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16,
-                                                 min(index * kBN + r, lk - 1) * stride + 16 * ((lane % CH) ^ tile_swizzle<D>(r)), 0, 0, 0);
+                                                 min(r, rows - 1) * static_cast<uint32_t>(stride) + 16 * ((lane % CH) ^ tile_swizzle<D>(r)),
+                                                 0, 0, 0);
       }
     }
   }
@@ -117,11 +121,9 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
   const int first = scalar(min(part * per, all)), last = scalar(min(first + per, all));
   const int last_own = scalar(active ? min(last, (most + kBN - 1) / kBN) : 0);
 
-  const uint32_t k_row = static_cast<uint32_t>(a.k.row), v_row = static_cast<uint32_t>(a.v.row);
-  const __amdgpu_buffer_rsrc_t rk = pack_resource(rows_base(a.k, k0, h), lk ? span(a.k, lk, 1, 2 * D) : 0);
-  const __amdgpu_buffer_rsrc_t rv = pack_resource(rows_base(a.v, k0, h), lk ? span(a.v, lk, 1, 2 * D) : 0);
-  auto bring_k = [&](uint16_t *tile, int index) { KeyTile<D>::bring(rk, k_row, tile, index, lk, w, lane); };
-  auto bring_v = [&](uint16_t *tile, int index) { KeyTile<D>::bring(rv, v_row, tile, index, lk, w, lane); };
+  char *const k_base = rows_base(a.k, k0, h), *const v_base = rows_base(a.v, k0, h);
+  auto bring_k = [&](uint16_t *tile, int index) { KeyTile<D>::bring(k_base, a.k.row, tile, index, lk, w, lane); };
+  auto bring_v = [&](uint16_t *tile, int index) { KeyTile<D>::bring(v_base, a.v.row, tile, index, lk, w, lane); };
   auto scores = [&](const uint16_t *kt, int kb) {
     f32x16 s;
 #pragma unroll

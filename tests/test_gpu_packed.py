@@ -249,6 +249,38 @@ def test_rows_where_they_lie(dtype):
     assert (p.double() - q.double()).abs().max() <= 4 * bound
 
 
+def test_offsets_past_32_bits():
+    """Keys and values in the rows of one wide projection, more than 2^32 bytes from the
+    first to the last, in a sequence's own rows and before it."""
+    n, width, d = 2_200_000, 8, 128
+    g = torch.Generator(device="cuda").manual_seed(30)
+    rows = torch.empty(n, width, d, dtype=torch.bfloat16, device="cuda")
+    for a in range(0, n, 200_000):
+        rows[a:a + 200_000] = torch.randn(200_000, width, d, generator=g, device="cuda").bfloat16()
+    assert rows.numel() * 2 > 1 << 32
+    lq, lk = [3, 2], [2_150_000, 50_000]
+    x = R.make(2, 2, lq, [1, 1], d, "bf16", seed=31)
+    x.update(lk=lk, ok=[0, lk[0], n], rows=(5, n), offsets_k=packed.offsets_of(lk),
+             k=rows[:, :2].transpose(0, 1), v=rows[:, 2:4].transpose(0, 1))
+    check(x, True)
+    # queries far apart: the same few rows of a wide projection as a dense copy of them
+    m = 40
+    y = R.make(2, 1, [m], [m], d, "bf16", seed=32)
+    a = attention_of(y, True)
+    off = y["offsets_q"]
+    far = rows[::n // m][:m, 4:6].transpose(0, 1)
+    with pytest.raises(B.ScopeError, match="unsupported"):   # 39 x 112640000 bytes >= 2^32
+        a.forward(far, y["k"], y["v"], off)
+    far = rows[::n // (2 * m)][:m, 4:6].transpose(0, 1)      # 39 x 56320000, past 2^31
+    far.copy_(y["q"])
+    want = [t.clone() for t in a.forward(y["q"], y["k"], y["v"], off)]
+    grads = [t.clone() for t in a.backward(y["q"], y["k"], y["v"], *want, y["d_o"], off)]
+    got = a.forward(far, y["k"], y["v"], off, into=a.outputs())
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    got = a.backward(far, y["k"], y["v"], *want, y["d_o"], off, into=a.gradients())
+    assert all(torch.equal(p, q) for p, q in zip(got, grads))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("causal", [True, False])
 def test_autograd(dtype, causal):
