@@ -2,7 +2,8 @@
 // statistics, and dQ (packed_plan.hip has the formulas).
 //
 // A block runs an item's up to 128 rows (query, head of the group) of a key head, a
-// wave 32 of them, over the keys that its last row sees, 64 at a time: K and V tiles
+// wave 32 of them, over the keys that its last row sees, 64 at a time (the forward at
+// d = 128: 32): K and V tiles
 // are brought into LDS by the buffer unit while the tile before is computed.  A
 // wave's tile is
 //   S^T = K_tile . Q^T                   keys x rows, a row per lane column
@@ -13,13 +14,15 @@
 // with ds as two bf16 terms, the second what rounding the first left: a row's ds sum
 // to zero, so dQ is a difference of larger sums and keeps more of their rounding.
 //
-// Two blocks share a CU, whose waves drift apart, so that one's matrix products run
-// beside the other's vector work; blocks of 256 rows, one a CU, took as long in the
-// forward and 8% longer in dQ, and 46 us for 31 on single tokens.  Both kernels fill
-// the matrix pipe until the card lowers its clock.  5 heads x 32760, d = 128: forward 2.6
-// ms, 1.05 PFLOP/s, matrix pipe 52% busy at 1.9 GHz; dQ 4.6 ms, 1.19 PFLOP/s of its four
-// products, 67% at 1.75.  d = 64, 10 heads: 0.94 PFLOP/s, and dQ 5.2 ms, bound by vector
-// instructions, 80% busy.
+// Several blocks share a CU, whose waves drift apart, so that one's matrix products run
+// beside another's vector work: two of 128 rows rather than one of 256 (dQ 8% faster,
+// single tokens 31 us for 46), and where 32 keys a tile leave registers for it, three (the
+// forward at d = 128, 1.05 -> 1.10 PFLOP/s; d = 64 holds four with 64 keys, and five with
+// 32 were 4% slower).  S of the next tile beside the weights of this one in a wave was no
+// faster.  The kernels fill the matrix pipe until the card lowers its clock.  5 heads x
+// 32760, d = 128: forward 2.5 ms, 1.10 PFLOP/s; dQ 4.6 ms, 1.19 PFLOP/s of its four
+// products, matrix pipe 67% busy at 1.75 GHz.  d = 64, 10 heads: 2.86 ms, 0.96 PFLOP/s,
+// and dQ 5.2 ms, both bound by vector instructions, 80% busy.
 #include "attention_tile.h"
 #include "packed.h"
 
@@ -33,24 +36,24 @@ constexpr int kWaves = kPackRows / 32;  // a wave owns 32 rows
 // Wave w's share of a tile of keys' rows, 1 KB per load, through a resource that starts
 // at the tile (a sequence may be longer than 32-bit offsets reach); rows past the last
 // key repeat it, with no weight.
-template <int D>
+template <int D, int N>
 struct KeyTile {
   static __device__ __forceinline__ void bring(char *base, int64_t stride, uint16_t *tile, int index, int lk, int w, int lane) {
     constexpr int CH = D / 8, RPL = 64 / CH;  // 16-byte chunks per row, rows per load
-    const int rows = min(lk - index * kBN, kBN);
-    const __amdgpu_buffer_rsrc_t from = pack_resource(base + static_cast<int64_t>(index) * kBN * stride,
+    const int rows = min(lk - index * N, N);
+    const __amdgpu_buffer_rsrc_t from = pack_resource(base + static_cast<int64_t>(index) * N * stride,
                                                       static_cast<uint32_t>(rows - 1) * static_cast<uint32_t>(stride) + 2 * D);
-    if (rows == kBN) {
+    if (rows == N) {
 #pragma unroll
-      for (int i = 0; i < kBN / kWaves / RPL; ++i) {
-        const int r0 = kBN / kWaves * w + RPL * i, r = r0 + lane / CH;
+      for (int i = 0; i < N / kWaves / RPL; ++i) {
+        const int r0 = N / kWaves * w + RPL * i, r = r0 + lane / CH;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16,
                                                  r * static_cast<uint32_t>(stride) + 16 * ((lane % CH) ^ tile_swizzle<D>(r)), 0, 0, 0);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < kBN / kWaves / RPL; ++i) {
-        const int r0 = kBN / kWaves * w + RPL * i, r = r0 + lane / CH;
+      for (int i = 0; i < N / kWaves / RPL; ++i) {
+        const int r0 = N / kWaves * w + RPL * i, r = r0 + lane / CH;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16,
                                                  min(r, rows - 1) * static_cast<uint32_t>(stride) + 16 * ((lane % CH) ^ tile_swizzle<D>(r)),
                                                  0, 0, 0);
@@ -61,8 +64,9 @@ struct KeyTile {
 
 template <int D, bool GRAD>
 __global__ __launch_bounds__(kWaves * 64)
-__attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel(PackArgs a, PackRows out) {
-  __shared__ __attribute__((aligned(16))) uint16_t K0[kBN * D], K1[kBN * D], V0[kBN * D], V1[kBN * D];
+__attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : GRAD ? 2 : 3))) void packed_queries_kernel(PackArgs a, PackRows out) {
+  constexpr int KB = GRAD || D == 64 ? 2 : 1, N = 32 * KB;  // blocks of 32 keys in a tile, and its keys
+  __shared__ __attribute__((aligned(16))) uint16_t K0[N * D], K1[N * D], V0[N * D], V1[N * D];
   int h, part, row0;
   int4 sq;
   if (!pack_item<false, kPackRows>(a, &h, &part, &sq, &row0)) return;
@@ -117,13 +121,13 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
   float m_run = -INFINITY, l_run = 0.0f;
 
   // the part's tiles
-  const int all = (block_most + kBN - 1) / kBN, per = (all + a.splits - 1) / a.splits;
+  const int all = (block_most + N - 1) / N, per = (all + a.splits - 1) / a.splits;
   const int first = scalar(min(part * per, all)), last = scalar(min(first + per, all));
-  const int last_own = scalar(active ? min(last, (most + kBN - 1) / kBN) : 0);
+  const int last_own = scalar(active ? min(last, (most + N - 1) / N) : 0);
 
   char *const k_base = rows_base(a.k, k0, h), *const v_base = rows_base(a.v, k0, h);
-  auto bring_k = [&](uint16_t *tile, int index) { KeyTile<D>::bring(k_base, a.k.row, tile, index, lk, w, lane); };
-  auto bring_v = [&](uint16_t *tile, int index) { KeyTile<D>::bring(v_base, a.v.row, tile, index, lk, w, lane); };
+  auto bring_k = [&](uint16_t *tile, int index) { KeyTile<D, N>::bring(k_base, a.k.row, tile, index, lk, w, lane); };
+  auto bring_v = [&](uint16_t *tile, int index) { KeyTile<D, N>::bring(v_base, a.v.row, tile, index, lk, w, lane); };
   auto scores = [&](const uint16_t *kt, int kb) {
     f32x16 s;
 #pragma unroll
@@ -159,26 +163,27 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
   };
 
   auto forward_tile = [&](int index, const uint16_t *kt, const uint16_t *vt) {
-    f32x16 s[2];
+    f32x16 s[KB];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[kb][e] = 0.0f;
 #pragma unroll
     for (int x = 0; x < D / 16; ++x)
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < KB; ++kb)
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.row(kt + 32 * kb * D, x), qf[x], s[kb], 0, 0, 0);
-    interleave<D / 8, 1, 0>();
-    if ((index + 1) * kBN > fewest) {
-      cut(s[0], index * kBN);
-      cut(s[1], index * kBN + 32);
+    interleave<KB * D / 16, 1, 0>();
+    if ((index + 1) * N > fewest) {
+      cut(s[0], index * N);
+      if constexpr (KB == 2) cut(s[KB - 1], index * N + 32);
     }
-    float mx0 = fmaxf(s[0][0], s[0][1]), mx1 = fmaxf(s[1][0], s[1][1]);
+    auto logit = [&](int i) { return s[i / 16][i % 16]; };
+    float mx0 = fmaxf(logit(0), logit(1)), mx1 = fmaxf(logit(8 * KB), logit(8 * KB + 1));
 #pragma unroll
-    for (int e = 2; e < 16; e += 2) {
-      mx0 = fmaxf(fmaxf(mx0, s[0][e]), s[0][e + 1]);
-      mx1 = fmaxf(fmaxf(mx1, s[1][e]), s[1][e + 1]);
+    for (int i = 2; i < 8 * KB; i += 2) {
+      mx0 = fmaxf(fmaxf(mx0, logit(i)), logit(i + 1));
+      mx1 = fmaxf(fmaxf(mx1, logit(8 * KB + i)), logit(8 * KB + i + 1));
     }
     float mx = fmaxf(mx0, mx1);
     {
@@ -201,7 +206,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
     }
     // no logit above -inf so far: weights of 0, where inf - inf would be NaN
     const float neg_m = m_run == -INFINITY ? 0.0f : -m_run;
-    bf16x8 pk[2][2];
+    bf16x8 pk[KB][2];
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     auto weights = [&](int kb) {
       float p[16];
@@ -215,15 +220,19 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
     };
     weights(0);
     asm volatile("" : "+v"(pk[0][0]), "+v"(pk[0][1]), "+v"(at.col_at));
-    // the second block's weights beside the first's product
     add(vt, pk[0]);
-    weights(1);
-    interleave<D / 16, 2, D == 128 ? 7 : 14>();
+    if constexpr (KB == 1) {
+      interleave<D / 16, 2, 0>();
+    } else {
+      // the second block's weights beside the first's product
+      weights(KB - 1);
+      interleave<D / 16, 2, 14>();
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(acc[db]));
-    asm volatile("" : "+v"(pk[1][0]), "+v"(pk[1][1]), "+v"(at.col_at));
-    add(vt + 32 * D, pk[1]);
-    interleave<D / 16, 2, 0>();
+      for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(acc[db]));
+      asm volatile("" : "+v"(pk[KB - 1][0]), "+v"(pk[KB - 1][1]), "+v"(at.col_at));
+      add(vt + 32 * D, pk[KB - 1]);
+      interleave<D / 16, 2, 0>();
+    }
     l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
   };
 
@@ -233,7 +242,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
     f32x16 s[2], dp[2];
     float p[2][16];
     bf16x8 dsk[2][2], rest[2][2];
-    const bool edge = (index + 1) * kBN > fewest;
+    const bool edge = (index + 1) * N > fewest;
     auto weights = [&](int kb) {  // p beside dP^T
       f32x16 x;
 #pragma unroll
@@ -270,7 +279,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
     s[0] = scores(kt, 0);
     interleave<D / 16, 1, 0>();
     asm volatile("" : "+v"(s[0]), "+v"(at.row_at));
-    if (edge) cut(s[0], index * kBN);
+    if (edge) cut(s[0], index * N);
     weights(0);
     gradient(0);
     s[1] = scores(kt, 1);
@@ -283,7 +292,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_kernel
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) asm volatile("" : "+v"(acc[db]));
     }
-    if (edge) cut(s[1], index * kBN + 32);
+    if (edge) cut(s[1], index * N + 32);
     weights(1);
     gradient(1);
     if constexpr (D == 128) {
