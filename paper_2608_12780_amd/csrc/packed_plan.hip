@@ -26,6 +26,7 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kBins = 1024;
+constexpr int kMostParts = 16;
 
 struct PackLists {
   PackArgs a;
@@ -172,27 +173,34 @@ __global__ __launch_bounds__(256) void pack_join_rows_kernel(PackArgs a, PackRow
   const int query = r / a.group, head = kv * a.group + r % a.group;
   if (query < ends.x || query >= ends.y) return;
   const float2 *ml = reinterpret_cast<const float2 *>(a.parts + a.splits * rows * D);
-  float top = 0.0f, l = 0.0f, f = a.scale;
+  // all parts' maxima and normalisers at once: their loads' latency is most of a small join
+  float w[kMostParts], f = a.scale;
   if constexpr (!GRAD) {
-    top = -INFINITY;
-    for (int p = 0; p < a.splits; ++p) top = fmaxf(top, ml[p * rows + row].x);
+    float2 s[kMostParts];
+#pragma unroll
+    for (int p = 0; p < kMostParts; ++p) s[p] = ml[min(p, a.splits - 1) * rows + row];
+    float top = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int p = 0; p < kMostParts; ++p) top = fmaxf(top, s[p].x);
     if (top == -INFINITY) top = 0.0f;
-    for (int p = 0; p < a.splits; ++p) {
-      const float2 s = ml[p * rows + row];
-      l = fmaf(s.y, __builtin_amdgcn_exp2f(s.x - top), l);
+#pragma unroll
+    for (int p = 0; p < kMostParts; ++p) {
+      w[p] = p < a.splits ? __builtin_amdgcn_exp2f(s[p].x - top) : 0.0f;
+      l = p < a.splits ? fmaf(s[p].y, w[p], l) : l;
     }
     f = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
     if (x == 0) a.lse[static_cast<size_t>(head) * a.rows_q + query] = l > 0.0f ? (top + __log2f(l)) * kPackLn2 : l == 0.0f ? -INFINITY : l;
   }
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-  for (int p = 0; p < a.splits; ++p) {
+#pragma unroll
+  for (int p = 0; p < kMostParts; ++p) {
+    if (p >= a.splits) break;
     const float4 v = *reinterpret_cast<const float4 *>(a.parts + (p * rows + row) * D + 4 * x);
-    const float w = GRAD ? 1.0f : __builtin_amdgcn_exp2f(ml[p * rows + row].x - top);
-    s.x = fmaf(v.x, w, s.x);
-    s.y = fmaf(v.y, w, s.y);
-    s.z = fmaf(v.z, w, s.z);
-    s.w = fmaf(v.w, w, s.w);
+    const float g = GRAD ? 1.0f : w[p];
+    s.x = fmaf(v.x, g, s.x);
+    s.y = fmaf(v.y, g, s.y);
+    s.z = fmaf(v.z, g, s.z);
+    s.w = fmaf(v.w, g, s.w);
   }
   T *to = reinterpret_cast<T *>(rows_base(out, query, head)) + 4 * x;
   if constexpr (sizeof(T) == 2)
@@ -237,17 +245,17 @@ __global__ __launch_bounds__(256) void pack_join_keys_kernel(PackArgs a, PackRow
   } while (0)
 
 // Parts that an item's tiles are cut into: as many as make `blocks` of the items, up to
-// 16 of `least` tiles or more.  The chip holds 512 blocks at once; items differ in length
-// as sequences do, and causal rows in keys, so that twice as many (dK and dV of bf16
-// inputs, whose longest items take longest: four times) end more evenly.  4 sequences of
-// 512 queries behind 5000 to 16000 keys, 16 heads in groups of 4: 276 us with 512, 212
-// with 1024; 24 prompts of 22 to 6600 tokens, d = 64, dK and dV: 797 us whole, 571 in two
-// parts, joining them included.  Single tokens' parts are short: 16 behind up to 8000
-// keys, 37 us with 512 and 43 with 1024.
+// 16 of `least` tiles or more.  The chip holds 512 to 768 blocks at once; items differ in
+// length as sequences do, and causal rows in keys, so that 1024 (dK and dV of bf16 inputs,
+// whose longest items take longest: 2048) end more evenly.  4 sequences of 512 queries
+// behind 5000 to 16000 keys, 16 heads in groups of 4: 276 us with 512, 212 with 1024; 24
+// prompts of 22 to 6600 tokens, d = 64, dK and dV: 797 us whole, 571 in two parts, joining
+// them included; single tokens of 16 sequences behind up to 8000 keys 43 us with 512, 39
+// with 1024 (with up to 64 parts 4 sequences of 16000 keys took 48 us for 38).
 int parts_of(long long items, long long tiles, int least, int blocks) {
   long long s = items > 0 ? blocks / items : 1;
   if (s > tiles / least) s = tiles / least;
-  return static_cast<int>(s < 1 ? 1 : s > 16 ? 16 : s);
+  return static_cast<int>(s < 1 ? 1 : s > kMostParts ? kMostParts : s);
 }
 
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
@@ -324,8 +332,7 @@ size_t packed_workspace(const scope_pack *p, void *base, PackArgs *a, PackCall *
   const long long items_q = p->kv_heads * ceil_div(ceil_div(rows, p->sequences), by_rows.rows) * p->sequences;
   const long long items_k = p->kv_heads * ceil_div(ceil_div(keys, p->sequences), by_keys.rows) * p->sequences;
   const int tile = bf16 ? 64 : 32;
-  const bool full = rows >= static_cast<long long>(by_rows.rows) * p->sequences;
-  const int splits_rows = parts_of(items_q, ceil_div(ceil_div(keys, p->sequences), tile), 4, full ? 1024 : 512);
+  const int splits_rows = parts_of(items_q, ceil_div(ceil_div(keys, p->sequences), tile), 4, 1024);
   const int splits_keys = parts_of(items_k, ceil_div(ceil_div(rows, p->sequences), 32), 8, bf16 ? 2048 : 1024);
   const size_t row_parts = splits_rows > 1 ? static_cast<size_t>(splits_rows) * p->kv_heads * rows * (4 * p->d + 8) : 0;
   const size_t key_parts = splits_keys > 1 ? static_cast<size_t>(splits_keys) * 2 * p->kv_heads * keys * 4 * p->d : 0;
