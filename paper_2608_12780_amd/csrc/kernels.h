@@ -387,8 +387,8 @@ struct PackCall {
   int d;
   bool bf16;
   PackRows o, dq, dk, dv;
-  PackList by_rows, by_keys;
-  int splits_rows, splits_keys;
+  PackList by_rows, by_keys, forward;  // forward: by_rows, or items of few rows
+  int splits_rows, splits_keys, splits_forward;
   int32_t *header;
 };
 // Lays the workspace out (base null: only its size) and chooses the launches.
@@ -406,6 +406,7 @@ inline unsigned pack_blocks(long long capacity, int kv_heads, int splits) {
   return static_cast<unsigned>((capacity * splits + 7) / 8 * 8 * kv_heads);
 }
 constexpr int kPackRows = 128;       // rows of a bf16 item by queries
+constexpr int kPackFewRows = 32;     // of one where sequences have few
 constexpr int kPackKeys = 128;       // keys of a bf16 item by keys
 constexpr int kPackRowsF32 = 64;     // rows, or keys, of an fp32 item
 

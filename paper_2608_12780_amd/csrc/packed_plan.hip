@@ -27,6 +27,7 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kBins = 1024;
 constexpr int kMostParts = 16;
+constexpr int kFewItems = 32;
 
 struct PackLists {
   PackArgs a;
@@ -260,11 +261,11 @@ int parts_of(long long items, long long tiles, int least, int blocks) {
 
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
-hipError_t prepare(const PackArgs &a, const PackCall &c, int lists, hipStream_t s) {
+hipError_t prepare(const PackArgs &a, const PackCall &c, const PackList &by_rows, int lists, hipStream_t s) {
   if (a.sequences <= 64) return hipSuccess;
   PackLists p{};
   p.a = a;
-  p.lists[0] = c.by_rows;
+  p.lists[0] = by_rows;
   p.lists[1] = c.by_keys;
   p.header = c.header;
   hipLaunchKernelGGL(pack_lists_kernel, dim3(lists), dim3(kThreads), 0, s, p);
@@ -280,17 +281,17 @@ hipError_t join_rows(const PackArgs &a, const PackRows &out, hipStream_t s) {
 
 template <typename T, int D>
 hipError_t forward(PackArgs a, const PackCall &c, hipStream_t s) {
-  PACK_TRY(prepare(a, c, 1, s));
-  a.list = c.by_rows;
+  PACK_TRY(prepare(a, c, c.forward, 1, s));
+  a.list = c.forward;
   a.count = c.header;
-  a.splits = c.splits_rows;
+  a.splits = c.splits_forward;
   PACK_TRY(sizeof(T) == 2 ? packed_queries(a, D, false, c.o, s) : packed_queries_f32(a, D, false, c.o, s));
   return a.splits > 1 ? join_rows<T, D, false>(a, c.o, s) : hipSuccess;
 }
 
 template <typename T, int D>
 hipError_t backward(PackArgs a, const PackCall &c, hipStream_t s) {
-  PACK_TRY(prepare(a, c, 2, s));
+  PACK_TRY(prepare(a, c, c.by_rows, 2, s));
   a.list = c.by_rows;
   a.count = c.header;
   a.splits = c.splits_rows;
@@ -324,17 +325,27 @@ size_t packed_workspace(const scope_pack *p, void *base, PackArgs *a, PackCall *
   PackList by_rows{nullptr, bf16 ? kPackRows : kPackRowsF32, 0}, by_keys{nullptr, bf16 ? kPackKeys : kPackRowsF32, 0};
   by_rows.capacity = static_cast<int>(rows / by_rows.rows + p->sequences);
   by_keys.capacity = static_cast<int>(keys / by_keys.rows + p->sequences);
+  // items that sequences of one length would give
+  auto items_of = [&](long long n, int list_rows) { return p->kv_heads * ceil_div(ceil_div(n, p->sequences), list_rows) * p->sequences; };
+  // Few queries of few sequences: items of 32 rows, whose keys a block's four waves share
+  // out among them, where parts alone would leave most waves idle.  16 items behind caches
+  // of up to 16000 keys 29 us for 38, 8 items 22 for 33, 32 items (8000 keys) 27 for 28, but
+  // 48 items 35 for 34 and 64 items 40.5 for 39.5.
+  const bool few = bf16 && rows <= static_cast<long long>(kPackFewRows) * p->sequences && items_of(rows, kPackFewRows) <= kFewItems;
+  PackList forward = by_rows;
+  if (few) forward.rows = kPackFewRows;
+  forward.capacity = static_cast<int>(rows / forward.rows + p->sequences);
   int32_t *header = reinterpret_cast<int32_t *>(take(64));
-  by_rows.items = reinterpret_cast<int4 *>(take(32 * static_cast<size_t>(by_rows.capacity)));
+  by_rows.items = forward.items = reinterpret_cast<int4 *>(take(32 * static_cast<size_t>(forward.capacity)));
   by_keys.items = reinterpret_cast<int4 *>(take(32 * static_cast<size_t>(by_keys.capacity)));
   float *stats = reinterpret_cast<float *>(take(8 * static_cast<size_t>(p->kv_heads) * rows));
-  // items that sequences of one length would give
-  const long long items_q = p->kv_heads * ceil_div(ceil_div(rows, p->sequences), by_rows.rows) * p->sequences;
-  const long long items_k = p->kv_heads * ceil_div(ceil_div(keys, p->sequences), by_keys.rows) * p->sequences;
   const int tile = bf16 ? 64 : 32;
-  const int splits_rows = parts_of(items_q, ceil_div(ceil_div(keys, p->sequences), tile), 4, 1024);
-  const int splits_keys = parts_of(items_k, ceil_div(ceil_div(rows, p->sequences), 32), 8, bf16 ? 2048 : 1024);
-  const size_t row_parts = splits_rows > 1 ? static_cast<size_t>(splits_rows) * p->kv_heads * rows * (4 * p->d + 8) : 0;
+  const long long key_tiles = ceil_div(ceil_div(keys, p->sequences), tile);
+  const int splits_rows = parts_of(items_of(rows, by_rows.rows), key_tiles, 4, 1024);
+  const int splits_keys = parts_of(items_of(keys, by_keys.rows), ceil_div(ceil_div(rows, p->sequences), 32), 8, bf16 ? 2048 : 1024);
+  const int splits_forward = few ? parts_of(items_of(rows, kPackFewRows), key_tiles, 4, 256) : splits_rows;
+  const int row_splits = splits_forward > splits_rows ? splits_forward : splits_rows;
+  const size_t row_parts = row_splits > 1 ? static_cast<size_t>(row_splits) * p->kv_heads * rows * (4 * p->d + 8) : 0;
   const size_t key_parts = splits_keys > 1 ? static_cast<size_t>(splits_keys) * 2 * p->kv_heads * keys * 4 * p->d : 0;
   float *parts = reinterpret_cast<float *>(take(row_parts > key_parts ? row_parts : key_parts));
   if (a) {
@@ -342,6 +353,8 @@ size_t packed_workspace(const scope_pack *p, void *base, PackArgs *a, PackCall *
     a->parts = parts;
     a->ends = header + 2;
     c->by_rows = by_rows;
+    c->forward = forward;
+    c->splits_forward = splits_forward;
     c->by_keys = by_keys;
     c->header = header;
     c->splits_rows = splits_rows;
@@ -357,7 +370,7 @@ bool packed_launchable(const scope_pack *p) {
   auto fits = [](long long capacity, long long heads, int splits, int threads) {
     return (capacity * splits + 7) / 8 * 8 * heads * threads < (1LL << 32);
   };
-  return fits(c.by_rows.capacity, p->kv_heads, c.splits_rows, 512) && fits(c.by_keys.capacity, p->kv_heads, c.splits_keys, 256) &&
+  return fits(c.by_rows.capacity, p->kv_heads, c.splits_rows, 512) && fits(c.forward.capacity, p->kv_heads, c.splits_forward, 256) && fits(c.by_keys.capacity, p->kv_heads, c.splits_keys, 256) &&
          static_cast<long long>(p->heads) * p->rows_q * (p->d / 4) < (1LL << 32) - 1024 &&
          static_cast<long long>(p->kv_heads) * p->rows_k * (p->d / 4) < (1LL << 32) - 1024;
 }

@@ -36,7 +36,7 @@ constexpr int kWaves = kPackRows / 32;  // a wave owns 32 rows
 // Wave w's share of a tile of keys' rows, 1 KB per load, through a resource that starts
 // at the tile (a sequence may be longer than 32-bit offsets reach); rows past the last
 // key repeat it, with no weight.
-template <int D, int N>
+template <int D, int N, int WAVES>
 struct KeyTile {
   static __device__ __forceinline__ void bring(char *base, int64_t stride, uint16_t *tile, int index, int lk, int w, int lane) {
     constexpr int CH = D / 8, RPL = 64 / CH;  // 16-byte chunks per row, rows per load
@@ -45,15 +45,15 @@ struct KeyTile {
                                                       static_cast<uint32_t>(rows - 1) * static_cast<uint32_t>(stride) + 2 * D);
     if (rows == N) {
 #pragma unroll
-      for (int i = 0; i < N / kWaves / RPL; ++i) {
-        const int r0 = N / kWaves * w + RPL * i, r = r0 + lane / CH;
+      for (int i = 0; i < N / WAVES / RPL; ++i) {
+        const int r0 = N / WAVES * w + RPL * i, r = r0 + lane / CH;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16,
                                                  r * static_cast<uint32_t>(stride) + 16 * ((lane % CH) ^ tile_swizzle<D>(r)), 0, 0, 0);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < N / kWaves / RPL; ++i) {
-        const int r0 = N / kWaves * w + RPL * i, r = r0 + lane / CH;
+      for (int i = 0; i < N / WAVES / RPL; ++i) {
+        const int r0 = N / WAVES * w + RPL * i, r = r0 + lane / CH;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(from, tile + r0 * D, 16,
                                                  min(r, rows - 1) * static_cast<uint32_t>(stride) + 16 * ((lane % CH) ^ tile_swizzle<D>(r)),
                                                  0, 0, 0);
@@ -62,26 +62,27 @@ struct KeyTile {
   }
 };
 
-template <int D, bool GRAD>
+template <int D, bool GRAD, bool FEW>
 __global__ __launch_bounds__(kWaves * 64)
-__attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : GRAD ? 2 : 3))) void packed_queries_kernel(PackArgs a, PackRows out) {
+__attribute__((amdgpu_waves_per_eu(FEW || (GRAD && D == 128) ? 2 : D == 64 ? 4 : 3))) void packed_queries_kernel(PackArgs a, PackRows out) {
   constexpr int KB = GRAD || D == 64 ? 2 : 1, N = 32 * KB;  // blocks of 32 keys in a tile, and its keys
-  __shared__ __attribute__((aligned(16))) uint16_t K0[N * D], K1[N * D], V0[N * D], V1[N * D];
+  constexpr int kItem = FEW ? kPackFewRows : kPackRows, kTiles = FEW ? kWaves : 1;  // rows; tiles in LDS
+  __shared__ __attribute__((aligned(16))) uint16_t K0[kTiles * N * D], K1[kTiles * N * D], V0[kTiles * N * D], V1[kTiles * N * D];
   int h, part, row0;
   int4 sq;
-  if (!pack_item<false, kPackRows>(a, &h, &part, &sq, &row0)) return;
+  if (!pack_item<false, kItem>(a, &h, &part, &sq, &row0)) return;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   TileReader<D> at(lane);
-  const int own = row0 + 32 * w + l32, row = min(own, rows - 1);
-  const bool valid = own < rows, active = row0 + 32 * w < rows;
+  const int w_row = row0 + (FEW ? 0 : 32 * w), own = w_row + l32, row = min(own, rows - 1);
+  const bool valid = own < rows, active = w_row < rows;
   const int query = row / a.group, member = row - query * a.group;
   const size_t stat = (static_cast<size_t>(h) * a.rows_q + q0) * a.group + row;  // of (key head, row)
   // keys that this row sees, and the wave's fewest and most
   const int seen = keys_seen(row, a.group, lq, lk, a.causal);
   const int fewest = __builtin_amdgcn_readlane(seen, 0), most = __builtin_amdgcn_readlane(seen, 31);
-  const int block_most = keys_seen(min(row0 + kPackRows, rows) - 1, a.group, lq, lk, a.causal);
+  const int block_most = keys_seen(min(row0 + kItem, rows) - 1, a.group, lq, lk, a.causal);
 
   bf16x8 qf[D / 16], gf[GRAD ? D / 16 : 1];
   {
@@ -126,8 +127,8 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : GRAD ? 2 : 3))) void packed_que
   const int last_own = scalar(active ? min(last, (most + N - 1) / N) : 0);
 
   char *const k_base = rows_base(a.k, k0, h), *const v_base = rows_base(a.v, k0, h);
-  auto bring_k = [&](uint16_t *tile, int index) { KeyTile<D, N>::bring(k_base, a.k.row, tile, index, lk, w, lane); };
-  auto bring_v = [&](uint16_t *tile, int index) { KeyTile<D, N>::bring(v_base, a.v.row, tile, index, lk, w, lane); };
+  auto bring_k = [&](uint16_t *tile, int index) { KeyTile<D, N, FEW ? 1 : kWaves>::bring(k_base, a.k.row, tile, index, lk, FEW ? 0 : w, lane); };
+  auto bring_v = [&](uint16_t *tile, int index) { KeyTile<D, N, FEW ? 1 : kWaves>::bring(v_base, a.v.row, tile, index, lk, FEW ? 0 : w, lane); };
   auto scores = [&](const uint16_t *kt, int kb) {
     f32x16 s;
 #pragma unroll
@@ -309,12 +310,18 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : GRAD ? 2 : 3))) void packed_que
     asm volatile("" : "+v"(at.row_at), "+v"(at.col_at));
   };
 
-  // one step: tile T computed while tile T + 1 is brought into the free buffers; every
-  // wave's loads land before the barrier
+  // one step: tile T computed while the next is brought into the free buffers.  Every wave
+  // takes all tiles, brought together: its loads land before the barrier.  FEW: a wave
+  // takes every kWaves-th tile, which it brings itself, and waits for no other.
+  constexpr int kStride = FEW ? kWaves : 1;
+  auto land = [&] {
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+    if constexpr (!FEW) __syncthreads();
+  };
   auto step = [&](int index, const uint16_t *kc, const uint16_t *vc, uint16_t *kn, uint16_t *vn) {
-    if (index + 1 < last) {
-      bring_k(kn, index + 1);
-      bring_v(vn, index + 1);
+    if (index + kStride < last) {
+      bring_k(kn, index + kStride);
+      bring_v(vn, index + kStride);
     }
     if (index < last_own) {
       if constexpr (GRAD)
@@ -322,21 +329,79 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : GRAD ? 2 : 3))) void packed_que
       else
         forward_tile(index, kc, vc);
     }
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-    __syncthreads();
+    land();
   };
-  if (first < last) {
-    bring_k(K0, first);
-    bring_v(V0, first);
+  const int start = first + (FEW ? w : 0), mine = FEW ? w * N * D : 0;
+  if (start < last) {
+    bring_k(K0 + mine, start);
+    bring_v(V0 + mine, start);
   }
-  __builtin_amdgcn_s_waitcnt(0x0F70);
-  __syncthreads();
-  for (int index = first; index < last; index += 2) {
-    step(index, K0, V0, K1, V1);
-    if (index + 1 < last) step(index + 1, K1, V1, K0, V0);
+  land();
+  for (int index = start; index < last; index += 2 * kStride) {
+    step(index, K0 + mine, V0 + mine, K1 + mine, V1 + mine);
+    if (index + kStride < last) step(index + kStride, K1 + mine, V1 + mine, K0 + mine, V0 + mine);
   }
 
-  const float l = l_run + __shfl_xor(l_run, 32);  // the halves of a row's sum
+  float l = l_run + __shfl_xor(l_run, 32);  // the halves of a row's sum
+  if constexpr (FEW) {
+    // the waves' sums, in wave order: a wave's share of the channels each
+    __shared__ float ms[kWaves][32], ls[kWaves][32];
+    // a wave's sums lie where its K tiles were, 16 bytes swizzled by the row
+    constexpr int kHalf = N / 2;  // rows in the first tile
+    auto sums = [&](int wave, int r, int c) {
+      uint16_t *tile = (r < kHalf ? K0 : K1) + wave * N * D;
+      return reinterpret_cast<float4 *>(tile) + (r % kHalf) * (D / 4) + ((c / 4) ^ (r & 15));
+    };
+    if (hf == 0) {
+      ms[w][l32] = m_run;
+      ls[w][l32] = l;
+    }
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *sums(w, l32, 32 * db + 8 * x + 4 * hf) =
+            make_float4(acc[db][4 * x], acc[db][4 * x + 1], acc[db][4 * x + 2], acc[db][4 * x + 3]);
+    __syncthreads();
+    m_run = fmaxf(fmaxf(ms[0][l32], ms[1][l32]), fmaxf(ms[2][l32], ms[3][l32]));
+    static_assert(kWaves == 4, "four waves' sums");
+    l = 0.0f;
+    float f[kWaves];
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      f[i] = __builtin_amdgcn_exp2f(ms[i][l32] - (m_run == -INFINITY ? 0.0f : m_run));
+      l = fmaf(ls[i][l32], f[i], l);
+    }
+    if (!valid) return;
+    const size_t total = static_cast<size_t>(a.kv_heads) * a.rows_q * a.group, i = part * total + stat;
+    const float scale = a.splits > 1 ? 1.0f : l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+    if (w == 0 && hf == 0) {
+      if (a.splits > 1)
+        reinterpret_cast<float2 *>(a.parts + a.splits * total * D)[i] = make_float2(m_run, l);
+      else
+        a.lse[static_cast<size_t>(h * a.group + member) * a.rows_q + q0 + query] =
+            l > 0.0f ? (m_run + __log2f(l)) * kPackLn2 : l == 0.0f ? -INFINITY : l;
+    }
+    uint16_t *to = reinterpret_cast<uint16_t *>(rows_base(out, q0, h * a.group) + query * out.row + member * out.head);
+#pragma unroll
+    for (int x = 0; x < D / kWaves / 8; ++x) {
+      const int c = D / kWaves * w + 8 * x + 4 * hf;
+      float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int j = 0; j < kWaves; ++j) {
+        const float4 v = *sums(j, l32, c);
+        s.x = fmaf(v.x, f[j], s.x);
+        s.y = fmaf(v.y, f[j], s.y);
+        s.z = fmaf(v.z, f[j], s.z);
+        s.w = fmaf(v.w, f[j], s.w);
+      }
+      if (a.splits > 1)
+        *reinterpret_cast<float4 *>(a.parts + i * D + c) = s;
+      else
+        *reinterpret_cast<uint2 *>(to + c) = make_uint2(pack_bf16(s.x * scale, s.y * scale), pack_bf16(s.z * scale, s.w * scale));
+    }
+    return;
+  }
   if (!valid) return;
   if (a.splits > 1) {  // the part's sums, and the forward's maximum and normaliser
     const size_t total = static_cast<size_t>(a.kv_heads) * a.rows_q * a.group, i = part * total + stat;
@@ -366,18 +431,19 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : GRAD ? 2 : 3))) void packed_que
                                                                      pack_bf16(acc[db][4 * x + 2] * f, acc[db][4 * x + 3] * f));
 }
 
-template <int D, bool GRAD>
+template <int D, bool GRAD, bool FEW>
 hipError_t run(const PackArgs &a, const PackRows &out, hipStream_t s) {
   const dim3 grid(pack_blocks(a.list.capacity, a.kv_heads, a.splits));
-  hipLaunchKernelGGL((packed_queries_kernel<D, GRAD>), grid, dim3(kWaves * 64), 0, s, a, out);
+  hipLaunchKernelGGL((packed_queries_kernel<D, GRAD, FEW>), grid, dim3(kWaves * 64), 0, s, a, out);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t packed_queries(const PackArgs &a, int d, bool grad, const PackRows &out, hipStream_t s) {
-  if (d == 128) return grad ? run<128, true>(a, out, s) : run<128, false>(a, out, s);
-  return grad ? run<64, true>(a, out, s) : run<64, false>(a, out, s);
+  if (a.list.rows == kPackFewRows) return d == 128 ? run<128, false, true>(a, out, s) : run<64, false, true>(a, out, s);
+  if (d == 128) return grad ? run<128, true, false>(a, out, s) : run<128, false, false>(a, out, s);
+  return grad ? run<64, true, false>(a, out, s) : run<64, false, false>(a, out, s);
 }
 
 }  // namespace scope

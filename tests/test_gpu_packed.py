@@ -77,6 +77,8 @@ LENGTHS = {
     "chunks": ([33, 3, 128], [500, 230, 129]),
     "tokens": ([1] * 9, [64, 65, 1, 63, 700, 128, 2, 300, 127]),
     "parts": ([37], [3001]),
+    "few": ([2, 1, 3, 1], [1500, 900, 3, 2100]),    # a block's waves share out the keys
+    "few_ragged": ([90, 1, 0, 4], [200, 700, 5, 3]),
     "long": ([1200], [1100]),
     "seventy": ([i % 5 for i in range(70)], [(3 * i) % 7 for i in range(70)]),
 }
