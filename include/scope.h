@@ -505,9 +505,8 @@ int32_t scope_packed_workspace_size(const scope_pack *pack, size_t *bytes);
  * (scale <= 0 selects 1/sqrt(d)).  A query that sees no key gives O = 0 and
  * lse = -inf.  Rows in no sequence are left as they were, and key rows in none are
  * not read.  Types as call 6 (fp32 inputs are not rounded, bf16 weights are); sums
- * and statistics are fp32.  A non-finite value row may reach queries of its sequence
- * up to 63 places before the first that sees it, or 31 keys' worth for a few queries;
- * a non-finite key row reaches only queries that see it.
+ * and statistics are fp32.  A non-finite key row reaches only queries that see it; a
+ * non-finite value row may also reach queries that see a key up to 63 before it.
  * Results repeat bit for bit.  Long sums may be cut into parts, whose number follows
  * from the sizes in `pack` alone.
  * Bad offsets cannot fault: each is taken as the largest so far within [0, rows] and
