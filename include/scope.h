@@ -506,7 +506,7 @@ int32_t scope_packed_workspace_size(const scope_pack *pack, size_t *bytes);
  * lse = -inf.  Rows in no sequence are left as they were, and key rows in none are
  * not read.  Types as call 6 (fp32 inputs are not rounded, bf16 weights are); sums
  * and statistics are fp32.  A non-finite key row reaches only queries that see it; a
- * non-finite value row may also reach queries that see a key up to 63 before it.
+ * non-finite value row may also reach queries whose last key lies up to 94 before it.
  * Results repeat bit for bit.  Long sums may be cut into parts, whose number follows
  * from the sizes in `pack` alone.
  * Bad offsets cannot fault: each is taken as the largest so far within [0, rows] and
