@@ -248,7 +248,10 @@ __global__ __launch_bounds__(256) void pack_join_keys_kernel(PackArgs a, PackRow
 // Parts that an item's tiles are cut into: as many as make `blocks` of the items, up to
 // 16 of `least` tiles or more.  The chip holds 512 to 768 blocks at once; items differ in
 // length as sequences do, and causal rows in keys, so that 1024 (dK and dV of bf16 inputs,
-// whose longest items take longest: 2048) end more evenly.  4 sequences of 512 queries
+// whose longest items take longest: 2048) end more evenly.  A tile of fp32 takes longer and
+// its join no longer, so that 2 tiles are enough for a part (6 sequences of 1224 tokens, 9
+// heads of 3: the whole backward 152 us for 293 with 4 and 8), where bf16's forward wants 4
+// (5 sequences of 1035 tokens, 32 heads of 8: 26 us for 36 with 2).  4 sequences of 512 queries
 // behind 5000 to 16000 keys, 16 heads in groups of 4: 276 us with 512, 212 with 1024; 24
 // prompts of 22 to 6600 tokens, d = 64, dK and dV: 797 us whole, 571 in two parts, joining
 // them included; single tokens of 16 sequences behind up to 8000 keys 43 us with 512, 39
@@ -341,8 +344,15 @@ size_t packed_workspace(const scope_pack *p, void *base, PackArgs *a, PackCall *
   float *stats = reinterpret_cast<float *>(take(8 * static_cast<size_t>(p->kv_heads) * rows));
   const int tile = bf16 ? 64 : 32;
   const long long key_tiles = ceil_div(ceil_div(keys, p->sequences), tile);
-  const int splits_rows = parts_of(items_of(rows, by_rows.rows), key_tiles, 4, 1024);
-  const int splits_keys = parts_of(items_of(keys, by_keys.rows), ceil_div(ceil_div(rows, p->sequences), 32), 8, bf16 ? 2048 : 1024);
+  const int splits_rows = parts_of(items_of(rows, by_rows.rows), key_tiles, bf16 ? 4 : 2, 1024);
+  // An item of dK and dV writes 2 x 128 fp32 rows a part: short parts (2 tiles) only up to
+  // the 512 blocks that the chip holds at once, long ones (8) beyond, to even out the ends.
+  // bf16, 24 sequences of 760 tokens in all, 24 heads of 3: the whole backward 42 us for 64
+  // with 8 alone; 11 sequences of 4996 tokens, 4 heads of one 134 for 145; but with 4 and
+  // 2048 blocks alone 17 sequences of 13527 tokens, 2 heads, took 73 us for 60.
+  const long long key_items = items_of(keys, by_keys.rows), row_tiles = ceil_div(ceil_div(rows, p->sequences), 32);
+  const int fill = parts_of(key_items, row_tiles, 2, bf16 ? 512 : 1024), even = parts_of(key_items, row_tiles, 8, 2048);
+  const int splits_keys = bf16 && even > fill ? even : fill;
   const int splits_forward = few ? parts_of(items_of(rows, kPackFewRows), key_tiles, 4, 256) : splits_rows;
   const int row_splits = splits_forward > splits_rows ? splits_forward : splits_rows;
   const size_t row_parts = row_splits > 1 ? static_cast<size_t>(row_splits) * p->kv_heads * rows * (4 * p->d + 8) : 0;
