@@ -126,6 +126,14 @@ def test_parts_follow_from_sizes():
     check(R.make(4, 1, [4000], [30], 64, "bf16", seed=9), False)     # dK, dV in parts
 
 
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "bf16"), (64, "f32"), (128, "f32")])
+def test_more_parts_than_tiles(d, dtype, causal):
+    """Parts follow from the average length: a short sequence's items have fewer tiles."""
+    check(R.make(8, 1, [700, 1, 40, 0], [700, 1, 60, 5], d, dtype, seed=10, before=1, after=2), causal)
+    check(R.make(2, 2, [900, 3], [2, 900], d, dtype, seed=11), causal)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_cache_with_room(dtype):
     """Keys behind a cache's length are not read into any result, whatever they hold."""
