@@ -484,7 +484,8 @@ int32_t scope_rotary(const scope_rotation *rotation, const int32_t *positions,
  * (call 10) the first lengths_k[s] of those, a cache with room for more.  Lengths may
  * differ and be 0.  With n queries and m keys of a sequence, query i sees every key,
  * or where `causal` the keys j <= i + m - n: the last query sees all, queries before
- * the first key see none.
+ * the first key see none.  Output rows in no sequence (before the first offset or
+ * from the last on) are left as they were, or where `clear` set to 0, lse to -inf.
  * Supported: d in {64, 128}, 1 <= sequences <= 65536, 0 <= rows <= 2^24, heads * rows
  * < 2^31 each, at most 2^30 queries of one key head, so few items that a launch needs
  * less than 2^32 threads; 16-byte aligned rows (pointers and strides); 66 rows in a row,
@@ -494,6 +495,7 @@ typedef struct {
   int32_t rows_q, rows_k; /* rows of q, o; of k, v */
   int32_t sequences;
   int32_t d, dtype, causal;
+  int32_t clear;          /* output rows in no sequence: 0 as they were, else set */
 } scope_pack;
 
 /* Workspace bytes that suffice for calls 10 and 11 with these sizes.        */
@@ -503,8 +505,7 @@ int32_t scope_packed_workspace_size(const scope_pack *pack, size_t *bytes);
  *   lse_i = log sum_j exp(scale <q_i, k_j>)   (fp32, natural log; [heads][rows_q])
  *   O_i   = sum_j exp(scale <q_i, k_j> - lse_i) v_j,  j over the keys that i sees
  * (scale <= 0 selects 1/sqrt(d)).  A query that sees no key gives O = 0 and
- * lse = -inf.  Rows in no sequence are left as they were, and key rows in none are
- * not read.  Types as call 6 (fp32 inputs are not rounded, bf16 weights are); sums
+ * lse = -inf.  Rows in no sequence are not read, those of O and lse as `clear` says.  Types as call 6 (fp32 inputs are not rounded, bf16 weights are); sums
  * and statistics are fp32.  A non-finite key row reaches only queries that see it; a
  * non-finite value row may also reach queries whose last key lies up to 94 before it.
  * Results repeat bit for bit.  Long sums may be cut into parts, whose number follows
@@ -524,7 +525,7 @@ int32_t scope_packed_attention(const scope_pack *pack, const void *q,
 /* 11. Gradients of call 10 (without lengths_k), formulas and types as call 7
  * without dropout: dK and dV sum over the query heads that share the key head.  dK
  * and dV are 0 for keys of a sequence that no query sees, dQ for queries that see no
- * key; rows in no sequence are left as they were.  A non-finite row of Q or d_o may
+ * key; rows in no sequence as `clear` says.  A non-finite row of Q or d_o may
  * reach dK and dV of keys of its sequence that it does not see, a non-finite row of
  * K or V dQ of queries that do not see it.  No gradient may overlap an input or
  * another one.  Otherwise as call 10.                                        */

@@ -113,12 +113,12 @@ def make_rotation(rows, heads, d, dtype, ranges, layout="pairs", inverse=False,
 
 class Pack(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("heads", "kv_heads", "rows_q", "rows_k",
-                                              "sequences", "d", "dtype", "causal")]
+                                              "sequences", "d", "dtype", "causal", "clear")]
 
 
-def make_pack(heads, kv_heads, rows_q, rows_k, sequences, d, dtype, causal) -> Pack:
+def make_pack(heads, kv_heads, rows_q, rows_k, sequences, d, dtype, causal, clear=False) -> Pack:
     return Pack(int(heads), int(kv_heads), int(rows_q), int(rows_k), int(sequences), int(d),
-                int(dtype), int(bool(causal)))
+                int(dtype), int(bool(causal)), int(bool(clear)))
 
 
 _lib = None

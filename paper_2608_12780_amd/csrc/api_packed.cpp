@@ -109,6 +109,7 @@ void set_pack(const scope_pack *p, const int32_t *offsets_q, const int32_t *offs
   a->rows_k = p->rows_k;
   a->sequences = p->sequences;
   a->causal = p->causal != 0;
+  a->clear = p->clear != 0;
   a->offsets_q = offsets_q;
   a->offsets_k = offsets_k;
   a->lengths_k = lengths_k;

@@ -363,7 +363,7 @@ struct PackList {
   int capacity;   // items at most
 };
 struct PackArgs {
-  int kv_heads, group, rows_q, rows_k, sequences, causal;
+  int kv_heads, group, rows_q, rows_k, sequences, causal, clear;
   PackRows q, k, v, o, d_o;  // o: gradients
   const int32_t *offsets_q, *offsets_k, *lengths_k;
   float scale, scale_log2;

@@ -21,7 +21,11 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : 2))) void packed_queries_f32_ke
   __shared__ __attribute__((aligned(16))) float K0[T::kFloats], K1[T::kFloats], V0[T::kFloats], V1[T::kFloats];
   int h, part, row0;
   int4 sq;
-  if (!pack_item<false, kPackRowsF32>(a, &h, &part, &sq, &row0)) return;
+  int2 ends;
+  const bool item = pack_item<false, kPackRowsF32>(a, &h, &part, &sq, &row0, &ends);
+  if (a.clear && a.splits == 1)
+    clear_rows<float, D, kThreads>(out, a.kv_heads * a.group, a.rows_q, ends, GRAD ? nullptr : a.lse);
+  if (!item) return;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -166,7 +170,13 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_f32_kerne
   __shared__ __attribute__((aligned(16))) float Q0[kQ], Q1[kQ], G0[T::kFloats], G1[T::kFloats];
   int h, part, key0;
   int4 sq;
-  if (!pack_item<true, kPackRowsF32>(a, &h, &part, &sq, &key0)) return;
+  int2 ends;
+  const bool item = pack_item<true, kPackRowsF32>(a, &h, &part, &sq, &key0, &ends);
+  if (a.clear && a.splits == 1) {
+    clear_rows<float, D, kThreads>(dk, a.kv_heads, a.rows_k, ends, nullptr);
+    clear_rows<float, D, kThreads>(dv, a.kv_heads, a.rows_k, ends, nullptr);
+  }
+  if (!item) return;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);

@@ -54,7 +54,13 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_kernel(Pa
   __shared__ __attribute__((aligned(16))) uint16_t Vs[VLDS ? kPackKeys * D : 8];
   int h, part, key0;
   int4 sq;
-  if (!pack_item<true, kPackKeys>(a, &h, &part, &sq, &key0)) return;
+  int2 ends;
+  const bool item = pack_item<true, kPackKeys>(a, &h, &part, &sq, &key0, &ends);
+  if (a.clear && a.splits == 1) {
+    clear_rows<uint16_t, D, 64 * kWaves>(dk, a.kv_heads, a.rows_k, ends, nullptr);
+    clear_rows<uint16_t, D, 64 * kWaves>(dv, a.kv_heads, a.rows_k, ends, nullptr);
+  }
+  if (!item) return;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);

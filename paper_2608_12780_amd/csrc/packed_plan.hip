@@ -161,6 +161,15 @@ __global__ __launch_bounds__(kThreads) void pack_lists_kernel(PackLists p) {
   }
 }
 
+// Four channels of an output row.
+template <typename T>
+__device__ __forceinline__ void store4(T *to, float x, float y, float z, float w) {
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(x, y), pack_bf16(z, w));
+  else
+    *reinterpret_cast<float4 *>(to) = make_float4(x, y, z, w);
+}
+
 // O and lse, or dQ, from the parts' sums.  A group of D / 4 lanes per row.
 template <typename T, int D, bool GRAD>
 __global__ __launch_bounds__(256) void pack_join_rows_kernel(PackArgs a, PackRows out) {
@@ -172,7 +181,13 @@ __global__ __launch_bounds__(256) void pack_join_rows_kernel(PackArgs a, PackRow
   if (row >= rows) return;
   const int kv = static_cast<int>(row / per), r = static_cast<int>(row % per);
   const int query = r / a.group, head = kv * a.group + r % a.group;
-  if (query < ends.x || query >= ends.y) return;
+  T *to = reinterpret_cast<T *>(rows_base(out, query, head)) + 4 * x;
+  if (query < ends.x || query >= ends.y) {  // in no sequence
+    if (!a.clear) return;
+    store4(to, 0.0f, 0.0f, 0.0f, 0.0f);
+    if (!GRAD && x == 0) a.lse[static_cast<size_t>(head) * a.rows_q + query] = -INFINITY;
+    return;
+  }
   const float2 *ml = reinterpret_cast<const float2 *>(a.parts + a.splits * rows * D);
   // all parts' maxima and normalisers at once: their loads' latency is most of a small join
   float w[kMostParts], f = a.scale;
@@ -203,11 +218,7 @@ __global__ __launch_bounds__(256) void pack_join_rows_kernel(PackArgs a, PackRow
     s.z = fmaf(v.z, g, s.z);
     s.w = fmaf(v.w, g, s.w);
   }
-  T *to = reinterpret_cast<T *>(rows_base(out, query, head)) + 4 * x;
-  if constexpr (sizeof(T) == 2)
-    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(s.x * f, s.y * f), pack_bf16(s.z * f, s.w * f));
-  else
-    *reinterpret_cast<float4 *>(to) = make_float4(s.x * f, s.y * f, s.z * f, s.w * f);
+  store4(to, s.x * f, s.y * f, s.z * f, s.w * f);
 }
 
 // dK (blockIdx.y 0) and dV from the parts' sums.
@@ -220,8 +231,12 @@ __global__ __launch_bounds__(256) void pack_join_keys_kernel(PackArgs a, PackRow
   const int2 ends = pack_ends(a, true);
   if (row >= rows) return;
   const int head = static_cast<int>(row / a.rows_k), key = static_cast<int>(row % a.rows_k);
-  if (key < ends.x || key >= ends.y) return;
   const int v = blockIdx.y;
+  T *to = reinterpret_cast<T *>(rows_base(v ? dv : dk, key, head)) + 4 * x;
+  if (key < ends.x || key >= ends.y) {
+    if (a.clear) store4(to, 0.0f, 0.0f, 0.0f, 0.0f);
+    return;
+  }
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
   for (int p = 0; p < a.splits; ++p) {
@@ -232,11 +247,7 @@ __global__ __launch_bounds__(256) void pack_join_keys_kernel(PackArgs a, PackRow
     s.w += y.w;
   }
   const float f = v ? 1.0f : a.scale;
-  T *to = reinterpret_cast<T *>(rows_base(v ? dv : dk, key, head)) + 4 * x;
-  if constexpr (sizeof(T) == 2)
-    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(s.x * f, s.y * f), pack_bf16(s.z * f, s.w * f));
-  else
-    *reinterpret_cast<float4 *>(to) = make_float4(s.x * f, s.y * f, s.z * f, s.w * f);
+  store4(to, s.x * f, s.y * f, s.z * f, s.w * f);
 }
 
 #define PACK_TRY(x)                  \

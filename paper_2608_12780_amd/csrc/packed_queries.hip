@@ -70,7 +70,11 @@ __attribute__((amdgpu_waves_per_eu(FEW || (GRAD && D == 128) ? 2 : D == 64 ? 4 :
   __shared__ __attribute__((aligned(16))) uint16_t K0[kTiles * N * D], K1[kTiles * N * D], V0[kTiles * N * D], V1[kTiles * N * D];
   int h, part, row0;
   int4 sq;
-  if (!pack_item<false, kItem>(a, &h, &part, &sq, &row0)) return;
+  int2 ends;
+  const bool item = pack_item<false, kItem>(a, &h, &part, &sq, &row0, &ends);
+  if (a.clear && a.splits == 1)
+    clear_rows<uint16_t, D, kWaves * 64>(out, a.kv_heads * a.group, a.rows_q, ends, GRAD ? nullptr : a.lse);
+  if (!item) return;
   const int q0 = sq.x, lq = sq.y, k0 = sq.z, lk = sq.w, rows = lq * a.group;
   const int t = threadIdx.x, lane = t & 63, l32 = lane & 31, hf = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);

@@ -24,8 +24,8 @@ def offsets_of(lengths, device="cuda"):
 class _PackedFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, owner, offsets_q, offsets_k, scale):
-        out, lse = owner._forward(q, k, v, offsets_q, offsets_k, None, scale, owner.outputs(),
-                                  owner._workspace(None), None)
+        out, lse = owner._forward(owner.pack, q, k, v, offsets_q, offsets_k, None, scale,
+                                  owner.outputs(), owner._workspace(None), None)
         # the sequences are those that the offsets hold now
         ctx.save_for_backward(q, k, v, out, lse, offsets_q.clone(), offsets_k.clone())
         ctx.owner, ctx.scale = owner, scale
@@ -40,8 +40,8 @@ class _PackedFunction(torch.autograd.Function):
             d_out = d_out.clone(memory_format=torch.contiguous_format)
         # rows in no sequence have no gradient
         into = tuple(torch.zeros(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-        grads = owner._backward(q, k, v, out, lse, d_out, offsets_q, offsets_k, ctx.scale, into,
-                                owner._workspace(None), None)
+        grads = owner._backward(owner.pack, q, k, v, out, lse, d_out, offsets_q, offsets_k, ctx.scale,
+                                into, owner._workspace(None), None)
         return (*(g if need else None for g, need in zip(grads, ctx.needs_input_grad)),
                 None, None, None, None)
 
@@ -65,7 +65,11 @@ class PackedAttention:
                  device="cuda", workspace=True):
         self.dtype = B.BF16 if dtype == "bf16" else B.F32
         self.tdtype = torch.bfloat16 if self.dtype == B.BF16 else torch.float32
-        self.pack = B.make_pack(heads, kv_heads, rows_q, rows_k, sequences, d, self.dtype, causal)
+        sizes = (heads, kv_heads, rows_q, rows_k, sequences, d, self.dtype, causal)
+        self.pack = B.make_pack(*sizes)
+        # into the buffers that this object holds: they have rows of earlier calls, whose
+        # offsets may have covered more
+        self._clearing = B.make_pack(*sizes, clear=True)
         self.device = torch.device(device)
         B.scope_packed_workspace_size(self.pack)  # refuses what the calls would
         self.workspace = B.alloc_packed_workspace(self.pack, device) if workspace else None
@@ -90,39 +94,46 @@ class PackedAttention:
                      for h, n in ((p.heads, p.rows_q), (p.kv_heads, p.rows_k),
                                   (p.kv_heads, p.rows_k)))
 
-    def _forward(self, q, k, v, offsets_q, offsets_k, lengths_k, scale, into, workspace, stream):
-        B.scope_packed_attention(self.pack, q, k, v, offsets_q, offsets_k, lengths_k, scale, *into,
+    def _forward(self, pack, q, k, v, offsets_q, offsets_k, lengths_k, scale, into, workspace,
+                 stream):
+        B.scope_packed_attention(pack, q, k, v, offsets_q, offsets_k, lengths_k, scale, *into,
                                  workspace, self.status, stream)
         return into
 
-    def _backward(self, q, k, v, out, lse, d_out, offsets_q, offsets_k, scale, into, workspace,
-                  stream):
-        B.scope_packed_attention_backward(self.pack, q, k, v, out, lse, d_out, offsets_q, offsets_k,
+    def _backward(self, pack, q, k, v, out, lse, d_out, offsets_q, offsets_k, scale, into,
+                  workspace, stream):
+        B.scope_packed_attention_backward(pack, q, k, v, out, lse, d_out, offsets_q, offsets_k,
                                           scale, *into, workspace, self.status, stream)
         return into
 
     def forward(self, q, k, v, offsets_q, offsets_k=None, lengths_k=None, scale=0.0, into=None,
                 stream=None):
-        """Returns (out, lse): `into`, or the buffers this object holds.  offsets_q and
+        """Returns (out, lse): `into`, whose rows in no sequence stay as they are, or the
+        buffers this object holds, where they are set to 0 and -inf.  offsets_q and
         offsets_k (the same where not given) are int32 [sequences + 1]; lengths_k, int32
         [sequences], the keys that each sequence's rows of k and v hold so far."""
+        pack = self.pack
         if into is None:
             with _allocating_on(stream):
                 self._out = into = self._out or self.outputs()
+            pack = self._clearing
         offsets_k = offsets_q if offsets_k is None else offsets_k
         workspace = self._workspace(stream) if self.workspace is None else self.workspace
-        return self._forward(q, k, v, offsets_q, offsets_k, lengths_k, scale, into, workspace,
+        return self._forward(pack, q, k, v, offsets_q, offsets_k, lengths_k, scale, into, workspace,
                              stream)
 
     def backward(self, q, k, v, out, lse, d_out, offsets_q, offsets_k=None, scale=0.0, into=None,
                  stream=None):
-        """Returns (dq, dk, dv): `into`, or the buffers this object holds."""
+        """Returns (dq, dk, dv): `into`, whose rows in no sequence stay as they are, or the
+        buffers this object holds, where they are set to 0."""
+        pack = self.pack
         if into is None:
             with _allocating_on(stream):
                 self._grads = into = self._grads or self.gradients()
+            pack = self._clearing
         offsets_k = offsets_q if offsets_k is None else offsets_k
         workspace = self._workspace(stream) if self.workspace is None else self.workspace
-        return self._backward(q, k, v, out, lse, d_out, offsets_q, offsets_k, scale, into,
+        return self._backward(pack, q, k, v, out, lse, d_out, offsets_q, offsets_k, scale, into,
                               workspace, stream)
 
     def attention(self, q, k, v, offsets_q, offsets_k=None, scale=0.0):
