@@ -459,7 +459,8 @@ typedef struct {
  * Sines and cosines are fp32 within 2^-22, products fp32, y rounded once.
  * A second tensor x2 -> y2 of heads[1] heads and the same positions (keys with
  * their queries) is turned by the same launch; heads[1] = 0: none.
- * y may be x with the same strides; otherwise they must not overlap (nor y, y2).
+ * y may be x, and y2 x2, with the same strides; otherwise an output must not overlap
+ * an input, its own or the other tensor's, nor the other output.
  * Requires rows >= 0, 1 <= heads[0], 2 <= d <= 1024 even, 1 <= axes <= 3, a finite
  * factor; every size below 2^31.  Any alignment of whole elements is taken;
  * 16-byte alignment of pointers and strides, with d (and for halves ranges'

@@ -169,8 +169,7 @@ int32_t scope_rotary(const scope_rotation *r, const int32_t *positions, const ui
   const void *xs[2] = {x, x2};
   void *ys[2] = {y, y2};
   const scope_strides *sx[2] = {x_strides, x2_strides}, *sy[2] = {y_strides, y2_strides};
-  bool dense[2] = {false, false};
-  int64_t bytes[2] = {0, 0};
+  int64_t x_bytes[2] = {0, 0}, y_bytes[2] = {0, 0};  // of tensors that are one block of memory
   for (int i = 0; i < 2; ++i) {
     const int heads = a.heads[i] = r->heads[i];
     if (!heads) continue;
@@ -190,13 +189,20 @@ int32_t scope_rotary(const scope_rotation *r, const int32_t *positions, const ui
     const int64_t whole = static_cast<int64_t>(heads) * r->rows * r->d;
     if (r->rows && xs[i] == ys[i] && (a.xs[i].row != a.ys[i].row || a.xs[i].head != a.ys[i].head) && whole > r->d)
       return SCOPE_ERR_INVALID_ARGUMENT;
-    if (r->rows && xs[i] != ys[i] && ex == whole && ey == whole && overlap(xs[i], ex * el, ys[i], ey * el))
-      return SCOPE_ERR_INVALID_ARGUMENT;
-    dense[i] = ey == whole;
-    bytes[i] = ey * el;
+    x_bytes[i] = ex == whole ? ex * el : 0;
+    y_bytes[i] = ey == whole ? ey * el : 0;
   }
-  if (r->rows && r->heads[1] && (y == y2 || (dense[0] && dense[1] && overlap(y, bytes[0], y2, bytes[1]))))
-    return SCOPE_ERR_INVALID_ARGUMENT;
+  // the same memory, or blocks of it that overlap (rows of one projection may interleave)
+  auto meet = [](const void *p, int64_t p_bytes, const void *q, int64_t q_bytes) {
+    return p == q || (p_bytes && q_bytes && overlap(p, p_bytes, q, q_bytes));
+  };
+  for (int i = 0; i < 2 && r->rows; ++i) {
+    if (!a.heads[i]) continue;
+    if (xs[i] != ys[i] && meet(xs[i], x_bytes[i], ys[i], y_bytes[i])) return SCOPE_ERR_INVALID_ARGUMENT;
+    // a thread stores heads of one tensor before it, or another, has loaded the other's
+    if (a.heads[1 - i] && meet(ys[i], y_bytes[i], xs[1 - i], x_bytes[1 - i])) return SCOPE_ERR_INVALID_ARGUMENT;
+  }
+  if (r->rows && r->heads[1] && meet(y, y_bytes[0], y2, y_bytes[1])) return SCOPE_ERR_INVALID_ARGUMENT;
   if (static_cast<int64_t>(r->rows) * r->d >= (1LL << 32) - 256) return SCOPE_ERR_UNSUPPORTED;  // threads of a launch
   if (!r->rows) return SCOPE_OK;
   return scope::rotary_run(a, r->dtype == SCOPE_BF16, pairs, vectors, r->d, static_cast<hipStream_t>(stream)) == hipSuccess

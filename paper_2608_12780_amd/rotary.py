@@ -114,8 +114,8 @@ class Rotary:
         """x [heads][n][d] (bf16 or fp32, any strides of heads and tokens) turned by
         positions, int32 [axes][n] or, with one axis, [n]; with x2, of other heads,
         both by one launch, as a pair.  inverse turns back, times the same factor:
-        the gradient.  Into `out` (a tensor, or a pair with x2; it may be the input)
-        or new tensors [heads][n][d].  Differentiable in x and x2 except into `out`,
+        the gradient.  Into `out` (a tensor, or a pair with x2; each may be its own
+        input, not the other's) or new tensors [heads][n][d].  Differentiable in x and x2 except into `out`,
         which is refused where a gradient is asked for."""
         if x.dim() != 3 or x.shape[2] != self.d:
             raise ValueError(f"x must be [heads][n][{self.d}], is {tuple(x.shape)}")
