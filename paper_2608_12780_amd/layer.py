@@ -15,6 +15,7 @@ from __future__ import annotations
 import contextlib
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding as B
 
@@ -23,6 +24,14 @@ def _allocating_on(stream):
     """Where a call allocates what it runs `stream` on: memory that torch's
     allocator gives out for another stream may still be in use there."""
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _refuse_tangents(name, *tensors):
+    """Raises where forward-mode differentiation follows one of the tensors: the result
+    would come without its tangent."""
+    if forward_ad._current_level >= 0 and any([
+            t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors]):
+        raise NotImplementedError(f"{name} has no forward-mode derivative")
 
 
 class TrainingAttention:

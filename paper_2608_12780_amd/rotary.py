@@ -12,7 +12,7 @@ import math
 import torch
 
 from . import binding as B
-from .layer import _allocating_on
+from .layer import _allocating_on, _refuse_tangents
 
 
 def frequencies(length, theta=10000.0, scaling=None, context=4096):
@@ -115,8 +115,9 @@ class Rotary:
         positions, int32 [axes][n] or, with one axis, [n]; with x2, of other heads,
         both by one launch, as a pair.  inverse turns back, times the same factor:
         the gradient.  Into `out` (a tensor, or a pair with x2; each may be its own
-        input, not the other's) or new tensors [heads][n][d].  Differentiable in x and x2 except into `out`,
-        which is refused where a gradient is asked for."""
+        input, not the other's) or new tensors [heads][n][d].  Differentiable in x and x2 (in
+        reverse mode; forward mode is refused) except into `out`, which is refused
+        where a gradient is asked for."""
         if x.dim() != 3 or x.shape[2] != self.d:
             raise ValueError(f"x must be [heads][n][{self.d}], is {tuple(x.shape)}")
         if x2 is not None and (x2.dim() != 3 or x2.shape[1:] != x.shape[1:] or x2.dtype != x.dtype):
@@ -128,6 +129,7 @@ class Rotary:
         if out is not None and (len(given) != (1 if x2 is None else 2)
                                 or any([t is None for t in given])):
             raise ValueError("out needs a tensor for each input")
+        _refuse_tangents("rotate", x, x2, *given)
         if torch.is_grad_enabled() and any([t is not None and t.requires_grad
                                             for t in (x, x2, *given)]):
             if given:
