@@ -152,11 +152,12 @@ class _DropoutFunction(torch.autograd.Function):
 
 def dropout(x, p, rng, residual=None, out=None, stream=None):
     """x / (1 - p) where kept, else 0, plus `residual` (call 8), into `out` or a
-    new tensor; differentiable in x and residual, except into `out`, which is
-    refused where a gradient is asked for.  `rng` is an int64 tensor (seed,
+    new tensor; differentiable in x and residual (in reverse mode; forward mode is
+    refused), except into `out`, which is refused where a gradient is asked for.  `rng` is an int64 tensor (seed,
     offset) on the GPU."""
     if residual is not None and residual.shape != x.shape:
         raise ValueError(f"residual is {tuple(residual.shape)}, x {tuple(x.shape)}")
+    _refuse_tangents("dropout", x, residual, out)
     if torch.is_grad_enabled() and (
             x.requires_grad or residual is not None and residual.requires_grad
             or out is not None and out.requires_grad):
