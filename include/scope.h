@@ -488,7 +488,7 @@ int32_t scope_rotary(const scope_rotation *rotation, const int32_t *positions,
  * the first key see none.  Output rows in no sequence (before the first offset or
  * from the last on) are left as they were, or where `clear` set to 0, lse to -inf.
  * Supported: d in {64, 128}, 1 <= sequences <= 65536, 0 <= rows <= 2^24, heads * rows
- * < 2^31 each, at most 2^30 queries of one key head, so few items that a launch needs
+ * < 2^31 each, fewer than 2^30 queries of one key head, so few items that a launch needs
  * less than 2^32 threads; 16-byte aligned rows (pointers and strides); 66 rows in a row,
  * of one key head or of all query heads that share it, within 2^32 bytes.     */
 typedef struct {

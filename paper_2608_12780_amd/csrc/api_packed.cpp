@@ -68,7 +68,8 @@ int32_t check_pack(const scope_pack *p) {
   if (p->heads > 65535 || p->rows_q > kMaxRows || p->rows_k > kMaxRows || p->sequences > 65536) return SCOPE_ERR_UNSUPPORTED;
   if (static_cast<int64_t>(p->heads) * p->rows_q >= (1LL << 31) || static_cast<int64_t>(p->kv_heads) * p->rows_k >= (1LL << 31))
     return SCOPE_ERR_UNSUPPORTED;
-  if (static_cast<int64_t>(p->heads / p->kv_heads) * p->rows_q > (1LL << 30)) return SCOPE_ERR_UNSUPPORTED;  // costs of 32 bits
+  // costs of 32 bits, and as many bytes of a key head's row statistics
+  if (static_cast<int64_t>(p->heads / p->kv_heads) * p->rows_q >= (1LL << 30)) return SCOPE_ERR_UNSUPPORTED;
   if (!scope::packed_launchable(p)) return SCOPE_ERR_UNSUPPORTED;
   return SCOPE_OK;
 }

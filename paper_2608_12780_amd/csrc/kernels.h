@@ -409,5 +409,6 @@ constexpr int kPackRows = 128;       // rows of a bf16 item by queries
 constexpr int kPackFewRows = 32;     // of one where sequences have few
 constexpr int kPackKeys = 128;       // keys of a bf16 item by keys
 constexpr int kPackRowsF32 = 64;     // rows, or keys, of an fp32 item
+constexpr int kPackThreads = 256;    // of a block of any of them
 
 }  // namespace scope

@@ -13,6 +13,7 @@ namespace scope {
 namespace {
 
 static_assert(kPackRowsF32 == kRows, "rows of a block");
+static_assert(kPackThreads == kThreads, "threads of a block");
 
 template <int D, bool GRAD>
 __global__ __launch_bounds__(kThreads)
@@ -217,7 +218,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_f32_kerne
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rg, d_o + r0 * D, 16, row_offset(row, a.group, a.d_o) + col, 0, 0, 0);
     }
     if (w < 2)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, q + T::kFloats + 64 * w, 4, 4 * min(index * kTile + lane, rows - 1), 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, q + T::kFloats + 64 * w, 4, 4u * static_cast<uint32_t>(min(index * kTile + lane, rows - 1)), 0, 0, 0);
   };
   auto compute = [&](const float *qt, const float *gt, int row0) {
     const float *st = qt + T::kFloats + 4 * g;

@@ -22,6 +22,7 @@ namespace scope {
 namespace {
 
 constexpr int kWaves = kPackKeys / 32;  // a wave owns 32 keys
+static_assert(64 * kWaves == kPackThreads, "threads of a block");
 
 // A tile's rows, 32 of them: 64 at d = 64 took as long, and at d = 128 would leave a CU
 // one block.
@@ -140,7 +141,7 @@ __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) void packed_keys_kernel(Pa
       }
     }
     if (w < 2)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, q + kStats + 2 * kPlane * w, 4, 4 * min(index * kRowTile + lane, rows - 1), 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, q + kStats + 2 * kPlane * w, 4, 4u * static_cast<uint32_t>(min(index * kRowTile + lane, rows - 1)), 0, 0, 0);
   };
 
   // 32 rows of a tile

@@ -384,16 +384,16 @@ size_t packed_workspace(const scope_pack *p, void *base, PackArgs *a, PackCall *
   return used;
 }
 
+// Fewer than 2^32 threads a launch.  Joins run for at most 1024 items of 128 rows, of 32
+// threads a row at most, and need no check.
 bool packed_launchable(const scope_pack *p) {
   PackArgs a{};
   PackCall c{};
   packed_workspace(p, nullptr, &a, &c);
-  auto fits = [](long long capacity, long long heads, int splits, int threads) {
-    return (capacity * splits + 7) / 8 * 8 * heads * threads < (1LL << 32);
+  auto fits = [p](long long capacity, int splits) {
+    return (capacity * splits + 7) / 8 * 8 * p->kv_heads * kPackThreads < (1LL << 32);
   };
-  return fits(c.by_rows.capacity, p->kv_heads, c.splits_rows, 512) && fits(c.forward.capacity, p->kv_heads, c.splits_forward, 256) && fits(c.by_keys.capacity, p->kv_heads, c.splits_keys, 256) &&
-         static_cast<long long>(p->heads) * p->rows_q * (p->d / 4) < (1LL << 32) - 1024 &&
-         static_cast<long long>(p->kv_heads) * p->rows_k * (p->d / 4) < (1LL << 32) - 1024;
+  return fits(c.by_rows.capacity, c.splits_rows) && fits(c.forward.capacity, c.splits_forward) && fits(c.by_keys.capacity, c.splits_keys);
 }
 
 hipError_t packed_forward(const PackArgs &a, const PackCall &c, hipStream_t s) {

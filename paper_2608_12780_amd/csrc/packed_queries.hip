@@ -32,6 +32,7 @@ namespace {
 
 constexpr float kLag = 8.0f;  // the running maximum may lag by 2^8
 constexpr int kWaves = kPackRows / 32;  // a wave owns 32 rows
+static_assert(64 * kWaves == kPackThreads, "threads of a block");
 
 // Wave w's share of a tile of keys' rows, 1 KB per load, through a resource that starts
 // at the tile (a sequence may be longer than 32-bit offsets reach); rows past the last
