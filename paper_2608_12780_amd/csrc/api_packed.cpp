@@ -12,13 +12,15 @@
 namespace {
 
 constexpr int kMaxRows = 1 << 24;
-constexpr int64_t kMaxStride = 1LL << 40;  // elements: products with rows stay in 64 bits
+constexpr int64_t kMaxStride = 1LL << 40;  // elements: products with heads stay in 64 bits
+constexpr int64_t kMaxRun = 1LL << 60;     // elements from the first row to the last
 
 // Elements from a tensor's first to past its last, or -1 where the strides are not
 // usable.  out: its rows must not overlap one another.
 int64_t extent(const scope_strides *t, int64_t heads, int64_t rows, int64_t d, bool out) {
   if (t->row < 0 || t->head < 0 || t->row > kMaxStride || t->head > kMaxStride) return -1;
   if (heads < 1 || rows < 1) return 0;
+  if (rows > 1 && t->row > kMaxRun / (rows - 1)) return -1;
   if (out) {
     if ((rows > 1 && t->row < d) || (heads > 1 && t->head < d)) return -1;
     const int64_t by_rows = (rows - 1) * t->row + d, by_heads = (heads - 1) * t->head + d;

@@ -56,3 +56,11 @@ def test_outputs_beside_the_other_tensor_are_taken(places):
     """They pass every check of memory: their number of rows alone is refused, after it."""
     n = 1 << 26
     assert call(n=n, **places(4 * n * D * 2)) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("row", [1 << 40, 1 << 39, (1 << 40) - 8])
+@pytest.mark.parametrize("name", ["xs", "ys"])
+def test_rows_out_of_64_bits_are_refused(name, row):
+    """2^24 or 2^25 steps of 2^39 or 2^40 elements: 0 modulo 2^64, or beyond 2^63."""
+    for n in ((1 << 24) + 1, (1 << 25) - 5, (1 << 25) + 1):
+        assert call(n=n, heads=(1, 0), **{name: (row, D)}) == INVALID, n
