@@ -372,7 +372,7 @@ size_t packed_workspace(const scope_pack *p, void *base, PackArgs *a, PackCall *
   if (a) {
     a->stats = stats;
     a->parts = parts;
-    a->ends = header + 2;
+    a->ends = header ? header + 2 : nullptr;
     c->by_rows = by_rows;
     c->forward = forward;
     c->splits_forward = splits_forward;
