@@ -506,8 +506,9 @@ int32_t scope_packed_workspace_size(const scope_pack *pack, size_t *bytes);
  *   lse_i = log sum_j exp(scale <q_i, k_j>)   (fp32, natural log; [heads][rows_q])
  *   O_i   = sum_j exp(scale <q_i, k_j> - lse_i) v_j,  j over the keys that i sees
  * (scale <= 0 selects 1/sqrt(d)).  A query that sees no key gives O = 0 and
- * lse = -inf.  Rows in no sequence are not read, those of O and lse as `clear` says.  Types as call 6 (fp32 inputs are not rounded, bf16 weights are); sums
- * and statistics are fp32.  A non-finite key row reaches only queries that see it; a
+ * lse = -inf.  Rows in no sequence are not read, those of O and lse as `clear` says.
+ * Types as call 6 (fp32 inputs are not rounded, bf16 weights are); sums and
+ * statistics are fp32.  A non-finite key row reaches only queries that see it; a
  * non-finite value row may also reach queries whose last key lies up to 94 before it.
  * Results repeat bit for bit.  Long sums may be cut into parts, whose number follows
  * from the sizes in `pack` alone.

@@ -355,15 +355,16 @@ struct PackRows {
   int64_t row, head;
 };
 // One list of work items, by falling cost: item i is a sequence's (first query row,
-// queries, first key row, keys) and (first row or key of the item, ..).  An item by
-// queries holds kRows rows (query, head of the group) of one key head.
+// queries, first key row, keys) and (first row or key of the item, unused).  An item by
+// queries holds rows (query, head of the group) of one key head.
 struct PackList {
   int4 *items;
   int rows;       // rows or keys of an item
   int capacity;   // items at most
 };
 struct PackArgs {
-  int kv_heads, group, rows_q, rows_k, sequences, causal, clear;
+  int kv_heads, group, rows_q, rows_k, sequences, causal;
+  int clear;  // output rows in no sequence are set to 0, lse to -inf
   PackRows q, k, v, o, d_o;  // o: gradients
   const int32_t *offsets_q, *offsets_k, *lengths_k;
   float scale, scale_log2;

@@ -3,8 +3,8 @@
 // nothing but the results is rounded.  A wave owns 16 rows (query, head of the group)
 // or keys, four waves a block; the other side's rows come 32 at a time through LDS.
 // The fp32 products run at a sixteenth of the bf16 rate and bound these kernels: 7
-// sequences of 356 to 1784 tokens, 4 heads in groups of 2, d = 128, dQ 101 us, dK and dV
-// 115, fp32 matrix pipe 64 to 66% busy.
+// sequences of 356 to 1784 tokens, 4 heads in groups of 2, d = 128, dQ 96 us, dK and dV
+// 108 (102 and 116 in the first calls after a pause), fp32 matrix pipe 63 to 66% busy.
 #include "attention_tile_f32.h"
 #include "packed.h"
 

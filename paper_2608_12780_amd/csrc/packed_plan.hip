@@ -134,7 +134,7 @@ __global__ __launch_bounds__(kThreads) void pack_lists_kernel(PackLists p) {
         const int place = atomicAdd(&hist[bin_of(sq, at)], 1);
         if (pass == 1 && place < list.capacity) {
           list.items[2 * place] = sq;
-          list.items[2 * place + 1] = make_int4(at, base + lo, 0, 0);
+          list.items[2 * place + 1].x = at;
         }
       }
       run_q = max(run_q, top_q);

@@ -8,8 +8,8 @@
 // position 2^24 is as exact as position 1.
 //
 // Bound by memory.  A 720p layer's queries and keys (24 + 24 heads x 118800 x 128 bf16)
-// take 560 us, 5.2 TB/s read and written, where a copy by torch reaches 4.8; gradients of
-// 5 + 5 heads x 32760, which leave the caches, 37 us (4.6 TB/s).  With at most 8 heads a
+// take 570 us, 5.1 TB/s read and written, where a copy by torch reaches 4.8; gradients of
+// 5 + 5 heads x 32760, which leave the caches, 36 us (4.6 TB/s).  With at most 8 heads a
 // thread and no loads ahead the gradients took 48, with at most 4 the layer 698: the
 // angles cost a thread about as much as 4 heads' rows.
 #include "common.h"

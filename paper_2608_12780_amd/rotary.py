@@ -23,8 +23,9 @@ def frequencies(length, theta=10000.0, scaling=None, context=4096):
       base    theta times s^(length / (length - 2)), which slows the slowest pair s
               times and leaves the fastest (length > 2);
       ramp    pairs that turn less than once over `context` divided by s, those
-              that turn more than 32 times left, between them in proportion; the
-              turned channels times 1 + 0.1 ln s."""
+              that turn more than 32 times left, between them in proportion to how
+              often they turn (not to their index); the turned channels times
+              1 + 0.1 ln s."""
     kind, s = scaling or (None, 1.0)
     if kind not in (None, "linear", "base", "ramp"):
         raise ValueError(f"scaling {kind!r}: linear, base or ramp")
