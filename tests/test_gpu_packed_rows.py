@@ -53,3 +53,29 @@ def test_2_to_the_28_rows():
         got = got.view(H, S, m, d)
         assert torch.equal(got, got[:, :1].expand_as(got)), name
         R.assert_within(name, got[:, 0], want, bound)
+
+
+def test_a_token_of_each_of_65536_sequences():
+    """Of 128 key heads: one key each, whose weight is 1, so that O is V, dV is dO, and the
+    other gradients are differences of two sums of the same d products."""
+    H, S, d = 128, 1 << 16, 64
+    g = torch.Generator(device="cuda").manual_seed(71)
+    q, k, v, d_o = (torch.randn(H, S, d, generator=g, device="cuda").bfloat16() for _ in range(4))
+    a = packed.PackedAttention(H, H, S, S, d, S)
+    off = packed.offsets_of([1] * S)
+    G.say("[packed rows] tokens forward")
+    out, lse = a.forward(q, k, v, off)
+    assert torch.equal(out, v)
+    G.say("[packed rows] tokens backward")
+    dq, dk, dv = a.backward(q, k, v, out, lse, d_o, off)
+    assert torch.equal(dv, d_o)
+    scale, U = d ** -0.5, R.U
+    for h in range(H):
+        s = (q[h].double() * k[h].double()).sum(1) * scale
+        e = (d + 8) * U * scale * (q[h].double() * k[h].double()).abs().sum(1) + 12 * U * s.abs() + 8 * U
+        assert ((lse[h].double() - s).abs() <= e).all(), h
+        # |ds| at most the errors of <d_o, v> and <d_o, o>; p and roundings within 5%
+        ds = 1.05 * 2 * (d + 8) * U * (d_o[h].double() * v[h].double()).abs().sum(1, keepdim=True)
+        assert (dq[h].double().abs() <= scale * ds * k[h].double().abs() + 1e-30).all(), h
+        assert (dk[h].double().abs() <= scale * ds * q[h].double().abs() + 1e-30).all(), h
+    assert int(a.status) == 0
